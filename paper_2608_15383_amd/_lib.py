@@ -1,4 +1,4 @@
-"""ctypes declarations of libexactmoe.so (include/exactmoe.h).
+"""ctypes declarations of libexactmoe.so (include/exactmoe*.h).
 
 Argument marshalling only: every step of the layer runs in the library.
 Loading fails loudly when the library has not been built.
@@ -19,6 +19,8 @@ EMOE_PATH_AUTO, EMOE_PATH_GEMV, EMOE_PATH_MFMA, EMOE_PATH_MIXED = 0, 1, 2, 3
 EMOE_MIXED_MFMA_ROWS = 16
 EMOE_GEMV_MAX_TOKENS = 4
 EMOE_NOALLOC_SCRATCH_BYTES = 32 << 20
+EMOE_F32, EMOE_BF16, EMOE_F16, EMOE_E4M3 = 0, 1, 2, 3
+EMOE_SERVING_TICKET_BYTES = 16384
 
 
 class Dims(C.Structure):
@@ -55,13 +57,48 @@ class DecoderWeights(C.Structure):
                 ("w_router", C.POINTER(C.c_void_p))]
 
 
+class PagedKVView(C.Structure):  # emoe_paged_kv
+    _fields_ = ([(n, C.c_void_p) for n in ("k_pages", "v_pages", "k_scale", "v_scale")]
+                + [(n, C.c_int64) for n in ("page_stride", "slot_stride", "head_stride")]
+                + [(n, C.c_int32) for n in ("dtype", "n_pages", "page_size", "n_kv_heads",
+                                            "head_dim")])
+
+
+class PagedAppendArgs(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "k", "v", "q_out", "positions", "seqs",
+                                           "page_table", "inv_freq")]
+                + [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride",
+                                            "table_stride")]
+                + [(n, C.c_int32) for n in ("dtype", "tokens", "n_heads", "n_seqs", "table_width",
+                                            "rotary_dim", "interleaved")])
+
+
+class PagedAttentionArgs(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "out", "lse", "lengths", "seqs", "page_table")]
+                + [(n, C.c_int64) for n in ("q_stride", "out_stride", "table_stride")]
+                + [("scale", C.c_float)]
+                + [(n, C.c_int32) for n in ("dtype", "rows", "n_heads", "n_seqs", "table_width",
+                                            "max_keys", "window")])
+
+
+class LogitsArgs(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("logits", "out", "next_token", "history",
+                                           "history_lengths", "prompt_lengths", "repetition",
+                                           "presence", "frequency", "bias_ids", "bias_values",
+                                           "bias_counts", "mask", "mask_rows")]
+                + [(n, C.c_int64) for n in ("logits_stride", "out_stride", "history_stride",
+                                            "bias_stride", "mask_stride")]
+                + [(n, C.c_int32) for n in ("dtype", "rows", "vocab", "history_width",
+                                            "bias_width", "n_masks")])
+
+
 _vp = C.c_void_p
 _i32 = C.c_int32
 _i32p = C.POINTER(C.c_int32)
 _i64p = C.POINTER(C.c_int64)
 _dimsp = C.POINTER(Dims)
 
-# name -> (restype, argtypes); mirrors include/exactmoe.h
+# name -> (restype, argtypes); mirrors include/exactmoe.h, exactmoe_decoder.h, exactmoe_serving.h
 SIGNATURES = {
     "emoe_status_string": (C.c_char_p, [_i32]),
     "emoe_last_error": (C.c_char_p, []),
@@ -101,6 +138,13 @@ SIGNATURES = {
     "emoe_test_set_step_keys": (_i32, [_vp, _i32]),
     "emoe_decoder_forward": (_i32, [_vp, _vp, _i32, _i32, _vp, _vp, _vp, C.c_size_t, _vp,
                                     C.POINTER(Stats)]),
+    "emoe_check_paged_kv": (_i32, [C.POINTER(PagedKVView)]),
+    "emoe_paged_append": (_i32, [C.POINTER(PagedKVView), C.POINTER(PagedAppendArgs), _vp]),
+    "emoe_paged_attention_workspace_bytes": (C.c_size_t, [C.POINTER(PagedKVView), _i32, _i32, _i32]),
+    "emoe_paged_attention": (_i32, [C.POINTER(PagedKVView), C.POINTER(PagedAttentionArgs), _vp,
+                                    C.c_size_t, _vp]),
+    "emoe_process_logits_workspace_bytes": (C.c_size_t, [_i32, _i32]),
+    "emoe_process_logits": (_i32, [C.POINTER(LogitsArgs), _vp, C.c_size_t, _vp]),
     "emoe_profile_begin": (_i32, [_i32]),
     "emoe_profile_end": (_i32, [_vp, _vp, _i32, _i32p]),
 }
