@@ -16,7 +16,7 @@ struct KvView {
   uint8_t *k, *v;
   const float *k_scale, *v_scale;
   int64_t page_bytes;
-  int32_t slot_bytes, head_bytes;
+  int32_t slot_bytes, head_bytes;  // below 2^30, as a page is
   int32_t n_pages, page_log2, n_kv_heads;
 };
 
@@ -153,86 +153,533 @@ struct AttendArg {
   uint16_t* out;
   float* lse;
   const int32_t *lengths, *seqs, *table;
+  uint32_t* tickets;
+  float* parts;
   int64_t q_stride, out_stride, table_stride;
   float scale;
-  int32_t rows, n_heads, n_seqs, table_width, max_keys, window;
+  int32_t row0, rows, n_heads, group, q_tiles, n_seqs, table_width, max_keys, window;
+  int32_t workers, part_floats;
 };
 
-template <class T, bool kE4M3>
-__device__ __forceinline__ float cache_value(const uint8_t* p, int i) {
-  if constexpr (kE4M3) return __builtin_amdgcn_cvt_f32_fp8((int)p[i], 0);
-  else return T::up(reinterpret_cast<const uint16_t*>(p)[i]);
-}
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-// One workgroup per (query head, row): tiles of 256 keys, a thread per key for
-// the scores and a thread per (dimension, key stripe) for the output, with the
-// running maximum and sum of the softmax.
-template <class T, bool kE4M3, int kDh>
-__global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) {
-  constexpr int kStripes = kThreads / kDh;
-  __shared__ float qs[kDh], ps[kThreads], red[4], part[kStripes][kDh];
-  __shared__ int64_t at[kThreads];
-  const int h = blockIdx.x % a.n_heads, r = blockIdx.x / a.n_heads, tid = threadIdx.x;
-  const int g = h / (a.n_heads / a.kv.n_kv_heads);
-  const int s = a.seqs ? a.seqs[r] : r;
+// The 16-bit type's matrix instruction (16 x 16 outputs, 32 products each) and
+// its pairs: of two floats, and of two E4M3 values (exact) of a dword's half.
+template <class T>
+struct Half16;
+template <>
+struct Half16<Bf16> {
+  __device__ static __forceinline__ f32x4 mfma(uint4 a, uint4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  template <bool kHi>
+  __device__ static __forceinline__ uint32_t from_e4m3(uint32_t w) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, kHi));
+  }
+};
+template <>
+struct Half16<Fp16> {
+  __device__ static __forceinline__ f32x4 mfma(uint4 a, uint4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+  template <bool kHi>
+  __device__ static __forceinline__ uint32_t from_e4m3(uint32_t w) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, kHi));
+  }
+};
+
+constexpr int kTileKeys = 32;   // keys of one wavefront's step
+constexpr int kAttnWaves = 4;
+constexpr int kUnitKeys = kTileKeys * kAttnWaves;
+constexpr int kMaxRows = 1024;  // rows of one launch
+constexpr int kMaxWorkers = EMOE_SERVING_TICKET_BYTES / 4;
+
+typedef const __attribute__((address_space(4))) int32_t* ConstI32;
+
+// 2^x by the hardware instruction (1 ulp; denormal results are 0).
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The keys that row `row` of the call sees: [first, n).
+struct Span {
+  int first, n, seq;
+};
+__device__ __forceinline__ Span span_of(const AttendArg& a, int row) {
+  Span s;
+  s.seq = a.seqs ? a.seqs[row] : row;
   int n = 0;
-  if ((uint32_t)s < (uint32_t)a.n_seqs) {
-    n = max(0, min(a.lengths[r], a.max_keys));
+  if ((uint32_t)s.seq < (uint32_t)a.n_seqs) {
+    n = max(0, min(a.lengths[row], a.max_keys));
     n = (int)min((int64_t)n, (int64_t)a.table_width << a.kv.page_log2);
   }
-  const int first = a.window > 0 ? max(0, n - a.window) : 0;
-  if (tid < kDh) qs[tid] = T::up(a.q[r * a.q_stride + (int64_t)h * kDh + tid]);
-  const float scale = a.scale * (kE4M3 && a.kv.k_scale ? a.kv.k_scale[g] : 1.0f);
-  float m = -INFINITY, l = 0.f, acc = 0.f;
-  const int dim = tid % kDh, stripe = tid / kDh;
-  for (int base = first; base < n; base += kThreads) {
-    const int j = base + tid;
-    int64_t off = -1;
-    float z = -INFINITY;
-    __syncthreads();
-    if (j < n) {
-      const int page = a.table[(int64_t)s * a.table_stride + (j >> a.kv.page_log2)];
-      if ((uint32_t)page < (uint32_t)a.kv.n_pages) {
-        off = page * a.kv.page_bytes + (int64_t)(j & ((1 << a.kv.page_log2) - 1)) * a.kv.slot_bytes +
-              (int64_t)g * a.kv.head_bytes;
-        z = 0.f;
-        for (int i = 0; i < kDh; ++i) z = fmaf(qs[i], cache_value<T, kE4M3>(a.kv.k + off, i), z);
-        z *= scale;
+  s.n = n;
+  s.first = a.window > 0 ? max(0, n - a.window) : 0;
+  return s;
+}
+// Its units of kUnitKeys keys, from the tile of its first key on; a row
+// without keys has one, which writes its zeros.
+__device__ __forceinline__ int units_of(int first, int n) {
+  const int t0 = first / kTileKeys, t1 = (n + kTileKeys - 1) / kTileKeys;
+  return max(1, (t1 - t0 + kAttnWaves - 1) / kAttnWaves);
+}
+
+// One tile of 32 keys of one key head, as the matrix instructions take it.
+//
+// Scores: S^T [key][query] = K Q^T.  The A operand's lane (l16, g) holds 8
+// dimensions of key l16 of a half tile, which is 16 bytes as they lie in the
+// cache (of E4M3: 16 dimensions, for two steps); any dimensions do, as long as
+// the query's lanes hold the same.  The result's lane (l16, g) has the scores
+// of keys 4g .. 4g+3 of each half for query l16.
+// Output: O^T [dim][query] = V^T P^T.  The B operand's lane wants 8 keys of
+// its query, and again any order of keys does: those 4g .. 4g+3 of both
+// halves, so the scores become weights in the registers that they are in.  The
+// A operand's lane wants the same 8 keys of one dimension; it loads kDh / 16
+// consecutive dimensions of each and transposes the 8 x 2 pairs with byte
+// permutes (32 of them per tile at 128 dimensions), which keeps values out of
+// LDS.  A query's running maximum, sum and output columns all live in lanes
+// l16 = query, so nothing is exchanged between lanes in the loop.
+template <class T, bool kE4M3, int kDh>
+struct Tile {
+  typedef Half16<T> H16;
+  static constexpr int kSteps = kDh / 32;
+  static constexpr int kItem = kE4M3 ? 1 : 2;
+  static constexpr int kKLoads = kDh * kItem / 64;  // 16-byte loads per key half
+  static constexpr int kDims = kDh / 16;            // output dimensions of a lane
+  static constexpr int kVWords = kDims * kItem / 4;
+  static constexpr bool kSplitV = !kE4M3 && kDh == 256;  // two 16-byte loads, 256 bytes apart
+
+  uint4 k[2][kKLoads];
+  uint32_t v[8][kVWords];
+
+  // The first of the 8 dimensions that lane group g holds in step c.
+  __device__ static __forceinline__ int q_dim(int c, int g) {
+    return kE4M3 ? 16 * (4 * (c >> 1) + g) + 8 * (c & 1) : 8 * (4 * c + g);
+  }
+  // Output dimension of matrix row m of accumulator c.
+  __device__ static __forceinline__ int out_dim(int m, int c) {
+    return kSplitV ? 128 * (c >> 3) + 8 * m + (c & 7) : kDims * m + c;
+  }
+
+  __device__ __forceinline__ void load_k(const uint8_t* const (&at)[2], int lane) {
+    const int off = 16 * (lane >> 4);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int c = 0; c < kKLoads; ++c)
+        k[h][c] = *reinterpret_cast<const uint4*>(at[h] + off + 64 * c);
+  }
+  __device__ __forceinline__ void load_v(const uint8_t* const (&at)[2], int slot_bytes, int lane) {
+    const int off = (kSplitV ? 16 : kVWords * 4) * (lane & 15);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint8_t* p = at[j >> 2] + (int64_t)(j & 3) * slot_bytes + off;
+      if constexpr (kVWords == 1) {
+        v[j][0] = *reinterpret_cast<const uint32_t*>(p);
+      } else if constexpr (kVWords == 2) {
+        const uint2 w = *reinterpret_cast<const uint2*>(p);
+        v[j][0] = w.x, v[j][1] = w.y;
+      } else {
+#pragma unroll
+        for (int u = 0; u < kVWords / 4; ++u) {
+          const uint4 w = *reinterpret_cast<const uint4*>(p + 256 * u);
+          v[j][4 * u] = w.x, v[j][4 * u + 1] = w.y, v[j][4 * u + 2] = w.z, v[j][4 * u + 3] = w.w;
+        }
       }
     }
-    at[tid] = off;
-    float mx = z;
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-    if ((tid & 63) == 0) red[tid >> 6] = mx;
-    __syncthreads();
-    const float m2 = fmaxf(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])), m);
-    const float ref = m2 == -INFINITY ? 0.f : m2;
-    const float p = off >= 0 ? expf(z - ref) : 0.f;
-    const float shrink = expf(m - ref);
-    m = m2;
-    ps[tid] = p;
-    float sum = p;
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
-    __syncthreads();
-    if ((tid & 63) == 0) red[tid >> 6] = sum;
-    __syncthreads();
-    l = l * shrink + ((red[0] + red[1]) + (red[2] + red[3]));
-    acc *= shrink;
-    for (int i = stripe; i < min(kThreads, n - base); i += kStripes)
-      if (at[i] >= 0) acc = fmaf(ps[i], cache_value<T, kE4M3>(a.kv.v + at[i], dim), acc);
   }
-  part[stripe][dim] = acc;
-  __syncthreads();
-  if (tid < kDh) {
-    float o = 0.f;
-    for (int i = 0; i < kStripes; ++i) o += part[i][tid];
-    o = l == 0.f ? 0.f : o / l;
-    if (kE4M3 && a.kv.v_scale) o *= a.kv.v_scale[g];
-    a.out[r * a.out_stride + (int64_t)h * kDh + tid] = (uint16_t)T::down(o);
+  __device__ __forceinline__ void scores(const uint4 (&q)[kSteps], f32x4 (&s)[2]) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < kSteps; ++c)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint4 a;
+        if constexpr (kE4M3) {
+          const uint4 w = k[h][c >> 1];
+          const uint32_t lo = (c & 1) ? w.z : w.x, hi = (c & 1) ? w.w : w.y;
+          a = make_uint4(H16::template from_e4m3<false>(lo), H16::template from_e4m3<true>(lo),
+                         H16::template from_e4m3<false>(hi), H16::template from_e4m3<true>(hi));
+        } else {
+          a = k[h][c];
+        }
+        s[h] = H16::mfma(a, q[c], s[h]);
+      }
   }
-  if (tid == 0 && a.lse) a.lse[(int64_t)r * a.n_heads + h] = l == 0.f ? -INFINITY : m + logf(l);
+  // Values of keys that are not there become 0: a weight of 0 does not undo a NaN.
+  __device__ __forceinline__ void clear_v(uint32_t there) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int w = 0; w < kVWords; ++w) v[j][w] = (there >> j) & 1 ? v[j][w] : 0u;
+  }
+  // The pair of dimensions (2w, 2w + 1) of key j.
+  template <int kW>
+  __device__ __forceinline__ uint32_t pair(int j) const {
+    if constexpr (kE4M3) return H16::template from_e4m3<(kW & 1) != 0>(v[j][kW >> 1]);
+    else return v[j][kW];
+  }
+  template <int kW>
+  __device__ __forceinline__ void add_pair(uint4 hi, uint4 lo, f32x4 (&acc)[kDims]) const {
+    uint32_t e[4], o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t a = pair<kW>(2 * i), b = pair<kW>(2 * i + 1);
+      e[i] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+      o[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    }
+    const uint4 ve = make_uint4(e[0], e[1], e[2], e[3]), vo = make_uint4(o[0], o[1], o[2], o[3]);
+    acc[2 * kW] = H16::mfma(ve, hi, acc[2 * kW]);
+    acc[2 * kW + 1] = H16::mfma(vo, hi, acc[2 * kW + 1]);
+    acc[2 * kW] = H16::mfma(ve, lo, acc[2 * kW]);
+    acc[2 * kW + 1] = H16::mfma(vo, lo, acc[2 * kW + 1]);
+    if constexpr (kW + 1 < kDims / 2) add_pair<kW + 1>(hi, lo, acc);
+  }
+};
+
+// The pages of a tile's four octets of keys (a page has 8 slots or more).
+struct Octets {
+  int32_t page[4];
+};
+__device__ __forceinline__ Octets octets_of(const AttendArg& a, ConstI32 table, int key0, int n) {
+  Octets o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int j = key0 + 8 * i;
+    o.page[i] = j < n ? table[j >> a.kv.page_log2] : -1;
+  }
+  return o;
+}
+
+// Split over the caches' lengths: all rows' units of 128 keys, times key heads
+// (and tiles of 16 query heads), stand in one line; each of up to `workers`
+// workgroups takes an equal run of it, whatever the rows' lengths are, and its
+// four wavefronts every fourth tile.  The outputs that a run covers whole it
+// writes; of the others (at most its first and its last) it leaves maximum,
+// sum and unscaled output in the workspace, and the last of such an output's
+// workgroups to finish joins them in the order of the line.  Bound by HBM: per
+// tile and wavefront 16 KB (16-bit, 128 dimensions) against about 130 vector
+// and 24 matrix instructions.
+template <class T, bool kE4M3, int kDh>
+__global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) {
+  typedef Tile<T, kE4M3, kDh> Tl;
+  constexpr int kRow = kDh + 4;  // padded: lanes 16 apart in dimensions, 1 in queries
+  __shared__ int pre[kMaxRows + 1], len[kMaxRows], seq[kMaxRows];
+  __shared__ int wave_sum[kThreads / 64];
+  __shared__ float ms[kAttnWaves][16], ls[kAttnWaves][16];
+  __shared__ __attribute__((aligned(16))) float os[kAttnWaves][16][kRow];
+  __shared__ int last;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+
+  // Units before each row.
+  {
+    const int per = (a.rows + kThreads - 1) / kThreads, r0 = tid * per;
+    int cnt[kMaxRows / kThreads], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kMaxRows / kThreads; ++i) {
+      cnt[i] = 0;
+      if (i < per && r0 + i < a.rows) {
+        const Span s = span_of(a, a.row0 + r0 + i);
+        len[r0 + i] = s.n;
+        seq[r0 + i] = s.seq;
+        cnt[i] = units_of(s.first, s.n);
+      }
+      sum += cnt[i];
+    }
+    int incl = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int t = __shfl_up(incl, d);
+      if (lane >= d) incl += t;
+    }
+    if (lane == 63) wave_sum[wave] = incl;
+    __syncthreads();
+    int at = incl - sum;
+    for (int w = 0; w < wave; ++w) at += wave_sum[w];
+#pragma unroll
+    for (int i = 0; i < kMaxRows / kThreads; ++i) {
+      if (i < per && r0 + i < a.rows) pre[r0 + i] = at;
+      at += cnt[i];
+    }
+    if (tid == 0) {
+      int all = 0;
+      for (int w = 0; w < kThreads / 64; ++w) all += wave_sum[w];
+      pre[a.rows] = all;
+    }
+    __syncthreads();
+  }
+  const int Y = a.kv.n_kv_heads * a.q_tiles;
+  const int total = __builtin_amdgcn_readfirstlane(pre[a.rows]) * Y;
+  const int run = (total + a.workers - 1) / a.workers;  // units per workgroup
+  const int w = blockIdx.x;
+  if ((int64_t)w * run >= total) return;
+  const int u_end = min((w + 1) * run, total);
+  int u = w * run;
+  bool first_segment = true;
+  int row = 0;
+  {
+    int hi = a.rows;  // pre[row] <= u / Y < pre[hi]
+    const int key = u / Y;
+    while (hi - row > 1) {
+      const int mid = (row + hi) >> 1;
+      if (pre[mid] <= key) row = mid; else hi = mid;
+    }
+  }
+  while (u < u_end) {
+    row = __builtin_amdgcn_readfirstlane(row);
+    const int base = __builtin_amdgcn_readfirstlane(pre[row]);
+    const int units = __builtin_amdgcn_readfirstlane(pre[row + 1]) - base;
+    const int n = __builtin_amdgcn_readfirstlane(len[row]);
+    const int sq = __builtin_amdgcn_readfirstlane(seq[row]);
+    const int y = (u - base * Y) / units, c0 = (u - base * Y) % units;
+    const int c1 = min(units, c0 + (u_end - u));
+    const int first = a.window > 0 ? max(0, n - a.window) : 0;
+    const int hk = y / a.q_tiles, qt = y % a.q_tiles;
+    const int head0 = hk * a.group + qt * 16;
+    const int heads = min(16, a.group - qt * 16);
+    const int64_t grow = a.row0 + row;
+
+    uint4 q[Tl::kSteps];
+#pragma unroll
+    for (int c = 0; c < Tl::kSteps; ++c) {
+      q[c] = make_uint4(0, 0, 0, 0);
+      if (l16 < heads)
+        q[c] = *reinterpret_cast<const uint4*>(a.q + grow * a.q_stride +
+                                               (int64_t)(head0 + l16) * kDh + Tl::q_dim(c, g));
+    }
+    float scale = a.scale * 1.4426950408889634f;
+    if (kE4M3 && a.kv.k_scale) scale *= a.kv.k_scale[hk];
+
+    f32x4 acc[Tl::kDims];
+#pragma unroll
+    for (int c = 0; c < Tl::kDims; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+
+    const int t0 = first / kTileKeys;
+    const int t_end = min(t0 + c1 * kAttnWaves, (n + kTileKeys - 1) / kTileKeys);
+    int t = t0 + c0 * kAttnWaves + wave;
+    const ConstI32 table = (ConstI32)(a.table + (int64_t)sq * a.table_stride);
+    const uint8_t* kbase = a.kv.k + (int64_t)hk * a.kv.head_bytes;
+    const uint8_t* vbase = a.kv.v + (int64_t)hk * a.kv.head_bytes;
+    const int slot_mask = (1 << a.kv.page_log2) - 1;
+
+    // Byte offsets of the tile's octets (of page 0 where there is no page: any
+    // place that may be read), and of this lane's keys in each half.
+    auto place = [&](const Octets& o, int key0, int64_t (&off)[4]) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int page = (uint32_t)o.page[i] < (uint32_t)a.kv.n_pages ? o.page[i] : 0;
+        off[i] = page * a.kv.page_bytes + (int64_t)((key0 + 8 * i) & slot_mask) * a.kv.slot_bytes;
+      }
+    };
+    Tl tile;
+    auto load_k = [&](const int64_t (&off)[4]) {
+      const uint8_t* at[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        at[h] = kbase + (l16 < 8 ? off[2 * h] : off[2 * h + 1]) + (l16 & 7) * a.kv.slot_bytes;
+      tile.load_k(at, lane);
+    };
+    auto load_v = [&](const int64_t (&off)[4]) {
+      const uint8_t* at[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        at[h] = vbase + (g < 2 ? off[2 * h] : off[2 * h + 1]) + 4 * (g & 1) * a.kv.slot_bytes;
+      tile.load_v(at, a.kv.slot_bytes, lane);
+    };
+
+    Octets now, next;
+    int64_t off[4];
+    if (t < t_end) {
+      now = octets_of(a, table, t * kTileKeys, n);
+      place(now, t * kTileKeys, off);
+      load_k(off);
+      load_v(off);
+      if (t + kAttnWaves < t_end) next = octets_of(a, table, (t + kAttnWaves) * kTileKeys, n);
+    }
+    while (t < t_end) {
+      const int key0 = t * kTileKeys, tn = t + kAttnWaves;
+      const bool more = tn < t_end;
+      f32x4 s[2];
+      tile.scores(q, s);
+      if (more) {
+        place(next, tn * kTileKeys, off);
+        load_k(off);
+      }
+      float z[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z[j] = s[j >> 2][j & 3] * scale;
+      bool whole = key0 >= first && key0 + kTileKeys <= n;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) whole = whole && (uint32_t)now.page[i] < (uint32_t)a.kv.n_pages;
+      if (!whole) {
+        uint32_t there = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int key = key0 + 16 * (j >> 2) + 4 * g + (j & 3);
+          const int page = g < 2 ? now.page[2 * (j >> 2)] : now.page[2 * (j >> 2) + 1];
+          if (key >= first && key < n && (uint32_t)page < (uint32_t)a.kv.n_pages) there |= 1u << j;
+          else z[j] = -INFINITY;
+        }
+        tile.clear_v(there);
+      }
+      // The maximum that the weights refer to moves only when a score exceeds
+      // it by 2^8: until then they stay below 256, and nothing is rescaled.
+      float top = z[0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) top = fmaxf(top, z[j]);
+      if (__any(top > m + 8.f)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m2 = fmaxf(m, top);
+        const float shrink = m2 == -INFINITY ? 0.f : exp2_hw(m - m2);
+        m = m2;
+        l *= shrink;
+#pragma unroll
+        for (int c = 0; c < Tl::kDims; ++c) acc[c] *= shrink;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+      // Weights in two 16-bit halves: what the first one's rounding leaves is
+      // the second, so the products see 16 bits of bf16 weights instead of 8.
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p0 = exp2_hw(z[2 * j] - ref), p1 = exp2_hw(z[2 * j + 1] - ref);
+        l += p0;
+        l += p1;
+        const uint32_t h0 = T::down(p0), h1 = T::down(p1);
+        hi[j] = h0 | (h1 << 16);
+        lo[j] = T::down(p0 - T::up(h0)) | (T::down(p1 - T::up(h1)) << 16);
+      }
+      tile.template add_pair<0>(make_uint4(hi[0], hi[1], hi[2], hi[3]),
+                                make_uint4(lo[0], lo[1], lo[2], lo[3]), acc);
+      if (more) {
+        load_v(off);
+        now = next;
+        if (tn + kAttnWaves < t_end) next = octets_of(a, table, (tn + kAttnWaves) * kTileKeys, n);
+      }
+      t = tn;
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+
+    // Join the wavefronts.
+    __syncthreads();  // the last segment's readers are done
+    if (g == 0) {
+      ms[wave][l16] = m;
+      ls[wave][l16] = l;
+    }
+    __syncthreads();
+    float M = ms[0][l16];
+#pragma unroll
+    for (int i = 1; i < kAttnWaves; ++i) M = fmaxf(M, ms[i][l16]);
+    const float mine = m == -INFINITY ? 0.f : exp2_hw(m - M);
+    if (l16 < heads) {
+#pragma unroll
+      for (int c = 0; c < Tl::kDims; c += 4)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<float4*>(&os[wave][l16][Tl::out_dim(4 * g + i, c)]) =
+              make_float4(acc[c][i] * mine, acc[c + 1][i] * mine, acc[c + 2][i] * mine,
+                          acc[c + 3][i] * mine);
+    }
+    __syncthreads();
+    const bool full = c0 == 0 && c1 == units;
+    // Maximum and sum of query h over the wavefronts.
+    auto join = [&](int h, float& M, float& L) {
+      M = ms[0][h];
+      for (int i = 1; i < kAttnWaves; ++i) M = fmaxf(M, ms[i][h]);
+      L = 0.f;
+      for (int i = 0; i < kAttnWaves; ++i)
+        L += ms[i][h] == -INFINITY ? 0.f : ls[i][h] * exp2_hw(ms[i][h] - M);
+    };
+    const float vs = kE4M3 && a.kv.v_scale ? a.kv.v_scale[hk] : 1.f;
+    auto store_out = [&](int h, int d, float4 o, float M, float L) {
+      const float inv = L == 0.f ? 0.f : vs / L;
+      uint2 r;
+      r.x = T::down(o.x * inv) | (T::down(o.y * inv) << 16);
+      r.y = T::down(o.z * inv) | (T::down(o.w * inv) << 16);
+      *reinterpret_cast<uint2*>(a.out + grow * a.out_stride + (int64_t)(head0 + h) * kDh + d) = r;
+      if (d == 0 && a.lse)
+        a.lse[grow * a.n_heads + head0 + h] =
+            L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    };
+    const int u0 = base * Y + y * units;  // this output's first unit
+    float* part = a.parts + (int64_t)(2 * w + (first_segment ? 0 : 1)) * a.part_floats;
+    for (int x = tid; x < heads * (kDh / 4); x += kThreads) {
+      const int h = x / (kDh / 4), d = 4 * (x % (kDh / 4));
+      float4 o = *reinterpret_cast<const float4*>(&os[0][h][d]);
+#pragma unroll
+      for (int i = 1; i < kAttnWaves; ++i) {
+        const float4 e = *reinterpret_cast<const float4*>(&os[i][h][d]);
+        o.x += e.x, o.y += e.y, o.z += e.z, o.w += e.w;
+      }
+      float M, L;
+      if (full || d == 0) join(h, M, L);
+      if (full) {
+        store_out(h, d, o, M, L);
+      } else {
+        uint64_t* p = reinterpret_cast<uint64_t*>(part + 32 + h * kDh + d);
+        const uint64_t a0 = (uint64_t)__float_as_uint(o.x) | ((uint64_t)__float_as_uint(o.y) << 32);
+        const uint64_t a1 = (uint64_t)__float_as_uint(o.z) | ((uint64_t)__float_as_uint(o.w) << 32);
+        __hip_atomic_store(p, a0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(p + 1, a1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (d == 0) {
+          st_u32<true>(part + h, __float_as_uint(M));
+          st_u32<true>(part + 16 + h, __float_as_uint(L));
+        }
+      }
+    }
+    if (!full) {
+      const int wa = u0 / run, wb = (u0 + units - 1) / run;
+      wait_memory();
+      __syncthreads();
+      if (tid == 0) {
+        last = __hip_atomic_fetch_add(&a.tickets[wa], 1u, __ATOMIC_RELAXED,
+                                      __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(wb - wa);
+        wait_memory();
+      }
+      __syncthreads();
+      if (last) {
+        const int parts = wb - wa + 1;
+        const int lead = u0 % run ? 1 : 0;  // the first one's last segment, or its first
+        auto part_at = [&](int i) {
+          return a.parts + (int64_t)(2 * (wa + i) + (i == 0 ? lead : 0)) * a.part_floats;
+        };
+        for (int x = tid; x < heads * (kDh / 4); x += kThreads) {
+          const int h = x / (kDh / 4), d = 4 * (x % (kDh / 4));
+          float M = -INFINITY;
+          for (int i = 0; i < parts; ++i) M = fmaxf(M, __uint_as_float(ld_u32<true>(part_at(i) + h)));
+          float L = 0.f;
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int i = 0; i < parts; ++i) {
+            const float* p = part_at(i);
+            const float mi = __uint_as_float(ld_u32<true>(p + h));
+            const float f = mi == -INFINITY ? 0.f : exp2_hw(mi - M);
+            L += f * __uint_as_float(ld_u32<true>(p + 16 + h));
+            const uint64_t* v = reinterpret_cast<const uint64_t*>(p + 32 + h * kDh + d);
+            const uint64_t a0 = __hip_atomic_load(v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const uint64_t a1 = __hip_atomic_load(v + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            o.x = fmaf(f, __uint_as_float((uint32_t)a0), o.x);
+            o.y = fmaf(f, __uint_as_float((uint32_t)(a0 >> 32)), o.y);
+            o.z = fmaf(f, __uint_as_float((uint32_t)a1), o.z);
+            o.w = fmaf(f, __uint_as_float((uint32_t)(a1 >> 32)), o.w);
+          }
+          store_out(h, d, o, M, L);
+        }
+        if (tid == 0) st_u32<true>(&a.tickets[wa], 0);
+      }
+    }
+    u += c1 - c0;
+    if (c1 == units && y == Y - 1) ++row;
+    first_segment = false;
+  }
 }
 
 // ---------------------------------------------------------------- checks
@@ -338,13 +785,33 @@ void launch_append(const AppendArg& a, int head_dim, bool inter, dim3 grid, hipS
 
 template <class T, bool kE4M3>
 void launch_attend(const AttendArg& a, int head_dim, hipStream_t stream) {
-  const dim3 grid((unsigned)(a.n_heads * a.rows));
+  const dim3 grid(a.workers);
   if (head_dim == 64)
     hipLaunchKernelGGL((paged_attention_kernel<T, kE4M3, 64>), grid, dim3(kThreads), 0, stream, a);
   else if (head_dim == 128)
     hipLaunchKernelGGL((paged_attention_kernel<T, kE4M3, 128>), grid, dim3(kThreads), 0, stream, a);
   else
     hipLaunchKernelGGL((paged_attention_kernel<T, kE4M3, 256>), grid, dim3(kThreads), 0, stream, a);
+}
+
+// How a call is launched: rows per launch (their units stay below 2^31), its
+// workgroups, and the floats of one workgroup's record for a split output.
+struct AttendPlan {
+  int64_t rows_per_launch;
+  int workers, part_floats;
+};
+constexpr int kWorkers = 768;  // three workgroups per CU
+AttendPlan attend_plan(const emoe_paged_kv& kv, int32_t rows, int32_t n_heads, int32_t max_keys) {
+  const int group = n_heads / kv.n_kv_heads;
+  const int64_t lines = (int64_t)kv.n_kv_heads * ((group + 15) / 16);
+  const int64_t most = lines * ((int64_t)max_keys / kUnitKeys + 2);  // units of one row
+  AttendPlan p;
+  p.rows_per_launch = (((int64_t)1 << 31) - 1 - kMaxWorkers) / most;
+  if (p.rows_per_launch > kMaxRows) p.rows_per_launch = kMaxRows;
+  const int64_t held = rows < p.rows_per_launch ? rows : p.rows_per_launch;
+  p.workers = (int)(held * most < kWorkers ? held * most : kWorkers);
+  p.part_floats = 32 + (group < 16 ? group : 16) * kv.head_dim;
+  return p;
 }
 
 }  // namespace
@@ -419,7 +886,8 @@ int32_t emoe_paged_append(const emoe_paged_kv* kv, const emoe_paged_append_args*
 size_t emoe_paged_attention_workspace_bytes(const emoe_paged_kv* kv, int32_t rows, int32_t n_heads,
                                             int32_t max_keys) {
   if (check_kv(kv) || rows < 0 || n_heads < 1 || n_heads % kv->n_kv_heads || max_keys < 0) return 0;
-  return EMOE_SERVING_TICKET_BYTES;
+  const AttendPlan p = attend_plan(*kv, rows, n_heads, max_keys);
+  return EMOE_SERVING_TICKET_BYTES + (size_t)2 * p.workers * p.part_floats * 4;
 }
 
 int32_t emoe_paged_attention(const emoe_paged_kv* kv, const emoe_paged_attention_args* args,
@@ -437,8 +905,6 @@ int32_t emoe_paged_attention(const emoe_paged_kv* kv, const emoe_paged_attention
                         kv->n_kv_heads);
   if (!std::isfinite(A.scale)) return report_error(EMOE_EINVAL, "scale is not finite");
   if (A.rows == 0) return EMOE_OK;
-  if ((int64_t)A.rows * A.n_heads >= (int64_t)1 << 30)
-    return report_error(EMOE_ESHAPE, "%d rows of %d heads", A.rows, A.n_heads);
   const int64_t qw = (int64_t)A.n_heads * kv->head_dim;
   if ((st = check_rows("q", A.q, A.q_stride, A.rows, qw))) return st;
   if ((st = check_rows("out", A.out, A.out_stride, A.rows, qw))) return st;
@@ -448,6 +914,9 @@ int32_t emoe_paged_attention(const emoe_paged_kv* kv, const emoe_paged_attention
     return report_error(EMOE_EINVAL, "workspace of %zu bytes < %zu needed", workspace ? workspace_bytes : 0,
                         need);
   if (!aligned16(workspace)) return report_error(EMOE_EINVAL, "workspace: need 16-byte alignment");
+  const AttendPlan plan = attend_plan(*kv, A.rows, A.n_heads, A.max_keys);
+  if (plan.rows_per_launch < 1)
+    return report_error(EMOE_ESHAPE, "max_keys %d with %d heads", A.max_keys, A.n_heads);
   AttendArg a;
   a.kv = view_of(*kv);
   a.q = static_cast<const uint16_t*>(A.q);
@@ -456,25 +925,35 @@ int32_t emoe_paged_attention(const emoe_paged_kv* kv, const emoe_paged_attention
   a.lengths = A.lengths;
   a.seqs = A.seqs;
   a.table = A.page_table;
+  a.tickets = static_cast<uint32_t*>(workspace);
+  a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + EMOE_SERVING_TICKET_BYTES);
   a.q_stride = A.q_stride;
   a.out_stride = A.out_stride;
   a.table_stride = A.table_stride;
   a.scale = A.scale;
-  a.rows = A.rows;
   a.n_heads = A.n_heads;
+  a.group = A.n_heads / kv->n_kv_heads;
+  a.q_tiles = (a.group + 15) / 16;
   a.n_seqs = A.n_seqs;
   a.table_width = A.table_width;
   a.max_keys = A.max_keys;
   a.window = A.window;
+  a.workers = plan.workers;
+  a.part_floats = plan.part_floats;
   const bool e4m3 = kv->dtype == EMOE_E4M3;
-  if (A.dtype == EMOE_BF16) {
-    if (e4m3) launch_attend<Bf16, true>(a, kv->head_dim, stream);
-    else launch_attend<Bf16, false>(a, kv->head_dim, stream);
-  } else {
-    if (e4m3) launch_attend<Fp16, true>(a, kv->head_dim, stream);
-    else launch_attend<Fp16, false>(a, kv->head_dim, stream);
+  for (int64_t r0 = 0; r0 < A.rows; r0 += plan.rows_per_launch) {
+    a.row0 = (int32_t)r0;
+    a.rows = (int32_t)(A.rows - r0 < plan.rows_per_launch ? A.rows - r0 : plan.rows_per_launch);
+    if (A.dtype == EMOE_BF16) {
+      if (e4m3) launch_attend<Bf16, true>(a, kv->head_dim, stream);
+      else launch_attend<Bf16, false>(a, kv->head_dim, stream);
+    } else {
+      if (e4m3) launch_attend<Fp16, true>(a, kv->head_dim, stream);
+      else launch_attend<Fp16, false>(a, kv->head_dim, stream);
+    }
+    if ((st = launched("paged_attention_kernel"))) return st;
   }
-  return launched("paged_attention_kernel");
+  return EMOE_OK;
 }
 
 }  // extern "C"
