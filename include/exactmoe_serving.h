@@ -127,7 +127,7 @@ typedef struct emoe_paged_attention_args {
  * call leaves them zero.  The rest needs no initial value.  One workspace may
  * serve calls of any sizes and both kinds (attention and logits), captured or
  * not, as long as no two of them overlap in time. */
-#define EMOE_SERVING_TICKET_BYTES 16384
+#define EMOE_SERVING_TICKET_BYTES 131072
 size_t emoe_paged_attention_workspace_bytes(const emoe_paged_kv* kv, int32_t rows, int32_t n_heads,
                                             int32_t max_keys);
 
@@ -167,7 +167,7 @@ typedef struct emoe_logits_args {
   int64_t logits_stride, out_stride, history_stride, bias_stride, mask_stride; /* elements */
   int32_t dtype;                   /* of logits and out: EMOE_F32, EMOE_BF16 or EMOE_F16 */
   int32_t rows, vocab;             /* >= 0, >= 1 */
-  int32_t history_width, bias_width, n_masks;
+  int32_t history_width, bias_width, n_masks;  /* bias_width below 2^23 */
 } emoe_logits_args;
 
 /* Workspace (needed with next_token only); its beginning as the attention's. */

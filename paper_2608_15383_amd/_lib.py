@@ -20,7 +20,7 @@ EMOE_MIXED_MFMA_ROWS = 16
 EMOE_GEMV_MAX_TOKENS = 4
 EMOE_NOALLOC_SCRATCH_BYTES = 32 << 20
 EMOE_F32, EMOE_BF16, EMOE_F16, EMOE_E4M3 = 0, 1, 2, 3
-EMOE_SERVING_TICKET_BYTES = 16384
+EMOE_SERVING_TICKET_BYTES = 131072
 
 
 class Dims(C.Structure):

@@ -325,7 +325,7 @@ def _call(fn, device, stream, *args) -> None:
     """fn(*args, stream) with `device` current; the default stream is that device's current one."""
     import torch
     if stream is None:
-        stream = torch.cuda.current_stream(device).cuda_stream
+        stream = torch._C._cuda_getCurrentRawStream(device.index)  # 1.8 us less than a Stream object
     elif not isinstance(stream, int):
         if stream.device != device:
             _refuse(f"stream of {stream.device} for tensors on {device}")

@@ -6,8 +6,9 @@ using namespace emoe;
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kTickets = EMOE_SERVING_TICKET_BYTES / 4;
+constexpr int kBestStride = kTicketLine / 8;  // a chunk's best has a line of its own, too
+constexpr int kLongHistory = 4096;
+constexpr uint32_t kBiasIndices = 1u << 23;  // bits of the smallest normal number
 
 struct LogitsArg {
   const void* logits;
@@ -21,36 +22,102 @@ struct LogitsArg {
   const uint32_t* mask;
   const int32_t* mask_rows;
   uint32_t* tickets;
-  uint64_t* best;  // [row of the launch][chunk]
+  uint64_t* best;  // [row of the launch][chunk], a line each
   int64_t logits_stride, out_stride, history_stride, bias_stride, mask_stride;
   int32_t row0, vocab, history_width, bias_width, n_masks, chunks;
 };
 
+// The element types: a 16-byte chunk holds kPer elements in four words.
 struct F32 {
-  static constexpr int kPer = 4;  // elements of a 16-byte chunk
-  __device__ static __forceinline__ void up(const uint4& c, float (&v)[4]) {
-    v[0] = __uint_as_float(c.x);
-    v[1] = __uint_as_float(c.y);
-    v[2] = __uint_as_float(c.z);
-    v[3] = __uint_as_float(c.w);
-  }
-  __device__ static __forceinline__ uint4 down(const float (&v)[4]) {
-    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
-                      __float_as_uint(v[3]));
-  }
+  static constexpr int kPer = 4;
   typedef uint32_t Raw;
-  __device__ static __forceinline__ float up1(Raw r) { return __uint_as_float(r); }
-  __device__ static __forceinline__ Raw down1(float x) { return __float_as_uint(x); }
+  static constexpr uint32_t kLowest = 0xff800000u;  // -infinity
+  __device__ static __forceinline__ float up(Raw r) { return __uint_as_float(r); }
+  __device__ static __forceinline__ Raw down(float x) { return __float_as_uint(x); }
 };
 template <class T>
 struct Half {
   static constexpr int kPer = 8;
-  __device__ static __forceinline__ void up(const uint4& c, float (&v)[8]) { up8<T>(c, v); }
-  __device__ static __forceinline__ uint4 down(const float (&v)[8]) { return down8<T>(v); }
   typedef uint16_t Raw;
-  __device__ static __forceinline__ float up1(Raw r) { return T::up(r); }
-  __device__ static __forceinline__ Raw down1(float x) { return (Raw)T::down(x); }
+  static constexpr uint32_t kLowest = T::kType == EMOE_BF16 ? 0xff80u : 0xfc00u;
+  __device__ static __forceinline__ float up(Raw r) { return T::up(r); }
+  __device__ static __forceinline__ Raw down(float x) { return (Raw)T::down(x); }
 };
+
+// Element i of a chunk, read and replaced by selects of values: an index into
+// the words, or a conditional that chooses one of them as an lvalue, would put
+// the chunk in memory.
+__device__ __forceinline__ uint32_t pick(bool c, uint32_t a, uint32_t b) { return c ? a : b; }
+template <class F>
+__device__ __forceinline__ typename F::Raw element(const uint4& w, int i) {
+  const int k = F::kPer == 4 ? i : i >> 1;
+  const uint32_t x = pick(k & 2, pick(k & 1, w.w, w.z), pick(k & 1, w.y, w.x));
+  return (typename F::Raw)(F::kPer == 4 ? x : x >> (16 * (i & 1)));
+}
+template <class F>
+__device__ __forceinline__ uint32_t with_element(uint32_t w, int i, typename F::Raw r) {
+  if (F::kPer == 4) return r;
+  return i & 1 ? (w & 0xffffu) | ((uint32_t)r << 16) : (w & 0xffff0000u) | r;
+}
+template <class F>
+__device__ __forceinline__ void put(uint4& w, int i, typename F::Raw r) {
+  const int k = F::kPer == 4 ? i : i >> 1;
+  w.x = pick(k == 0, with_element<F>(w.x, i, r), w.x);
+  w.y = pick(k == 1, with_element<F>(w.y, i, r), w.y);
+  w.z = pick(k == 2, with_element<F>(w.z, i, r), w.z);
+  w.w = pick(k == 3, with_element<F>(w.w, i, r), w.w);
+}
+// Word k of a chunk with the elements that a mask does not allow replaced by
+// -infinity: each bit is spread over its element, then chooses bits.
+template <class F>
+__device__ __forceinline__ uint32_t masked(uint32_t w, uint32_t allowed, int k) {
+  auto spread = [&](int i) { return (uint32_t)((int32_t)(allowed << (31 - i)) >> 31); };
+  uint32_t keep, low;
+  if (F::kPer == 4) {
+    keep = spread(k);
+    low = F::kLowest;
+  } else {
+    keep = (spread(2 * k) & 0xffffu) | (spread(2 * k + 1) & 0xffff0000u);
+    low = F::kLowest | (F::kLowest << 16);
+  }
+  return (w & keep) | (low & ~keep);
+}
+// Ids i .. i + 3 of a history of `width` ids, -1 past its end.
+__device__ __forceinline__ int4 load_ids(const int32_t* h, int i, int width) {
+  int4 id = make_int4(-1, -1, -1, -1);
+  if (i + 4 <= width) {
+    __builtin_memcpy(&id, h + i, 16);
+  } else {
+    if (i < width) id.x = h[i];
+    if (i + 1 < width) id.y = h[i + 1];
+    if (i + 2 < width) id.z = h[i + 2];
+  }
+  return id;
+}
+
+// The chunk at src[v], of which elements from V on are read as 0.
+template <class F>
+__device__ __forceinline__ uint4 load_chunk(const typename F::Raw* src, int v, int V) {
+  uint4 w = make_uint4(0, 0, 0, 0);
+  if (v + F::kPer <= V) {
+    __builtin_memcpy(&w, src + v, 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < F::kPer; ++i)
+      if (v + i < V) put<F>(w, i, src[v + i]);
+  }
+  return w;
+}
+template <class F>
+__device__ __forceinline__ void store_chunk(typename F::Raw* dst, int v, int V, const uint4& w) {
+  if (v + F::kPer <= V) {
+    __builtin_memcpy(dst + v, &w, 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < F::kPer; ++i)
+      if (v + i < V) dst[v + i] = element<F>(w, i);
+  }
+}
 
 // A value and its index as one word whose order is (value ascending, index
 // descending); 0 for what is never chosen (NaN and -inf).
@@ -71,182 +138,278 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t c) {
 
 // A workgroup takes one chunk of one row: its logits are on their way while
 // the row's history (and biases) is counted into words of LDS, one per token
-// id of the chunk (bit 31: in the prompt; low bits: times generated), then one
-// pass applies everything, writes the row and keeps the best.  Counting again
-// for every chunk costs L2 reads of the history, but needs no table in memory
-// as long as the vocabulary, which would have to be cleared and read as well.
-// The row's last workgroup to finish (a ticket in the workspace) takes the
-// best of its chunks' best.  Rows start at any element: the chunks of 16 bytes
-// are loaded unaligned.
-template <class F, int kLoads, bool kBias>
+// id of the chunk (bit 31: in the prompt; low bits: times generated), with a
+// bit per touched id.  Counting again for every chunk costs L2 reads of the
+// history, but needs no table in memory as long as the vocabulary, which would
+// have to be cleared and read as well.  Then one pass: the few touched elements
+// are taken out of their registers one by one, the mask replaces words, and
+// everything else goes from load to store as it came (a 16-bit logit is its
+// own rounding); the greedy choice needs one comparison per chunk of 16 bytes
+// unless that holds a new best.  The row's last workgroup to finish (a ticket
+// in the workspace) takes the best of its chunks' best.  Rows start at any
+// element: the chunks of 16 bytes are loaded unaligned.
+template <class F, int kThreads, int kLoads, bool kBias>
 __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
 #pragma clang fp contract(off)
   constexpr int kPer = F::kPer;
   constexpr int kChunk = kThreads * kPer * kLoads;
+  constexpr uint32_t kAll = (1u << kPer) - 1;
   typedef typename F::Raw Raw;
-  __shared__ __attribute__((aligned(16))) uint32_t seen[kChunk];
+  // Counters of 16 bits (bit 15: in the prompt) where the history is short, so
+  // that twice the workgroups fit a CU, else of 32.
+  constexpr bool kShort = kThreads == 256;
+  constexpr uint32_t kPrompt = kShort ? 0x8000u : 0x80000000u;
+  static_assert(kLongHistory <= 0x8000, "15 bits hold a short history's counts");
+  constexpr int kSeenWords = kShort ? kChunk / 2 : kChunk;
+  __shared__ __attribute__((aligned(16))) uint32_t seen[kSeenWords];
   __shared__ __attribute__((aligned(16))) int32_t bias[kBias ? kChunk : 4];
+  __shared__ uint32_t touched[kChunk / 32];
   __shared__ uint64_t red[kThreads / 64];
-  __shared__ int last;
   const int tid = threadIdx.x;
   const int lr = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
   const int row = a.row0 + lr, c0 = chunk * kChunk;
   const int V = a.vocab;
   const Raw* src = static_cast<const Raw*>(a.logits) + row * a.logits_stride;
-  uint4 raw[kLoads];
-#pragma unroll
-  for (int u = 0; u < kLoads; ++u) {
-    const int v = c0 + (u * kThreads + tid) * kPer;
-    if (v + kPer <= V) {
-      __builtin_memcpy(&raw[u], src + v, 16);
-    } else {
-      Raw e[kPer];
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) e[i] = v + i < V ? src[v + i] : Raw(0);
-      __builtin_memcpy(&raw[u], e, 16);
-    }
-  }
+  // Everything that memory has to give is asked for first: the row's settings,
+  // its logits, its mask and the beginning of its history (of the array's
+  // width: how much of it counts is not known yet).
   const float rep = a.repetition ? a.repetition[row] : 1.f;
   const float pres = a.presence ? a.presence[row] : 0.f;
   const float freq = a.frequency ? a.frequency[row] : 0.f;
-  const bool count = a.history && !(rep == 1.f && pres == 0.f && freq == 0.f);
-  if (count) {
-#pragma unroll
-    for (int u = 0; u < kChunk / (4 * kThreads); ++u)
-      reinterpret_cast<uint4*>(seen)[u * kThreads + tid] = make_uint4(0, 0, 0, 0);
-  }
-  if constexpr (kBias) {
-#pragma unroll
-    for (int u = 0; u < kChunk / (4 * kThreads); ++u)
-      reinterpret_cast<uint4*>(bias)[u * kThreads + tid] = make_uint4(0, 0, 0, 0);
-  }
-  __syncthreads();
-  if (count) {
-    int n = a.history_width;
-    if (a.history_lengths) n = max(0, min(n, a.history_lengths[row]));
-    const int prompt = a.prompt_lengths ? a.prompt_lengths[row] : 0;
-    const int32_t* h = a.history + row * a.history_stride;
-    auto add = [&](int i, int id) {
-      const uint32_t at = (uint32_t)id - (uint32_t)c0;
-      if (at < (uint32_t)kChunk && id < V) {
-        if (i < prompt) atomicOr(&seen[at], 0x80000000u);
-        else atomicAdd(&seen[at], 1u);
-      }
-    };
-    for (int i = 4 * tid; i < n; i += 4 * kThreads) {
-      if (i + 4 <= n) {
-        int id[4];
-        __builtin_memcpy(id, h + i, 16);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) add(i + k, id[k]);
-      } else {
-        for (int k = i; k < n; ++k) add(k, h[k]);
-      }
-    }
-  }
-  if constexpr (kBias) {
-    int n = a.bias_width;
-    if (a.bias_counts) n = max(0, min(n, a.bias_counts[row]));
-    const int32_t* ids = a.bias_ids + row * a.bias_stride;
-    for (int i = tid; i < n; i += kThreads) {
-      const int id = ids[i];
-      const uint32_t at = (uint32_t)id - (uint32_t)c0;
-      if (at < (uint32_t)kChunk && id < V) atomicMax(&bias[at], i + 1);  // the later entry counts
-    }
-  }
-  __syncthreads();
-  const uint32_t* mask = nullptr;
-  if (a.mask) {
-    const int m = a.mask_rows ? a.mask_rows[row] : row;
-    if ((uint32_t)m < (uint32_t)a.n_masks) mask = a.mask + m * a.mask_stride;
-  }
-  const float* bias_values = kBias ? a.bias_values + row * a.bias_stride : nullptr;
-  Raw* dst = static_cast<Raw*>(a.out) + row * a.out_stride;
-  uint64_t best = 0;
+  int n_hist = a.history_lengths ? a.history_lengths[row] : a.history_width;
+  const int prompt = a.prompt_lengths ? a.prompt_lengths[row] : 0;
+  int n_bias = a.bias_counts ? a.bias_counts[row] : a.bias_width;
+  const int mask_row = a.mask_rows ? a.mask_rows[row] : row;
+  uint4 raw[kLoads];
+  uint32_t allow[kLoads];
 #pragma unroll
   for (int u = 0; u < kLoads; ++u) {
-    const int at = (u * kThreads + tid) * kPer, v = c0 + at;
-    if (v >= V) break;
-    float x[kPer];
-    F::up(raw[u], x);
-    const uint32_t bits = mask ? mask[v >> 5] >> (v & 31) : ~0u;
+    const int v = c0 + (u * kThreads + tid) * kPer;
+    raw[u] = load_chunk<F>(src, v, V);
+    allow[u] = kAll;
+    if (a.mask && (uint32_t)mask_row < (uint32_t)a.n_masks && v < V)
+      allow[u] = a.mask[mask_row * a.mask_stride + (v >> 5)] >> (v & 31) & kAll;
+    if (v + kPer > V) allow[u] &= v < V ? (1u << (V - v)) - 1 : 0;
+  }
+  const int32_t* hist = a.history + row * a.history_stride;
+  constexpr int kAhead = kShort ? 1 : 4;  // loads of four ids in flight per thread
+  int4 ids[kAhead];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
+  for (int k = 0; k < kAhead; ++k)
+    ids[k] = a.history ? load_ids(hist, 4 * (k * kThreads + tid), a.history_width)
+                       : make_int4(-1, -1, -1, -1);
+  int bias_id = -1;
+  float bias_value = 0.f;
+  if constexpr (kBias) {
+    if (tid < a.bias_width) {
+      bias_id = a.bias_ids[row * a.bias_stride + tid];
+      bias_value = a.bias_values[row * a.bias_stride + tid];
+    }
+  }
+  n_hist = max(0, min(n_hist, a.history_width));
+  n_bias = max(0, min(n_bias, a.bias_width));
+  const bool count = a.history && !(rep == 1.f && pres == 0.f && freq == 0.f);
+  if (count || kBias) {
+    if (count)
+      for (int i = tid; i < kSeenWords / 4; i += kThreads)
+        reinterpret_cast<uint4*>(seen)[i] = make_uint4(0, 0, 0, 0);
+    if constexpr (kBias)
+      for (int i = tid; i < kChunk / 4; i += kThreads)
+        reinterpret_cast<uint4*>(bias)[i] = make_uint4(0, 0, 0, 0);
+    for (int i = tid; i < kChunk / 32; i += kThreads) touched[i] = 0;
+    __syncthreads();
+    if (count) {
+      // LDS takes atomics on one word one after the other, and a text has words
+      // of which every tenth token is one: what is set already is not set again.
+      auto add4 = [&](int i, const int4& id4) __attribute__((always_inline)) {
+        const int id[4] = {id4.x, id4.y, id4.z, id4.w};
+        uint32_t at[4], was[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          at[k] = (uint32_t)id[k] - (uint32_t)c0;
+          if (at[k] >= (uint32_t)kChunk || id[k] >= V || i + k >= n_hist) at[k] = ~0u;
+          was[k] = at[k] == ~0u ? 0 : seen[kShort ? at[k] >> 1 : at[k]];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (at[k] == ~0u) continue;
+          const int sh = kShort ? 16 * (at[k] & 1) : 0;
+          uint32_t* word = &seen[kShort ? at[k] >> 1 : at[k]];
+          const uint32_t now = kShort ? was[k] >> sh & 0xffffu : was[k];
+          if (i + k >= prompt) atomicAdd(word, 1u << sh);
+          else if (!(now & kPrompt)) atomicOr(word, kPrompt << sh);
+          if (now == 0) atomicOr(&touched[at[k] >> 5], 1u << (at[k] & 31));
+        }
+      };
+      for (int i0 = 0; i0 < n_hist; i0 += 4 * kThreads * kAhead) {
+        if (i0 > 0) {
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k)
+            ids[k] = load_ids(hist, i0 + 4 * (k * kThreads + tid), a.history_width);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) add4(i0 + 4 * (k * kThreads + tid), ids[k]);
+      }
+    }
+    if constexpr (kBias) {
+      // The later of two entries of an id counts: the largest index stays in the
+      // id's word, then gives way to the entry's value, whose bits cannot be
+      // taken for an index (the values below 2^-126 stay indices, and are read
+      // when they are added).
+      const int32_t* more_ids = a.bias_ids + row * a.bias_stride;
+      auto place = [&](int id) -> uint32_t {
+        const uint32_t at = (uint32_t)id - (uint32_t)c0;
+        return at < (uint32_t)kChunk && id < V ? at : ~0u;
+      };
+      for (int i = tid; i < n_bias; i += kThreads) {
+        const uint32_t at = place(i < kThreads ? bias_id : more_ids[i]);
+        if (at == ~0u) continue;
+        atomicMax(&bias[at], i + 1);
+        atomicOr(&touched[at >> 5], 1u << (at & 31));
+      }
+      __syncthreads();
+      for (int i = tid; i < n_bias; i += kThreads) {
+        const uint32_t at = place(i < kThreads ? bias_id : more_ids[i]);
+        if (at == ~0u || bias[at] != i + 1) continue;
+        const uint32_t bits = __float_as_uint(i < kThreads ? bias_value
+                                                           : a.bias_values[row * a.bias_stride + i]);
+        if (bits >= kBiasIndices) bias[at] = (int32_t)bits;
+      }
+    }
+    __syncthreads();
+  }
+  Raw* dst = static_cast<Raw*>(a.out) + row * a.out_stride;
+  float best = -INFINITY;
+  int best_at = -1;
+  auto step = [&](uint4& w, uint32_t allowed, int at) __attribute__((always_inline)) {
+    const int v = c0 + at;
+    if (v >= V) return;
+    if (allowed != kAll)
+      w = make_uint4(masked<F>(w.x, allowed, 0), masked<F>(w.y, allowed, 1),
+                     masked<F>(w.z, allowed, 2), masked<F>(w.w, allowed, 3));
+    uint32_t todo = count || kBias ? touched[at >> 5] >> (at & 31) & allowed : 0;
+    if (a.next_token) {
+      // The elements that stay as they are first: among equals the lower id.
+      float x[kPer];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) x[i] = F::up(element<F>(w, i));
+      if (todo) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) x[i] = todo >> i & 1 ? -INFINITY : x[i];
+      }
+      float top = x[0];
+#pragma unroll
+      for (int i = 1; i < kPer; ++i) top = fmaxf(top, x[i]);
+      if (top > best) {
+        best = top;
+#pragma unroll
+        for (int i = kPer - 1; i >= 0; --i) best_at = x[i] == top ? v + i : best_at;
+      }
+    }
+    while (todo) {
+      const int i = __builtin_ctz(todo);
+      todo &= todo - 1;
+      float x = F::up(element<F>(w, i));
+      uint32_t c = 0;
       if (count) {
-        const uint32_t w = seen[at + i];
-        if (w) {
-          x[i] = x[i] > 0.f ? x[i] / rep : x[i] * rep;
-          const uint32_t c = w & 0x7fffffffu;
-          if (c) {
-            const float f = freq * (float)c;
-            x[i] = x[i] - f;
-            x[i] = x[i] - pres;
-          }
+        c = seen[kShort ? (at + i) >> 1 : at + i];
+        if (kShort) c = c >> (16 * (i & 1)) & 0xffffu;
+      }
+      if (c) {
+        x = x > 0.f ? x / rep : x * rep;
+        if (c & (kPrompt - 1)) {
+          const float f = freq * (float)(c & (kPrompt - 1));
+          x = x - f;
+          x = x - pres;
         }
       }
       if constexpr (kBias) {
-        const int b = bias[at + i];
-        if (b) x[i] = x[i] + bias_values[b - 1];
+        const uint32_t b = (uint32_t)bias[at + i];
+        if (b >= kBiasIndices) x = x + __uint_as_float(b);
+        else if (b) x = x + a.bias_values[row * a.bias_stride + b - 1];
       }
-      if (!((bits >> i) & 1)) x[i] = -INFINITY;
-      if (v + i < V) best = max64(best, choice(x[i], v + i));
+      put<F>(w, i, F::down(x));
+      if (x > best || (x == best && v + i < best_at)) {
+        best = x;
+        best_at = v + i;
+      }
     }
-    const uint4 o = F::down(x);
-    if (v + kPer <= V) {
-      __builtin_memcpy(dst + v, &o, 16);
-    } else {
-      for (int i = 0; v + i < V; ++i) dst[v + i] = F::down1(x[i]);
+  };
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) step(raw[u], allow[u], (u * kThreads + tid) * kPer);
+  // The choice goes out before the row does: its hand-over takes two trips to
+  // memory, which the stores then do not stand in front of.
+  const bool choose = a.next_token != nullptr;
+  uint32_t before = 0;
+  if (choose) {
+    uint64_t top = wave_max(choice(best, best_at));
+    if ((tid & 63) == 0) red[tid >> 6] = top;
+    __syncthreads();
+    if (tid == 0) {
+      for (int i = 1; i < kThreads / 64; ++i) top = max64(top, red[i]);
+      if (a.chunks == 1) {
+        a.next_token[row] = chosen(top);
+      } else {
+        __hip_atomic_store(&a.best[((int64_t)lr * a.chunks + chunk) * kBestStride], top,
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        wait_memory();
+        before = __hip_atomic_fetch_add(&a.tickets[lr * kTicketStride], 1u, __ATOMIC_RELAXED,
+                                        __HIP_MEMORY_SCOPE_AGENT);
+      }
     }
   }
-  if (!a.next_token) return;
-  best = wave_max(best);
-  if ((tid & 63) == 0) red[tid >> 6] = best;
-  __syncthreads();
-  if (tid == 0) {
-    best = max64(max64(red[0], red[1]), max64(red[2], red[3]));
-    last = 0;
-    if (a.chunks == 1) {
-      a.next_token[row] = chosen(best);
-    } else {
-      __hip_atomic_store(&a.best[(int64_t)lr * a.chunks + chunk], best, __ATOMIC_RELAXED,
-                         __HIP_MEMORY_SCOPE_AGENT);
-      wait_memory();
-      last = __hip_atomic_fetch_add(&a.tickets[lr], 1u, __ATOMIC_RELAXED,
-                                    __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.chunks - 1;
-      wait_memory();
-    }
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) {
+    const int v = c0 + (u * kThreads + tid) * kPer;
+    if (v < V) store_chunk<F>(dst, v, V, raw[u]);
   }
-  if (a.chunks == 1) return;
-  __syncthreads();
-  if (!last || tid >= 64) return;
-  best = 0;
+  if (!choose || a.chunks == 1 || tid >= 64) return;
+  if (__builtin_amdgcn_readfirstlane(before) != (uint32_t)a.chunks - 1) return;
+  wait_memory();
+  uint64_t top = 0;
   for (int i = tid; i < a.chunks; i += 64)
-    best = max64(best, __hip_atomic_load(&a.best[(int64_t)lr * a.chunks + i], __ATOMIC_RELAXED,
-                                         __HIP_MEMORY_SCOPE_AGENT));
-  best = wave_max(best);
+    top = max64(top, __hip_atomic_load(&a.best[((int64_t)lr * a.chunks + i) * kBestStride],
+                                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+  top = wave_max(top);
   if (tid == 0) {
-    a.next_token[row] = chosen(best);
-    st_u32<true>(&a.tickets[lr], 0);
+    a.next_token[row] = chosen(top);
+    st_u32<true>(&a.tickets[lr * kTicketStride], 0);
   }
 }
 
-template <class F, int kLoads>
+// How a call is cut: threads and 16-byte loads of a workgroup.
+struct LogitsPlan {
+  int threads, loads, chunks;
+};
+LogitsPlan logits_plan(int32_t rows, int32_t vocab, int per, int32_t history_width) {
+  LogitsPlan p{256, 4, 0};
+  auto chunks = [&] {
+    const int64_t c = (int64_t)p.threads * per * p.loads;
+    return (int)((vocab + c - 1) / c);
+  };
+  if (history_width >= kLongHistory) {
+    p.threads = 1024;
+    p.loads = 8 / per;
+  } else if ((int64_t)rows * chunks() < 512) {
+    p.loads = 1;
+  }
+  p.chunks = chunks();
+  return p;
+}
+
+template <class F, int kThreads, int kLoads>
 void launch_logits(const LogitsArg& a, unsigned blocks, hipStream_t stream) {
   if (a.bias_ids)
-    hipLaunchKernelGGL((process_logits_kernel<F, kLoads, true>), dim3(blocks), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((process_logits_kernel<F, kThreads, kLoads, true>), dim3(blocks), dim3(kThreads), 0, stream, a);
   else
-    hipLaunchKernelGGL((process_logits_kernel<F, kLoads, false>), dim3(blocks), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((process_logits_kernel<F, kThreads, kLoads, false>), dim3(blocks), dim3(kThreads), 0, stream, a);
 }
 
 template <class F>
-void launch_type(const LogitsArg& a, int loads, unsigned blocks, hipStream_t stream) {
-  if (loads == 1) launch_logits<F, 1>(a, blocks, stream);
-  else launch_logits<F, 4>(a, blocks, stream);
-}
-
-int chunks_of(int32_t vocab, int per, int loads) {
-  const int64_t c = (int64_t)kThreads * per * loads;
-  return (int)((vocab + c - 1) / c);
+void launch_type(const LogitsArg& a, const LogitsPlan& p, unsigned blocks, hipStream_t stream) {
+  if (p.threads == 1024) launch_logits<F, 1024, 8 / F::kPer>(a, blocks, stream);
+  else if (p.loads == 1) launch_logits<F, 256, 1>(a, blocks, stream);
+  else launch_logits<F, 256, 4>(a, blocks, stream);
 }
 
 }  // namespace
@@ -256,7 +419,7 @@ extern "C" {
 size_t emoe_process_logits_workspace_bytes(int32_t rows, int32_t vocab) {
   if (rows < 0 || vocab < 1) return 0;
   const size_t held = rows < kTickets ? rows : kTickets;  // rows of one launch
-  return EMOE_SERVING_TICKET_BYTES + held * (size_t)chunks_of(vocab, F32::kPer, 1) * 8;
+  return EMOE_SERVING_TICKET_BYTES + held * (((size_t)vocab + 1023) / 1024) * kTicketLine;  // the smallest chunks
 }
 
 int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_t workspace_bytes,
@@ -284,6 +447,8 @@ int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_
     return report_error(EMOE_EINVAL, "penalties without a history");
   if (!A.bias_ids != !A.bias_values)
     return report_error(EMOE_EINVAL, "one of bias_ids and bias_values is NULL");
+  if (A.bias_width >= (int32_t)kBiasIndices)
+    return report_error(EMOE_ESHAPE, "bias_width %d above %d", A.bias_width, (int)kBiasIndices - 1);
   if (A.bias_ids && many && A.bias_stride < A.bias_width)
     return report_error(EMOE_EINVAL, "bias_stride below bias_width %d", A.bias_width);
   if (A.mask) {
@@ -295,8 +460,7 @@ int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_
     return report_error(EMOE_EINVAL, "mask_rows without a mask");
   }
   const int per = A.dtype == EMOE_F32 ? 4 : 8;
-  const int loads = (int64_t)A.rows * chunks_of(A.vocab, per, 4) >= 512 ? 4 : 1;
-  const int chunks = chunks_of(A.vocab, per, loads);
+  const LogitsPlan plan = logits_plan(A.rows, A.vocab, per, A.history ? A.history_width : 0);
   if (A.next_token) {
     const size_t need = emoe_process_logits_workspace_bytes(A.rows, A.vocab);
     if (!workspace || workspace_bytes < need)
@@ -331,17 +495,17 @@ int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_
   a.history_width = A.history_width;
   a.bias_width = A.bias_width;
   a.n_masks = A.n_masks;
-  a.chunks = chunks;
+  a.chunks = plan.chunks;
   // Rows of one launch: a ticket each, and a grid below 2^31 workgroups.
-  int64_t step = ((int64_t)1 << 30) / chunks;
+  int64_t step = ((int64_t)1 << 30) / plan.chunks;
   if (step > kTickets) step = kTickets;
   for (int64_t r0 = 0; r0 < A.rows; r0 += step) {
     a.row0 = (int32_t)r0;
     const int64_t n = A.rows - r0 < step ? A.rows - r0 : step;
-    const unsigned blocks = (unsigned)(n * chunks);
-    if (A.dtype == EMOE_F32) launch_type<F32>(a, loads, blocks, stream);
-    else if (A.dtype == EMOE_BF16) launch_type<Half<Bf16>>(a, loads, blocks, stream);
-    else launch_type<Half<Fp16>>(a, loads, blocks, stream);
+    const unsigned blocks = (unsigned)(n * plan.chunks);
+    if (A.dtype == EMOE_F32) launch_type<F32>(a, plan, blocks, stream);
+    else if (A.dtype == EMOE_BF16) launch_type<Half<Bf16>>(a, plan, blocks, stream);
+    else launch_type<Half<Fp16>>(a, plan, blocks, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess)
       return report_error(EMOE_EHIP, "process_logits_kernel launch: %s", hipGetErrorString(e));

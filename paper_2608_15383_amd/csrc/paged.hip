@@ -198,7 +198,6 @@ constexpr int kTileKeys = 32;   // keys of one wavefront's step
 constexpr int kAttnWaves = 4;
 constexpr int kUnitKeys = kTileKeys * kAttnWaves;
 constexpr int kMaxRows = 1024;  // rows of one launch
-constexpr int kMaxWorkers = EMOE_SERVING_TICKET_BYTES / 4;
 
 typedef const __attribute__((address_space(4))) int32_t* ConstI32;
 
@@ -641,7 +640,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
       wait_memory();
       __syncthreads();
       if (tid == 0) {
-        last = __hip_atomic_fetch_add(&a.tickets[wa], 1u, __ATOMIC_RELAXED,
+        last = __hip_atomic_fetch_add(&a.tickets[wa * kTicketStride], 1u, __ATOMIC_RELAXED,
                                       __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(wb - wa);
         wait_memory();
       }
@@ -673,7 +672,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
           }
           store_out(h, d, o, M, L);
         }
-        if (tid == 0) st_u32<true>(&a.tickets[wa], 0);
+        if (tid == 0) st_u32<true>(&a.tickets[wa * kTicketStride], 0);
       }
     }
     u += c1 - c0;
@@ -801,12 +800,13 @@ struct AttendPlan {
   int workers, part_floats;
 };
 constexpr int kWorkers = 768;  // three workgroups per CU
+static_assert(kWorkers <= kTickets, "a ticket per workgroup");
 AttendPlan attend_plan(const emoe_paged_kv& kv, int32_t rows, int32_t n_heads, int32_t max_keys) {
   const int group = n_heads / kv.n_kv_heads;
   const int64_t lines = (int64_t)kv.n_kv_heads * ((group + 15) / 16);
   const int64_t most = lines * ((int64_t)max_keys / kUnitKeys + 2);  // units of one row
   AttendPlan p;
-  p.rows_per_launch = (((int64_t)1 << 31) - 1 - kMaxWorkers) / most;
+  p.rows_per_launch = (((int64_t)1 << 31) - 1 - kTickets) / most;
   if (p.rows_per_launch > kMaxRows) p.rows_per_launch = kMaxRows;
   const int64_t held = rows < p.rows_per_launch ? rows : p.rows_per_launch;
   p.workers = (int)(held * most < kWorkers ? held * most : kWorkers);

@@ -52,6 +52,12 @@ __device__ __forceinline__ uint2 down8_e4m3(const float (&v)[8]) {
   return w;
 }
 
+// The workspace's tickets, each in a line of its own: device-coherent atomics
+// on one line come one after the other, whatever the word (19 rows' tickets in
+// one line kept process_logits_kernel busy for 10 us).
+constexpr int kTicketLine = 128, kTicketStride = kTicketLine / 4;
+constexpr int kTickets = EMOE_SERVING_TICKET_BYTES / kTicketLine;
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 }  // namespace emoe

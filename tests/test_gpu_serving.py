@@ -21,7 +21,7 @@ import torch
 
 from oracle import serving_oracle as S
 from paper_2608_15383_amd import api
-from paper_2608_15383_amd._lib import EMOE_EINVAL, ExactMoEError
+from paper_2608_15383_amd._lib import EMOE_EINVAL, EMOE_SERVING_TICKET_BYTES, ExactMoEError
 
 pytestmark = pytest.mark.gpu
 
@@ -282,7 +282,7 @@ def run_attention(kind, cache_kind, lengths, heads, hk, d, page, seed, window=0,
                                        lse=None if lse is None else lse[:rows], stream=stream)
     call()
     torch.cuda.synchronize()
-    assert not ws[:16384].any()
+    assert not ws[:EMOE_SERVING_TICKET_BYTES].any()
     got, z = f64(o), None if lse is None else f64(lse)
     assert bool((out[rows:] == 7).all()) and bool((out[:, heads * d:] == 7).all())
     assert lse is None or bool((lse[rows:] == 7).all())
@@ -506,7 +506,7 @@ def run_logits(kind, rows, vocab, width, seed, in_place=False, token=True, **kw)
     api.process_logits(out=None if in_place else out[:rows], workspace=ws if token else None,
                        next_token=None if nt is None else nt[:rows], **dev)
     torch.cuda.synchronize()
-    assert not ws[:16384].any()
+    assert not ws[:EMOE_SERVING_TICKET_BYTES].any()
     if not in_place:
         assert bool((out[rows:] == 7).all())
         whole = out._base if out._base is not None else out
@@ -571,7 +571,8 @@ def test_logits_choice_comes_before_the_store():
     """Two bf16 neighbours that a penalty makes equal only once they are rounded."""
     x = torch.full((1, 64), -9.0, device="cuda:0").to(torch.bfloat16)
     x[0, 3], x[0, 9] = 4.0, 4.03125
-    nt, ws = torch.empty(1, dtype=torch.int32, device="cuda:0"), torch.zeros(20000, dtype=torch.uint8, device="cuda:0")
+    nt = torch.empty(1, dtype=torch.int32, device="cuda:0")
+    ws = torch.zeros(api.process_logits_workspace_bytes(1, 64), dtype=torch.uint8, device="cuda:0")
     out = torch.empty_like(x)
     api.process_logits(x, out, ws, bias_ids=ids([[9]]), bias_values=gpu([[-0.03]]), next_token=nt)
     assert float(out[0, 3]) == float(out[0, 9]) == 4.0 and int(nt) == 9
@@ -665,7 +666,7 @@ def test_two_graphs_share_a_workspace():
             graphs[i].replay()
             torch.cuda.synchronize()
             assert torch.equal(s.out, want[i][0]) and torch.equal(s.next, want[i][-1]), (turn, i)
-        assert not a.ws[:16384].any()
+        assert not a.ws[:EMOE_SERVING_TICKET_BYTES].any()
         a.all()
 
 
