@@ -194,6 +194,8 @@ struct Half16<Fp16> {
   }
 };
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kTileKeys = 32;   // keys of one wavefront's step
 constexpr int kAttnWaves = 4;
 constexpr int kUnitKeys = kTileKeys * kAttnWaves;
@@ -203,6 +205,12 @@ typedef const __attribute__((address_space(4))) int32_t* ConstI32;
 
 // 2^x by the hardware instruction (1 ulp; denormal results are 0).
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// What a part of a softmax with maximum m counts for beside maximum M.  One
+// that saw no score counts for 0, by a product: its sums may be NaN.
+__device__ __forceinline__ float part_weight(float m, float M) {
+  return m == -INFINITY ? 0.f : exp2_hw(m - M);
+}
 
 // The keys that row `row` of the call sees: [first, n).
 struct Span {
@@ -227,87 +235,128 @@ __device__ __forceinline__ int units_of(int first, int n) {
   return max(1, (t1 - t0 + kAttnWaves - 1) / kAttnWaves);
 }
 
-// One tile of 32 keys of one key head, as the matrix instructions take it.
+// One tile of 32 keys of one key head, as the matrix instructions take it: two
+// halves of two octets, an octet being 8 slots of one page.
 //
 // Scores: S^T [key][query] = K Q^T.  The A operand's lane (l16, g) holds 8
-// dimensions of key l16 of a half tile, which is 16 bytes as they lie in the
-// cache (of E4M3: 16 dimensions, for two steps); any dimensions do, as long as
-// the query's lanes hold the same.  The result's lane (l16, g) has the scores
-// of keys 4g .. 4g+3 of each half for query l16.
+// dimensions of row l16; any dimensions do, as long as the query's lanes hold
+// the same, and any key may be any row.  Row 4r + i of a half is slot
+// 2r + (i & 1) of its octet i >> 1.  A load takes one octet, 8 lanes to a slot,
+// so that it covers whole 128-byte lines (4 lanes to a slot, the operand's own
+// arrangement, read the cache at 5.3 TB/s where this reaches 6): lanes with
+// i >> 1 = 0 hold the row's first 4 chunks and the others the next 4, and lanes
+// l and l ^ 2 trade what they have of the other one's octet.  All addresses are
+// a scalar of the octet plus an offset that a lane keeps.
 // Output: O^T [dim][query] = V^T P^T.  The B operand's lane wants 8 keys of
-// its query, and again any order of keys does: those 4g .. 4g+3 of both
-// halves, so the scores become weights in the registers that they are in.  The
-// A operand's lane wants the same 8 keys of one dimension; it loads kDh / 16
-// consecutive dimensions of each and transposes the 8 x 2 pairs with byte
-// permutes (32 of them per tile at 128 dimensions), which keeps values out of
-// LDS.  A query's running maximum, sum and output columns all live in lanes
-// l16 = query, so nothing is exchanged between lanes in the loop.
+// its query, in any order: those of the rows that its scores are in, so scores
+// become weights in the registers that hold them.  The A operand's lane wants
+// the same 8 keys of one dimension; it loads kDh / 16 consecutive dimensions of
+// each and transposes with byte permutes (32 of them per tile at 128
+// dimensions), which keeps values out of LDS.  A query's running maximum, sum
+// and output columns all live in lanes l16 = query, so nothing is exchanged
+// between queries in the loop.
 template <class T, bool kE4M3, int kDh>
 struct Tile {
   typedef Half16<T> H16;
   static constexpr int kSteps = kDh / 32;
   static constexpr int kItem = kE4M3 ? 1 : 2;
-  static constexpr int kKLoads = kDh * kItem / 64;  // 16-byte loads per key half
-  static constexpr int kDims = kDh / 16;            // output dimensions of a lane
+  static constexpr int kChunk = kE4M3 && kDh == 64 ? 8 : 16;  // bytes of a lane's load
+  static constexpr int kChunkWords = kChunk / 4;
+  static constexpr int kChunkDims = kChunk / kItem;
+  static constexpr int kSub = kChunkDims / 8;              // steps of a chunk
+  static constexpr int kPairs = kDh / (8 * kChunkDims);    // loads of an octet
+  static constexpr int kDims = kDh / 16;                   // output dimensions of a lane
   static constexpr int kVWords = kDims * kItem / 4;
-  static constexpr bool kSplitV = !kE4M3 && kDh == 256;  // two 16-byte loads, 256 bytes apart
+  static constexpr bool kSplitV = !kE4M3 && kDh == 256;    // two 16-byte loads, 256 bytes apart
 
-  uint4 k[2][kKLoads];
+  uint32_t k[4][kPairs][kChunkWords];
   uint32_t v[8][kVWords];
 
   // The first of the 8 dimensions that lane group g holds in step c.
   __device__ static __forceinline__ int q_dim(int c, int g) {
-    return kE4M3 ? 16 * (4 * (c >> 1) + g) + 8 * (c & 1) : 8 * (4 * c + g);
+    return kChunkDims * (4 * (c / kSub) + g) + 8 * (c % kSub);
   }
   // Output dimension of matrix row m of accumulator c.
   __device__ static __forceinline__ int out_dim(int m, int c) {
     return kSplitV ? 128 * (c >> 3) + 8 * m + (c & 7) : kDims * m + c;
   }
-
-  __device__ __forceinline__ void load_k(const uint8_t* const (&at)[2], int lane) {
-    const int off = 16 * (lane >> 4);
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int c = 0; c < kKLoads; ++c)
-        k[h][c] = *reinterpret_cast<const uint4*>(at[h] + off + 64 * c);
+  // A lane's offset from an octet's first slot: its key's chunk, its value's
+  // dimensions (of the slot 2g; the slot after it for odd i).
+  __device__ static __forceinline__ uint32_t k_offset(int lane, int slot_bytes) {
+    const int m = lane & 15, slot = 2 * (m >> 2) + (m & 1);
+    return slot * slot_bytes + kChunk * (2 * (m & 2) + (lane >> 4));
   }
-  __device__ __forceinline__ void load_v(const uint8_t* const (&at)[2], int slot_bytes, int lane) {
-    const int off = (kSplitV ? 16 : kVWords * 4) * (lane & 15);
+  __device__ static __forceinline__ uint32_t v_offset(int lane, int slot_bytes) {
+    return 2 * (lane >> 4) * slot_bytes + (kSplitV ? 16 : kVWords * 4) * (lane & 15);
+  }
+
+  __device__ __forceinline__ void load_k(const uint8_t* const (&octet)[4], uint32_t off) {
+#pragma unroll
+    for (int o = 0; o < 4; ++o)
+#pragma unroll
+      for (int p = 0; p < kPairs; ++p) {
+        const uint8_t* at = octet[o] + off + 8 * kChunk * p;
+        if constexpr (kChunkWords == 4) {
+          const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at));
+          k[o][p][0] = w.x, k[o][p][1] = w.y, k[o][p][2] = w.z, k[o][p][3] = w.w;
+        } else {
+          const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(at));
+          k[o][p][0] = w.x, k[o][p][1] = w.y;
+        }
+      }
+  }
+  __device__ __forceinline__ void load_v(const uint8_t* const (&octet)[4], int slot_bytes,
+                                         uint32_t off) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const uint8_t* p = at[j >> 2] + (int64_t)(j & 3) * slot_bytes + off;
+      const uint8_t* p = octet[j >> 1] + (j & 1) * slot_bytes + off;
       if constexpr (kVWords == 1) {
-        v[j][0] = *reinterpret_cast<const uint32_t*>(p);
+        v[j][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
       } else if constexpr (kVWords == 2) {
-        const uint2 w = *reinterpret_cast<const uint2*>(p);
+        const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
         v[j][0] = w.x, v[j][1] = w.y;
       } else {
 #pragma unroll
         for (int u = 0; u < kVWords / 4; ++u) {
-          const uint4 w = *reinterpret_cast<const uint4*>(p + 256 * u);
+          const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 256 * u));
           v[j][4 * u] = w.x, v[j][4 * u + 1] = w.y, v[j][4 * u + 2] = w.z, v[j][4 * u + 3] = w.w;
         }
       }
     }
   }
-  __device__ __forceinline__ void scores(const uint4 (&q)[kSteps], f32x4 (&s)[2]) const {
+  // Scores of the half h's rows: step by step, chunks of the first octet and
+  // of the second traded between lanes l and l ^ 2.
+  __device__ __forceinline__ void scores(const uint4 (&q)[kSteps], bool second, f32x4 (&s)[2]) const {
 #pragma unroll
     for (int h = 0; h < 2; ++h) s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int c = 0; c < kSteps; ++c)
+    for (int p = 0; p < kPairs; ++p)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        uint4 a;
-        if constexpr (kE4M3) {
-          const uint4 w = k[h][c >> 1];
-          const uint32_t lo = (c & 1) ? w.z : w.x, hi = (c & 1) ? w.w : w.y;
-          a = make_uint4(H16::template from_e4m3<false>(lo), H16::template from_e4m3<true>(lo),
-                         H16::template from_e4m3<false>(hi), H16::template from_e4m3<true>(hi));
-        } else {
-          a = k[h][c];
+        uint32_t c0[kChunkWords], c1[kChunkWords];
+#pragma unroll
+        for (int w = 0; w < kChunkWords; ++w) {
+          const uint32_t a = k[2 * h][p][w], b = k[2 * h + 1][p][w];
+          const uint32_t a2 = __builtin_amdgcn_update_dpp(0, (int)a, 0x4E, 0xF, 0xF, true);
+          const uint32_t b2 = __builtin_amdgcn_update_dpp(0, (int)b, 0x4E, 0xF, 0xF, true);
+          c0[w] = second ? b2 : a;
+          c1[w] = second ? b : a2;
         }
-        s[h] = H16::mfma(a, q[c], s[h]);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int sub = 0; sub < kSub; ++sub) {
+            const uint32_t(&c)[kChunkWords] = half ? c1 : c0;
+            uint4 x;
+            if constexpr (kE4M3) {
+              const uint32_t lo = c[2 * sub], hi = c[2 * sub + 1];
+              x = make_uint4(H16::template from_e4m3<false>(lo), H16::template from_e4m3<true>(lo),
+                             H16::template from_e4m3<false>(hi), H16::template from_e4m3<true>(hi));
+            } else {
+              x = make_uint4(c[0], c[1], c[2], c[3]);
+            }
+            s[h] = H16::mfma(x, q[(2 * p + half) * kSub + sub], s[h]);
+          }
       }
   }
   // Values of keys that are not there become 0: a weight of 0 does not undo a NaN.
@@ -372,11 +421,18 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
   __shared__ int wave_sum[kThreads / 64];
   __shared__ float ms[kAttnWaves][16], ls[kAttnWaves][16];
   __shared__ __attribute__((aligned(16))) float os[kAttnWaves][16][kRow];
-  __shared__ int last;
+  __shared__ float4 striped[kThreads];
+  __shared__ float striped_m[kThreads], striped_l[kThreads];
+  __shared__ int last, first_row;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
+  const uint32_t k_off = Tl::k_offset(lane, a.kv.slot_bytes);
+  const uint32_t v_off = Tl::v_offset(lane, a.kv.slot_bytes);
 
-  // Units before each row.
+  // Units before each row, and where this worker's run of them begins.
+  const int Y = a.kv.n_kv_heads * a.q_tiles;
+  const int w = blockIdx.x / Y, y = blockIdx.x % Y;
+  int total = 0;
   {
     const int per = (a.rows + kThreads - 1) / kThreads, r0 = tid * per;
     int cnt[kMaxRows / kThreads], sum = 0;
@@ -400,43 +456,35 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
     if (lane == 63) wave_sum[wave] = incl;
     __syncthreads();
     int at = incl - sum;
-    for (int w = 0; w < wave; ++w) at += wave_sum[w];
+    for (int i = 0; i < kAttnWaves; ++i) {
+      at += i < wave ? wave_sum[i] : 0;
+      total += wave_sum[i];
+    }
+    const int start = w * ((total + a.workers - 1) / a.workers);
 #pragma unroll
     for (int i = 0; i < kMaxRows / kThreads; ++i) {
-      if (i < per && r0 + i < a.rows) pre[r0 + i] = at;
+      if (i < per && r0 + i < a.rows) {
+        pre[r0 + i] = at;
+        if (start >= at && start < at + cnt[i]) first_row = r0 + i;
+      }
       at += cnt[i];
     }
-    if (tid == 0) {
-      int all = 0;
-      for (int w = 0; w < kThreads / 64; ++w) all += wave_sum[w];
-      pre[a.rows] = all;
-    }
+    if (tid == kThreads - 1) pre[a.rows] = total;
     __syncthreads();
   }
-  const int Y = a.kv.n_kv_heads * a.q_tiles;
-  const int total = __builtin_amdgcn_readfirstlane(pre[a.rows]) * Y;
-  const int run = (total + a.workers - 1) / a.workers;  // units per workgroup
-  const int w = blockIdx.x;
+  total = __builtin_amdgcn_readfirstlane(total);
+  const int run = (total + a.workers - 1) / a.workers;  // units per worker
   if ((int64_t)w * run >= total) return;
   const int u_end = min((w + 1) * run, total);
-  int u = w * run;
+  int u = w * run, row = first_row;
   bool first_segment = true;
-  int row = 0;
-  {
-    int hi = a.rows;  // pre[row] <= u / Y < pre[hi]
-    const int key = u / Y;
-    while (hi - row > 1) {
-      const int mid = (row + hi) >> 1;
-      if (pre[mid] <= key) row = mid; else hi = mid;
-    }
-  }
-  while (u < u_end) {
+  for (; u < u_end; ++row) {
     row = __builtin_amdgcn_readfirstlane(row);
     const int base = __builtin_amdgcn_readfirstlane(pre[row]);
     const int units = __builtin_amdgcn_readfirstlane(pre[row + 1]) - base;
     const int n = __builtin_amdgcn_readfirstlane(len[row]);
     const int sq = __builtin_amdgcn_readfirstlane(seq[row]);
-    const int y = (u - base * Y) / units, c0 = (u - base * Y) % units;
+    const int c0 = u - base;
     const int c1 = min(units, c0 + (u_end - u));
     const int first = a.window > 0 ? max(0, n - a.window) : 0;
     const int hk = y / a.q_tiles, qt = y % a.q_tiles;
@@ -468,8 +516,8 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
     const uint8_t* vbase = a.kv.v + (int64_t)hk * a.kv.head_bytes;
     const int slot_mask = (1 << a.kv.page_log2) - 1;
 
-    // Byte offsets of the tile's octets (of page 0 where there is no page: any
-    // place that may be read), and of this lane's keys in each half.
+    // The tile's octets (of page 0 where there is no page: any place that may
+    // be read), from the first byte of their slots.
     auto place = [&](const Octets& o, int key0, int64_t (&off)[4]) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -479,18 +527,12 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
     };
     Tl tile;
     auto load_k = [&](const int64_t (&off)[4]) {
-      const uint8_t* at[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        at[h] = kbase + (l16 < 8 ? off[2 * h] : off[2 * h + 1]) + (l16 & 7) * a.kv.slot_bytes;
-      tile.load_k(at, lane);
+      const uint8_t* const at[4] = {kbase + off[0], kbase + off[1], kbase + off[2], kbase + off[3]};
+      tile.load_k(at, k_off);
     };
     auto load_v = [&](const int64_t (&off)[4]) {
-      const uint8_t* at[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        at[h] = vbase + (g < 2 ? off[2 * h] : off[2 * h + 1]) + 4 * (g & 1) * a.kv.slot_bytes;
-      tile.load_v(at, a.kv.slot_bytes, lane);
+      const uint8_t* const at[4] = {vbase + off[0], vbase + off[1], vbase + off[2], vbase + off[3]};
+      tile.load_v(at, a.kv.slot_bytes, v_off);
     };
 
     Octets now, next;
@@ -506,7 +548,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
       const int key0 = t * kTileKeys, tn = t + kAttnWaves;
       const bool more = tn < t_end;
       f32x4 s[2];
-      tile.scores(q, s);
+      tile.scores(q, (lane & 2) != 0, s);
       if (more) {
         place(next, tn * kTileKeys, off);
         load_k(off);
@@ -521,9 +563,9 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
         uint32_t there = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int key = key0 + 16 * (j >> 2) + 4 * g + (j & 3);
-          const int page = g < 2 ? now.page[2 * (j >> 2)] : now.page[2 * (j >> 2) + 1];
-          if (key >= first && key < n && (uint32_t)page < (uint32_t)a.kv.n_pages) there |= 1u << j;
+          const int key = key0 + 8 * (j >> 1) + 2 * g + (j & 1);
+          if (key >= first && key < n && (uint32_t)now.page[j >> 1] < (uint32_t)a.kv.n_pages)
+            there |= 1u << j;
           else z[j] = -INFINITY;
         }
         tile.clear_v(there);
@@ -578,7 +620,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
     float M = ms[0][l16];
 #pragma unroll
     for (int i = 1; i < kAttnWaves; ++i) M = fmaxf(M, ms[i][l16]);
-    const float mine = m == -INFINITY ? 0.f : exp2_hw(m - M);
+    const float mine = part_weight(m, M);
     if (l16 < heads) {
 #pragma unroll
       for (int c = 0; c < Tl::kDims; c += 4)
@@ -596,7 +638,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
       for (int i = 1; i < kAttnWaves; ++i) M = fmaxf(M, ms[i][h]);
       L = 0.f;
       for (int i = 0; i < kAttnWaves; ++i)
-        L += ms[i][h] == -INFINITY ? 0.f : ls[i][h] * exp2_hw(ms[i][h] - M);
+        L += ls[i][h] * part_weight(ms[i][h], M);
     };
     const float vs = kE4M3 && a.kv.v_scale ? a.kv.v_scale[hk] : 1.f;
     auto store_out = [&](int h, int d, float4 o, float M, float L) {
@@ -609,8 +651,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
         a.lse[grow * a.n_heads + head0 + h] =
             L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
     };
-    const int u0 = base * Y + y * units;  // this output's first unit
-    float* part = a.parts + (int64_t)(2 * w + (first_segment ? 0 : 1)) * a.part_floats;
+    float* part = a.parts + (int64_t)(2 * blockIdx.x + (first_segment ? 0 : 1)) * a.part_floats;
     for (int x = tid; x < heads * (kDh / 4); x += kThreads) {
       const int h = x / (kDh / 4), d = 4 * (x % (kDh / 4));
       float4 o = *reinterpret_cast<const float4*>(&os[0][h][d]);
@@ -636,47 +677,92 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
       }
     }
     if (!full) {
-      const int wa = u0 / run, wb = (u0 + units - 1) / run;
+      // The workers that share this output; the first one's ticket is theirs.
+      const int wa = base / run, wb = (base + units - 1) / run;
+      uint32_t* ticket = &a.tickets[(wa * Y + y) * kTicketStride];
       wait_memory();
       __syncthreads();
       if (tid == 0) {
-        last = __hip_atomic_fetch_add(&a.tickets[wa * kTicketStride], 1u, __ATOMIC_RELAXED,
+        last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED,
                                       __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(wb - wa);
         wait_memory();
       }
       __syncthreads();
       if (last) {
         const int parts = wb - wa + 1;
-        const int lead = u0 % run ? 1 : 0;  // the first one's last segment, or its first
+        const int lead = base % run ? 1 : 0;  // the first one's last segment, or its first
         auto part_at = [&](int i) {
-          return a.parts + (int64_t)(2 * (wa + i) + (i == 0 ? lead : 0)) * a.part_floats;
+          return a.parts + (int64_t)(2 * ((wa + i) * Y + y) + (i == 0 ? lead : 0)) * a.part_floats;
         };
-        for (int x = tid; x < heads * (kDh / 4); x += kThreads) {
-          const int h = x / (kDh / 4), d = 4 * (x % (kDh / 4));
-          float M = -INFINITY;
-          for (int i = 0; i < parts; ++i) M = fmaxf(M, __uint_as_float(ld_u32<true>(part_at(i) + h)));
-          float L = 0.f;
+        // Eight parts at a time, everything of theirs in flight at once; the
+        // parts are dealt over the threads that one part's outputs leave idle.
+        const int items = heads * (kDh / 4);
+        const int stripes = items < kThreads ? kThreads / items : 1;
+        for (int x = tid; x < items * stripes; x += kThreads) {
+          const int item = x % items, h = item / (kDh / 4), d = 4 * (item % (kDh / 4));
+          float M = -INFINITY, L = 0.f;
           float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int i = 0; i < parts; ++i) {
-            const float* p = part_at(i);
-            const float mi = __uint_as_float(ld_u32<true>(p + h));
-            const float f = mi == -INFINITY ? 0.f : exp2_hw(mi - M);
-            L += f * __uint_as_float(ld_u32<true>(p + 16 + h));
-            const uint64_t* v = reinterpret_cast<const uint64_t*>(p + 32 + h * kDh + d);
-            const uint64_t a0 = __hip_atomic_load(v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            const uint64_t a1 = __hip_atomic_load(v + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            o.x = fmaf(f, __uint_as_float((uint32_t)a0), o.x);
-            o.y = fmaf(f, __uint_as_float((uint32_t)(a0 >> 32)), o.y);
-            o.z = fmaf(f, __uint_as_float((uint32_t)a1), o.z);
-            o.w = fmaf(f, __uint_as_float((uint32_t)(a1 >> 32)), o.w);
+          constexpr int kAhead = 8;
+          for (int i0 = x / items; i0 < parts; i0 += kAhead * stripes) {
+            float m_of[kAhead], l_of[kAhead];
+            uint64_t lo[kAhead], hi[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+              const float* p = part_at(min(i0 + k * stripes, parts - 1));
+              const uint64_t* v = reinterpret_cast<const uint64_t*>(p + 32 + h * kDh + d);
+              m_of[k] = __uint_as_float(ld_u32<true>(p + h));
+              l_of[k] = __uint_as_float(ld_u32<true>(p + 16 + h));
+              lo[k] = __hip_atomic_load(v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+              hi[k] = __hip_atomic_load(v + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            float top = M;
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+              if (i0 + k * stripes >= parts) m_of[k] = -INFINITY;  // the last part again
+              top = fmaxf(top, m_of[k]);
+            }
+            const float shrink = part_weight(M, top);
+            M = top;
+            L *= shrink;
+            o.x *= shrink, o.y *= shrink, o.z *= shrink, o.w *= shrink;
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+              const float f = part_weight(m_of[k], M);
+              L = fmaf(f, l_of[k], L);
+              o.x = fmaf(f, __uint_as_float((uint32_t)lo[k]), o.x);
+              o.y = fmaf(f, __uint_as_float((uint32_t)(lo[k] >> 32)), o.y);
+              o.z = fmaf(f, __uint_as_float((uint32_t)hi[k]), o.z);
+              o.w = fmaf(f, __uint_as_float((uint32_t)(hi[k] >> 32)), o.w);
+            }
           }
-          store_out(h, d, o, M, L);
+          if (stripes == 1) {
+            store_out(h, d, o, M, L);
+          } else {
+            striped[x] = o;
+            striped_m[x] = M;
+            striped_l[x] = L;
+          }
         }
-        if (tid == 0) st_u32<true>(&a.tickets[wa * kTicketStride], 0);
+        if (stripes > 1) {
+          __syncthreads();
+          if (tid < items) {
+            float M = striped_m[tid], L = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int i = 1; i < stripes; ++i) M = fmaxf(M, striped_m[tid + i * items]);
+            for (int x = tid; x < items * stripes; x += items) {
+              const float f = part_weight(striped_m[x], M);
+              const float4 e = striped[x];
+              L = fmaf(f, striped_l[x], L);
+              o.x = fmaf(f, e.x, o.x), o.y = fmaf(f, e.y, o.y);
+              o.z = fmaf(f, e.z, o.z), o.w = fmaf(f, e.w, o.w);
+            }
+            store_out(tid / (kDh / 4), 4 * (tid % (kDh / 4)), o, M, L);
+          }
+        }
+        if (tid == 0) st_u32<true>(ticket, 0);
       }
     }
     u += c1 - c0;
-    if (c1 == units && y == Y - 1) ++row;
     first_segment = false;
   }
 }
@@ -784,7 +870,7 @@ void launch_append(const AppendArg& a, int head_dim, bool inter, dim3 grid, hipS
 
 template <class T, bool kE4M3>
 void launch_attend(const AttendArg& a, int head_dim, hipStream_t stream) {
-  const dim3 grid(a.workers);
+  const dim3 grid((unsigned)(a.workers * a.kv.n_kv_heads * a.q_tiles));
   if (head_dim == 64)
     hipLaunchKernelGGL((paged_attention_kernel<T, kE4M3, 64>), grid, dim3(kThreads), 0, stream, a);
   else if (head_dim == 128)
@@ -793,23 +879,25 @@ void launch_attend(const AttendArg& a, int head_dim, hipStream_t stream) {
     hipLaunchKernelGGL((paged_attention_kernel<T, kE4M3, 256>), grid, dim3(kThreads), 0, stream, a);
 }
 
-// How a call is launched: rows per launch (their units stay below 2^31), its
-// workgroups, and the floats of one workgroup's record for a split output.
+// How a call is launched: rows per launch (their units stay below 2^31), the
+// workers of each line and the lines (key heads times tiles of 16 queries),
+// and the floats of one workgroup's record for a split output.
 struct AttendPlan {
   int64_t rows_per_launch;
-  int workers, part_floats;
+  int workers, lines, part_floats;
 };
-constexpr int kWorkers = 768;  // three workgroups per CU
-static_assert(kWorkers <= kTickets, "a ticket per workgroup");
+constexpr int kWorkers = 512;
 AttendPlan attend_plan(const emoe_paged_kv& kv, int32_t rows, int32_t n_heads, int32_t max_keys) {
   const int group = n_heads / kv.n_kv_heads;
-  const int64_t lines = (int64_t)kv.n_kv_heads * ((group + 15) / 16);
-  const int64_t most = lines * ((int64_t)max_keys / kUnitKeys + 2);  // units of one row
+  const int64_t most = (int64_t)max_keys / kUnitKeys + 2;  // units of one row
   AttendPlan p;
+  p.lines = kv.n_kv_heads * ((group + 15) / 16);
   p.rows_per_launch = (((int64_t)1 << 31) - 1 - kTickets) / most;
   if (p.rows_per_launch > kMaxRows) p.rows_per_launch = kMaxRows;
   const int64_t held = rows < p.rows_per_launch ? rows : p.rows_per_launch;
-  p.workers = (int)(held * most < kWorkers ? held * most : kWorkers);
+  int64_t workers = kWorkers / p.lines;
+  if (workers < 1) workers = 1;
+  p.workers = (int)(held * most < workers ? held * most : workers);
   p.part_floats = 32 + (group < 16 ? group : 16) * kv.head_dim;
   return p;
 }
@@ -887,7 +975,7 @@ size_t emoe_paged_attention_workspace_bytes(const emoe_paged_kv* kv, int32_t row
                                             int32_t max_keys) {
   if (check_kv(kv) || rows < 0 || n_heads < 1 || n_heads % kv->n_kv_heads || max_keys < 0) return 0;
   const AttendPlan p = attend_plan(*kv, rows, n_heads, max_keys);
-  return EMOE_SERVING_TICKET_BYTES + (size_t)2 * p.workers * p.part_floats * 4;
+  return EMOE_SERVING_TICKET_BYTES + (size_t)2 * p.workers * p.lines * p.part_floats * 4;
 }
 
 int32_t emoe_paged_attention(const emoe_paged_kv* kv, const emoe_paged_attention_args* args,
@@ -915,8 +1003,6 @@ int32_t emoe_paged_attention(const emoe_paged_kv* kv, const emoe_paged_attention
                         need);
   if (!aligned16(workspace)) return report_error(EMOE_EINVAL, "workspace: need 16-byte alignment");
   const AttendPlan plan = attend_plan(*kv, A.rows, A.n_heads, A.max_keys);
-  if (plan.rows_per_launch < 1)
-    return report_error(EMOE_ESHAPE, "max_keys %d with %d heads", A.max_keys, A.n_heads);
   AttendArg a;
   a.kv = view_of(*kv);
   a.q = static_cast<const uint16_t*>(A.q);

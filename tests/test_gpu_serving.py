@@ -415,6 +415,24 @@ def test_attention_without_a_finite_score():
         assert torch.isnan(out).all()
 
 
+@pytest.mark.parametrize("n", [5, 128, 3000])
+def test_attention_of_nan(n):
+    """A query of NaN has NaN outputs, however its row is split; its neighbours do not notice."""
+    c = Cache("bf16", 400, 8, 1, 64, 0)
+    c.fill([(p, s) for p in range(400) for s in range(8)])
+    q = torch.randn(3, 2, 64, device="cuda:0").to(torch.bfloat16)
+    out, lse, ok = torch.empty_like(q), torch.empty(3, 2, device="cuda:0"), torch.empty_like(q)
+    ws = torch.zeros(api.paged_attention_workspace_bytes(c.kv, 3, 2, n), dtype=torch.uint8, device="cuda:0")
+    args = (gpu(np.tile(np.arange(400, dtype=np.int32), (3, 1))), ids([n] * 3))
+    api.paged_attention(c.kv, q, *args, ok, ws, n)
+    q[1, 0] = math.nan
+    api.paged_attention(c.kv, q, *args, out, ws, n, lse=lse)
+    assert torch.isnan(out[1, 0]).all() and torch.isnan(lse[1, 0])
+    ok[1, 0] = 0
+    out[1, 0] = 0
+    assert torch.equal(out, ok)
+
+
 def test_attention_offsets_past_32_bits():
     """A pool above 8 GiB: the pages at its two ends."""
     page, hk, d = 64, 8, 128
