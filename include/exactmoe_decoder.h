@@ -84,7 +84,7 @@ int32_t emoe_decoder_destroy(emoe_decoder* dec);
  * then the head on the last token: logits (device f32 [V]) and the greedy
  * next token (device int32 [1]; ties to the lower id).  A prompt is one call
  * with pos0 = 0; each decode step is a call with T = 1.  pos0 + T must not
- * exceed max_positions.  stats (nullable) accumulates the MoE layers'
+ * exceed max_positions.  EMOE_ESTATE without a KV cache.  stats (nullable) accumulates the MoE layers'
  * counters.  Blocks the host when a layer's cache is not fully resident
  * (emoe_moe_forward's batched expert-id transfer). */
 int32_t emoe_decoder_forward(emoe_decoder* dec, const int32_t* tokens, int32_t T, int32_t pos0,

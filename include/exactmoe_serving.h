@@ -176,6 +176,46 @@ size_t emoe_process_logits_workspace_bytes(int32_t rows, int32_t vocab);
 int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_t workspace_bytes,
                             hipStream_t stream);
 
+/* ---------------------------------------------------------------- the decoder over a paged cache */
+/* Tokens of many sequences in one call of the synthetic decoder: prompts,
+ * parts of prompts and decode steps, mixed as the caller likes. */
+typedef struct emoe_decoder_batch {
+  const int32_t* tokens;      /* device [n_tokens], ids outside [0, V) are clamped */
+  const int32_t* positions;   /* device [n_tokens] */
+  const int32_t* seqs;        /* device [n_tokens], or NULL: token t is of sequence t */
+  const int32_t* page_table;  /* device [n_seqs][table_width], for every layer */
+  const int32_t* out_rows;    /* device [n_out]: tokens whose logits are wanted (clamped to the call's
+                                 tokens), or NULL: all (n_out = n_tokens) */
+  int64_t table_stride;
+  int32_t n_tokens, n_seqs, table_width;
+  int32_t n_out;              /* 1 .. n_tokens */
+  int32_t max_keys;           /* bound of positions[] + 1 */
+} emoe_decoder_batch;
+
+/* Workspace of emoe_decoder_forward_paged; needs no initial value, since the
+ * call clears its tickets itself. */
+size_t emoe_decoder_paged_workspace_bytes(const emoe_decoder_dims* dims, int32_t n_tokens,
+                                          int32_t n_out, int32_t max_keys);
+
+/* As emoe_decoder_forward, with emoe_paged_append and emoe_paged_attention per
+ * layer in place of the contiguous cache, and emoe_process_logits at the end.
+ *   kv: host array of n_layers caches with n_heads key heads of head_dim, bf16
+ *       or e4m3; pages are written at the tokens' positions, and the positions
+ *       before them that a token attends to must hold earlier tokens';
+ *   logits: device f32 [n_out][V], after processing;
+ *   process: penalties, biases and masks of the n_out rows (the arrays and
+ *       their widths and strides; the other fields are not read), or NULL;
+ *   next_token: device int32 [n_out], or NULL.
+ * A token with seqs[t] outside [0, n_seqs) or a negative position is padding:
+ * it appends nothing and attends to nothing; its logits mean nothing.
+ * Captured into a graph as emoe_moe_forward is: with fully resident experts,
+ * and up to 4 tokens per call (more take rocBLAS, whose calls choose memory). */
+int32_t emoe_decoder_forward_paged(emoe_decoder* dec, const emoe_paged_kv* kv,
+                                   const emoe_decoder_batch* batch, float* logits,
+                                   const emoe_logits_args* process, int32_t* next_token,
+                                   void* workspace, size_t workspace_bytes, hipStream_t stream,
+                                   emoe_stats* stats);
+
 #ifdef __cplusplus
 }
 #endif

@@ -92,6 +92,13 @@ class LogitsArgs(C.Structure):
                                             "bias_width", "n_masks")])
 
 
+class DecoderBatch(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("tokens", "positions", "seqs", "page_table", "out_rows")]
+                + [("table_stride", C.c_int64)]
+                + [(n, C.c_int32) for n in ("n_tokens", "n_seqs", "table_width", "n_out",
+                                            "max_keys")])
+
+
 _vp = C.c_void_p
 _i32 = C.c_int32
 _i32p = C.POINTER(C.c_int32)
@@ -145,6 +152,10 @@ SIGNATURES = {
                                     C.c_size_t, _vp]),
     "emoe_process_logits_workspace_bytes": (C.c_size_t, [_i32, _i32]),
     "emoe_process_logits": (_i32, [C.POINTER(LogitsArgs), _vp, C.c_size_t, _vp]),
+    "emoe_decoder_paged_workspace_bytes": (C.c_size_t, [C.POINTER(DecoderDims), _i32, _i32, _i32]),
+    "emoe_decoder_forward_paged": (_i32, [_vp, C.POINTER(PagedKVView), C.POINTER(DecoderBatch), _vp,
+                                          C.POINTER(LogitsArgs), _vp, _vp, C.c_size_t, _vp,
+                                          C.POINTER(Stats)]),
     "emoe_profile_begin": (_i32, [_i32]),
     "emoe_profile_end": (_i32, [_vp, _vp, _i32, _i32p]),
 }

@@ -12,7 +12,7 @@ import math
 import numpy as np
 
 from . import _lib
-from ._lib import (DecoderDims, DecoderWeights, Dims, LogitsArgs, PagedAppendArgs,
+from ._lib import (DecoderBatch, DecoderDims, DecoderWeights, Dims, LogitsArgs, PagedAppendArgs,
                    PagedAttentionArgs, PagedKVView, Stats, WsLayout, check, lib,
                    EMOE_BF16, EMOE_E4M3, EMOE_EINVAL, EMOE_F16, EMOE_F32, EMOE_PATH_AUTO, EMOE_PATH_GEMV, EMOE_PATH_MFMA, EMOE_PATH_MIXED,
                    EMOE_MIXED_MFMA_ROWS, ExactMoEError)
@@ -223,9 +223,9 @@ class Decoder:
     weights: dict of device bf16 tensors: embed [V][d], lm_head [V][d],
     final_norm [d], and per-layer lists attn_norm, wqkv [3d][d], wo [d][d],
     moe_norm, w_router [E][d].  caches: list of Cache (one per layer).
-    kv: device buffer of decoder_kv_bytes(dd) bytes."""
+    kv: device buffer of decoder_kv_bytes(dd) bytes, or None for forward_paged only."""
 
-    def __init__(self, dd: DecoderDims, weights: dict, caches, kv):
+    def __init__(self, dd: DecoderDims, weights: dict, caches, kv=None):
         n = dd.n_layers
         arr = lambda name: (C.c_void_p * n)(*[_ptr(t) for t in weights[name]])
         self._arrays = {k: arr(k) for k in ("attn_norm", "wqkv", "wo", "moe_norm", "w_router")}
@@ -266,6 +266,34 @@ class Decoder:
                                          _ptr(logits), _ptr(next_token), _ptr(workspace), nbytes,
                                          _stream(stream),
                                          C.byref(stats) if stats is not None else None))
+
+    def forward_paged(self, kvs, tokens, positions, page_table, logits, workspace, max_keys: int,
+                      seqs=None, out_rows=None, next_token=None, stream=None,
+                      stats: Stats | None = None, **processing) -> None:
+        """emoe_decoder_forward_paged: tokens, positions (device int32 [n], of sequences seqs [n] or
+        0 .. n-1) over one PagedKV per layer; logits f32 [n or len(out_rows)][V], after the
+        `processing` (process_logits' history, penalties, biases and mask) of their rows."""
+        dev, n = tokens.device, tokens.shape[0]
+        rows = n if out_rows is None else out_rows.shape[0]
+        if len(kvs) != self.dims.n_layers or any(kv.device != dev for kv in kvs):
+            _refuse(f"need {self.dims.n_layers} caches on {dev}")
+        vocab = self.dims.vocab
+        lp = _array(logits, "logits", EMOE_F32, (rows, vocab), dev)
+        if rows > 1 and logits.stride(0) != vocab:
+            _refuse("logits must be contiguous")
+        batch = DecoderBatch(_array(tokens, "tokens", -1, (n,), dev),
+                             _array(positions, "positions", -1, (n,), dev),
+                             _array(seqs, "seqs", -1, (n,), dev),
+                             _array(page_table, "page_table", -1, (None, None), dev),
+                             _array(out_rows, "out_rows", -1, (rows,), dev), page_table.stride(0), n,
+                             page_table.shape[0], page_table.shape[1], rows, max_keys)
+        process = _processing(dev, rows, vocab, **processing)
+        nt = _array(next_token, "next_token", -1, (rows,), dev)
+        views = (PagedKVView * len(kvs))(*[kv.view for kv in kvs])
+        wp, wn = _workspace(workspace, dev)
+        fn, tail = lib().emoe_decoder_forward_paged, C.byref(stats) if stats is not None else None
+        _call(lambda *a: fn(*a, tail), dev, stream, self.handle, views, C.byref(batch), lp,
+              C.byref(process), nt, wp, wn)
 
 
 # ---------------------------------------------------------------- many sequences at once
@@ -439,6 +467,37 @@ def process_logits_workspace_bytes(rows: int, vocab: int) -> int:
     return int(lib().emoe_process_logits_workspace_bytes(rows, vocab))
 
 
+def _processing(dev, rows: int, vocab: int, history=None, history_lengths=None,
+                prompt_lengths=None, repetition=None, presence=None, frequency=None, bias_ids=None,
+                bias_values=None, bias_counts=None, mask=None, mask_rows=None) -> LogitsArgs:
+    """The penalties, biases and masks of `rows` rows of logits, checked."""
+    args, row = LogitsArgs(), (rows,)
+    if history is not None:
+        args.history = _array(history, "history", -1, (rows, None), dev)
+        args.history_stride, args.history_width = history.stride(0), history.shape[1]
+    args.history_lengths = _array(history_lengths, "history_lengths", -1, row, dev)
+    args.prompt_lengths = _array(prompt_lengths, "prompt_lengths", -1, row, dev)
+    args.repetition = _array(repetition, "repetition", EMOE_F32, row, dev)
+    args.presence = _array(presence, "presence", EMOE_F32, row, dev)
+    args.frequency = _array(frequency, "frequency", EMOE_F32, row, dev)
+    if bias_ids is not None or bias_values is not None:
+        if bias_ids is None or bias_values is None:
+            _refuse("one of bias_ids and bias_values is missing")
+        args.bias_ids = _array(bias_ids, "bias_ids", -1, (rows, None), dev)
+        args.bias_values = _array(bias_values, "bias_values", EMOE_F32, tuple(bias_ids.shape), dev)
+        if rows > 1 and bias_ids.stride(0) != bias_values.stride(0):
+            _refuse("bias_ids and bias_values have different row strides")
+        args.bias_counts = _array(bias_counts, "bias_counts", -1, row, dev)
+        args.bias_stride, args.bias_width = bias_ids.stride(0), bias_ids.shape[1]
+    if mask is not None:
+        args.mask = _array(mask, "mask", -1, (None, None), dev)
+        if mask.shape[1] * 32 < vocab:
+            _refuse(f"mask: {mask.shape[1]} words for a vocabulary of {vocab}")
+        args.mask_stride, args.n_masks = mask.stride(0), mask.shape[0]
+    args.mask_rows = _array(mask_rows, "mask_rows", -1, row, dev)
+    return args
+
+
 def process_logits(logits, out=None, workspace=None, history=None, history_lengths=None,
                    prompt_lengths=None, repetition=None, presence=None, frequency=None,
                    bias_ids=None, bias_values=None, bias_counts=None, mask=None, mask_rows=None,
@@ -456,36 +515,18 @@ def process_logits(logits, out=None, workspace=None, history=None, history_lengt
     op, os = lp, logits.stride(0)
     if out is not None:
         op, os = _array(out, "out", code, (rows, vocab), dev), out.stride(0)
-    row = (rows,)
-    args = LogitsArgs(lp, op, _array(next_token, "next_token", -1, row, dev),
-                      _array(history, "history", -1, (rows, None), dev),
-                      _array(history_lengths, "history_lengths", -1, row, dev),
-                      _array(prompt_lengths, "prompt_lengths", -1, row, dev),
-                      _array(repetition, "repetition", EMOE_F32, row, dev),
-                      _array(presence, "presence", EMOE_F32, row, dev),
-                      _array(frequency, "frequency", EMOE_F32, row, dev))
+    args = _processing(dev, rows, vocab, history, history_lengths, prompt_lengths, repetition,
+                       presence, frequency, bias_ids, bias_values, bias_counts, mask, mask_rows)
+    args.logits, args.out = lp, op
+    args.next_token = _array(next_token, "next_token", -1, (rows,), dev)
     args.logits_stride, args.out_stride = logits.stride(0), os
     args.dtype, args.rows, args.vocab = code, rows, vocab
-    if history is not None:
-        args.history_stride, args.history_width = history.stride(0), history.shape[1]
-    if bias_ids is not None or bias_values is not None:
-        width = (bias_ids if bias_ids is not None else bias_values).shape[1]
-        args.bias_ids = _array(bias_ids, "bias_ids", -1, (rows, width), dev)
-        args.bias_values = _array(bias_values, "bias_values", EMOE_F32, (rows, width), dev)
-        args.bias_counts = _array(bias_counts, "bias_counts", -1, row, dev)
-        if bias_ids is not None and bias_values is not None and \
-                rows > 1 and bias_ids.stride(0) != bias_values.stride(0):
-            _refuse("bias_ids and bias_values have different row strides")
-        args.bias_stride, args.bias_width = (bias_ids if bias_ids is not None
-                                             else bias_values).stride(0), width
-    if mask is not None:
-        args.mask = _array(mask, "mask", -1, (None, None), dev)
-        if mask.shape[1] * 32 < vocab:
-            _refuse(f"mask: {mask.shape[1]} words for a vocabulary of {vocab}")
-        args.mask_stride, args.n_masks = mask.stride(0), mask.shape[0]
-    args.mask_rows = _array(mask_rows, "mask_rows", -1, row, dev)
     wp, wn = _workspace(workspace, dev)
     _call(lib().emoe_process_logits, dev, stream, C.byref(args), wp, wn)
+
+
+def decoder_paged_workspace_bytes(dd: DecoderDims, n_tokens: int, n_out: int, max_keys: int) -> int:
+    return int(lib().emoe_decoder_paged_workspace_bytes(C.byref(dd), n_tokens, n_out, max_keys))
 
 
 def profile_begin(max_kernels: int) -> None:
@@ -509,5 +550,5 @@ __all__ = ["Dims", "Stats", "WsLayout", "ExactMoEError", "EMOE_PATH_AUTO", "EMOE
            "moe_forward", "moe_forward_noalloc", "decoder_dims", "decoder_kv_bytes",
            "decoder_workspace_bytes", "Decoder", "moe_forward_sequential", "test_fail_copy_after", "profile_begin", "profile_end",
            "PagedKV", "rope_frequencies", "paged_append", "paged_attention",
-           "paged_attention_workspace_bytes", "process_logits", "process_logits_workspace_bytes",
+           "paged_attention_workspace_bytes", "decoder_paged_workspace_bytes", "process_logits", "process_logits_workspace_bytes",
            "lib"]

@@ -12,7 +12,7 @@
 
 #include "common.h"
 #include "device_rope.h"
-#include "exactmoe_decoder.h"
+#include "serving.h"
 
 using namespace emoe;
 
@@ -183,6 +183,11 @@ __global__ __launch_bounds__(kThreads) void dense_gemv_kernel(int N, int K, cons
     }
 }
 
+// Angular frequencies base^(-2i/Dh) of a decoder, fp64, formed when it is made.
+struct RopeTable {
+  double inv[kMaxHeadDim / 2];
+};
+
 // x[t] = embed[clamp(tokens[t])], one workgroup per token, 16-byte copies.
 __global__ __launch_bounds__(kThreads) void embed_kernel(int V, int d, const int32_t* tokens,
                                                          const uint16_t* embed, uint16_t* x) {
@@ -192,6 +197,38 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(int V, int d, const int
   const uint4* src = reinterpret_cast<const uint4*>(embed + (int64_t)tok * d);
   uint4* dst = reinterpret_cast<uint4*>(x + (int64_t)t * d);
   for (int i = threadIdx.x; i < d / 8; i += kThreads) dst[i] = src[i];
+}
+
+// The beginning of a call over paged caches: embed_kernel's rows, each token's
+// number of keys (its own position included; 0 for padding), the rotation's
+// frequencies in memory, and the attention's tickets cleared (by the
+// workgroups from n_tokens on).
+struct PagedStart {
+  const int32_t *tokens, *positions, *seqs;
+  int32_t* lengths;
+  double* inv_freq;
+  uint4* tickets;
+  int32_t n_tokens, n_seqs, half;
+};
+__global__ __launch_bounds__(kThreads) void paged_start_kernel(int V, int d, PagedStart a,
+                                                               RopeTable rope, const uint16_t* embed,
+                                                               uint16_t* x) {
+  const int t = blockIdx.x;
+  if (t >= a.n_tokens) {
+    const int i = (t - a.n_tokens) * kThreads + threadIdx.x;
+    if (i < EMOE_SERVING_TICKET_BYTES / 16) a.tickets[i] = make_uint4(0, 0, 0, 0);
+    if (t == a.n_tokens && threadIdx.x < a.half) a.inv_freq[threadIdx.x] = rope.inv[threadIdx.x];
+    return;
+  }
+  int tok = a.tokens[t];
+  tok = tok < 0 ? 0 : (tok >= V ? V - 1 : tok);
+  const uint4* src = reinterpret_cast<const uint4*>(embed + (int64_t)tok * d);
+  uint4* dst = reinterpret_cast<uint4*>(x + (int64_t)t * d);
+  for (int i = threadIdx.x; i < d / 8; i += kThreads) dst[i] = src[i];
+  if (threadIdx.x == 0) {
+    const int p = a.positions[t], s = a.seqs ? a.seqs[t] : t;
+    a.lengths[t] = p >= 0 && p < INT32_MAX && (uint32_t)s < (uint32_t)a.n_seqs ? p + 1 : 0;
+  }
 }
 
 // Sum over the workgroup in a fixed order (wavefront butterflies, then the
@@ -218,13 +255,21 @@ __device__ __forceinline__ float block_max(float v, float* red) {
 
 // Per token row: if delta, x = bf16(x + delta) (written back); then
 // out = bf16(x / sqrt(mean(x^2) + eps) * g), in fp32.  d is a multiple of 8
-// and at most 8 * 256 * 4 (four 8-element chunks per thread).
+// and at most 8 * 256 * 4 (four 8-element chunks per thread).  kPick: row t of
+// out is that of token rows[t] (clamped to the call's tokens; null: t), and x
+// stays as it is.
+struct PickRows {
+  const int32_t* rows;
+  int32_t tokens;
+};
+template <bool kPick>
 __global__ __launch_bounds__(kThreads) void add_rmsnorm_kernel(int d, uint16_t* x,
                                                                const uint16_t* delta,
                                                                const uint16_t* g, float eps,
-                                                               uint16_t* out) {
+                                                               uint16_t* out, PickRows pick) {
   __shared__ float red[4];
-  const int t = blockIdx.x;
+  int t = blockIdx.x;
+  if (kPick && pick.rows) t = max(0, min(pick.rows[t], pick.tokens - 1));
   uint4* xr = reinterpret_cast<uint4*>(x + (int64_t)t * d);
   const uint4* dr = delta ? reinterpret_cast<const uint4*>(delta + (int64_t)t * d) : nullptr;
   const int n8 = d / 8;
@@ -245,7 +290,7 @@ __global__ __launch_bounds__(kThreads) void add_rmsnorm_kernel(int d, uint16_t* 
         const float hi = bf16_to_f32(w[p] >> 16) + bf16_to_f32(u[p] >> 16);
         w[p] = f32_to_bf16_rne(lo) | (f32_to_bf16_rne(hi) << 16);
       }
-      xr[i] = make_uint4(w[0], w[1], w[2], w[3]);
+      if (!kPick) xr[i] = make_uint4(w[0], w[1], w[2], w[3]);
     }
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
@@ -257,7 +302,7 @@ __global__ __launch_bounds__(kThreads) void add_rmsnorm_kernel(int d, uint16_t* 
   }
   const float inv = 1.0f / sqrtf(block_sum(ss, red) / (float)d + eps);
   const uint4* gr = reinterpret_cast<const uint4*>(g);
-  uint4* orow = reinterpret_cast<uint4*>(out + (int64_t)t * d);
+  uint4* orow = reinterpret_cast<uint4*>(out + (int64_t)blockIdx.x * d);
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
     const int i = threadIdx.x + c * kThreads;
@@ -274,11 +319,6 @@ __global__ __launch_bounds__(kThreads) void add_rmsnorm_kernel(int d, uint16_t* 
     orow[i] = make_uint4(o[0], o[1], o[2], o[3]);
   }
 }
-
-// Angular frequencies base^(-2i/Dh) of a decoder, fp64, formed when it is made.
-struct RopeTable {
-  double inv[kMaxHeadDim / 2];
-};
 
 // Rotary positions on q (in place in qkv) and k, and the cache append of k
 // and v, for token t at position pos0 + t.  Element i < Dh/2 of a head pairs
@@ -643,6 +683,43 @@ struct WsLayout {
   size_t x0, x1, n, qkv, attn, moe_y, moe_ws, moe_ws_bytes, total;
 };
 
+// What a call over paged caches has besides: tickets first, as the attention's
+// and the logits' workspace begins, which `shared` serves.
+struct PagedLayout {
+  size_t shared, shared_bytes, lengths, inv_freq, base, total;
+};
+
+WsLayout decoder_ws_layout(const emoe_decoder_dims& dd, int T);
+
+PagedLayout paged_layout(const emoe_decoder_dims& dd, int T, int n_out, int max_keys) {
+  emoe_paged_kv kv{};  // any cache of the decoder's heads: sizes only
+  kv.k_pages = kv.v_pages = reinterpret_cast<void*>(256);
+  kv.slot_stride = dd.moe.d_model;
+  kv.head_stride = dd.head_dim;
+  kv.page_stride = 8 * (int64_t)dd.moe.d_model;
+  kv.dtype = EMOE_BF16;
+  kv.n_pages = 1;
+  kv.page_size = 8;
+  kv.n_kv_heads = dd.n_heads;
+  kv.head_dim = dd.head_dim;
+  PagedLayout L{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += align_up(bytes);
+    return at;
+  };
+  const size_t attn = emoe_paged_attention_workspace_bytes(&kv, T, dd.n_heads, max_keys);
+  const size_t logits = emoe_process_logits_workspace_bytes(n_out, dd.vocab);
+  L.shared_bytes = attn > logits ? attn : logits;
+  L.shared = take(L.shared_bytes);
+  L.lengths = take((size_t)T * 4);
+  L.inv_freq = take(sizeof(RopeTable));
+  L.base = take(decoder_ws_layout(dd, T).total);
+  L.total = off;
+  return L;
+}
+
 WsLayout decoder_ws_layout(const emoe_decoder_dims& dd, int T) {
   WsLayout L{};
   const size_t d = dd.moe.d_model;
@@ -758,7 +835,7 @@ int32_t emoe_decoder_create(const emoe_decoder_dims* dims, const emoe_decoder_we
                             emoe_cache* const* caches, void* kv_cache, emoe_decoder** out) {
   int32_t st = check_decoder_dims(dims);
   if (st) return st;
-  if (!w || !caches || !kv_cache || !out) return report_error(EMOE_EINVAL, "NULL argument");
+  if (!w || !caches || !out) return report_error(EMOE_EINVAL, "NULL argument");
   *out = nullptr;
   const int L = dims->n_layers;
   if (!w->embed || !w->lm_head || !w->final_norm || !w->attn_norm || !w->wqkv || !w->wo ||
@@ -819,6 +896,7 @@ int32_t emoe_decoder_forward(emoe_decoder* dec, const int32_t* tokens, int32_t T
                         T, pos0, D.max_positions);
   if (!tokens || !logits || !next_token || !workspace)
     return report_error(EMOE_EINVAL, "NULL tokens, logits, next_token or workspace");
+  if (!dec->kv) return report_error(EMOE_ESTATE, "the decoder was created without a KV cache");
   const WsLayout L = decoder_ws_layout(D, T);
   if (ws_bytes < L.total)
     return report_error(EMOE_EINVAL, "workspace of %zu bytes < %zu needed", ws_bytes, L.total);
@@ -854,8 +932,8 @@ int32_t emoe_decoder_forward(emoe_decoder* dec, const int32_t* tokens, int32_t T
         return st;
       if (delta) std::swap(xa, xb);  // xa is x + delta
     } else {
-      DEC_LAUNCH(add_rmsnorm_kernel, dim3(T), dim3(kThreads), 0, stream, d, xa, delta,
-                 dec->attn_norm[l], D.rms_eps, n);
+      DEC_LAUNCH(add_rmsnorm_kernel<false>, dim3(T), dim3(kThreads), 0, stream, d, xa, delta,
+                 dec->attn_norm[l], D.rms_eps, n, PickRows());
       if ((st = dense(dec, T, 3 * d, d, n, dec->wqkv[l], nullptr, qkv, false, stream))) return st;
     }
     if (step_attn) {
@@ -879,8 +957,8 @@ int32_t emoe_decoder_forward(emoe_decoder* dec, const int32_t* tokens, int32_t T
     }
     if ((st = dense(dec, T, d, d, attn, dec->wo[l], xa, xb, false, stream))) return st;  // x += attn Wo^T
     std::swap(xa, xb);
-    DEC_LAUNCH(add_rmsnorm_kernel, dim3(T), dim3(kThreads), 0, stream, d, xa, nullptr,
-               dec->moe_norm[l], D.rms_eps, n);
+    DEC_LAUNCH(add_rmsnorm_kernel<false>, dim3(T), dim3(kThreads), 0, stream, d, xa, nullptr,
+               dec->moe_norm[l], D.rms_eps, n, PickRows());
     if ((st = emoe_moe_forward(dec->caches[l], T, n, dec->w_router[l], nullptr, D.renormalize,
                                EMOE_PATH_AUTO, moe_y, moe_ws, L.moe_ws_bytes, stream, stats)))
       return st;
@@ -893,12 +971,148 @@ int32_t emoe_decoder_forward(emoe_decoder* dec, const int32_t* tokens, int32_t T
     if ((st = dense_gemv<true>(1, D.vocab, d, xa + last, dec->lm_head, nullptr, logits, true, nm, stream)))
       return st;
   } else {
-    DEC_LAUNCH(add_rmsnorm_kernel, dim3(1), dim3(kThreads), 0, stream, d, xa + last, delta + last,
-               dec->final_norm, D.rms_eps, n);
+    DEC_LAUNCH(add_rmsnorm_kernel<false>, dim3(1), dim3(kThreads), 0, stream, d, xa + last, delta + last,
+               dec->final_norm, D.rms_eps, n, PickRows());
     if ((st = dense(dec, 1, D.vocab, d, n, dec->lm_head, nullptr, logits, true, stream))) return st;
   }
   DEC_LAUNCH(argmax_kernel, dim3(1), dim3(1024), 0, stream, D.vocab, logits, next_token);
   return EMOE_OK;
+}
+
+size_t emoe_decoder_paged_workspace_bytes(const emoe_decoder_dims* dims, int32_t n_tokens,
+                                          int32_t n_out, int32_t max_keys) {
+  if (check_decoder_dims(dims) != EMOE_OK || n_tokens < 1 || n_out < 1 || n_out > n_tokens || max_keys < 0)
+    return 0;
+  return paged_layout(*dims, n_tokens, n_out, max_keys).total;
+}
+
+int32_t emoe_decoder_forward_paged(emoe_decoder* dec, const emoe_paged_kv* kv,
+                                   const emoe_decoder_batch* batch, float* logits,
+                                   const emoe_logits_args* process, int32_t* next_token,
+                                   void* workspace, size_t ws_bytes, hipStream_t stream,
+                                   emoe_stats* stats) {
+  if (!dec) return report_error(EMOE_EINVAL, "decoder is NULL");
+  if (!kv || !batch || !logits || !workspace)
+    return report_error(EMOE_EINVAL, "NULL kv, batch, logits or workspace");
+  const emoe_decoder_dims& D = dec->dims;
+  const emoe_decoder_batch& B = *batch;
+  const int T = B.n_tokens, n_out = B.n_out;
+  if (T < 1 || n_out < 1 || B.max_keys < 0)
+    return report_error(EMOE_EINVAL, "n_tokens %d, n_out %d, max_keys %d", T, n_out, B.max_keys);
+  if (B.out_rows ? n_out > T : n_out != T)
+    return report_error(EMOE_EINVAL, "n_out %d of n_tokens %d: need at most as many, all without out_rows",
+                        n_out, T);
+  if (!B.tokens || !B.positions) return report_error(EMOE_EINVAL, "NULL tokens or positions");
+  const int d = D.moe.d_model, H = D.n_heads, Dh = D.head_dim;
+  int32_t st;
+  for (int l = 0; l < D.n_layers; ++l) {
+    if ((st = emoe_check_paged_kv(&kv[l]))) return st;
+    if (kv[l].n_kv_heads != H || kv[l].head_dim != Dh || kv[l].dtype == EMOE_F16)
+      return report_error(EMOE_ESHAPE, "cache of layer %d: need %d key heads of %d, bf16 or e4m3", l, H, Dh);
+  }
+  if (!aligned16(workspace)) return report_error(EMOE_EINVAL, "workspace: need 16-byte alignment");
+  const PagedLayout P = paged_layout(D, T, n_out, B.max_keys);
+  if (ws_bytes < P.total)
+    return report_error(EMOE_EINVAL, "workspace of %zu bytes < %zu needed", ws_bytes, P.total);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const WsLayout L = decoder_ws_layout(D, T);
+  auto at = [&](size_t off) { return reinterpret_cast<uint16_t*>(ws + P.base + off); };
+  uint16_t *xa = at(L.x0), *xb = at(L.x1), *n = at(L.n), *qkv = at(L.qkv), *attn = at(L.attn),
+           *moe_y = at(L.moe_y);
+  int32_t* lengths = reinterpret_cast<int32_t*>(ws + P.lengths);
+  double* inv_freq = reinterpret_cast<double*>(ws + P.inv_freq);
+
+  // The arguments of every layer's calls, which differ in their cache only, and
+  // of the logits; what the caller gave of them is checked before anything runs.
+  emoe_paged_append_args ap{};
+  ap.q = ap.q_out = qkv;
+  ap.k = qkv + d;
+  ap.v = qkv + 2 * d;
+  ap.q_stride = ap.k_stride = ap.v_stride = ap.q_out_stride = 3 * (int64_t)d;
+  ap.positions = B.positions;
+  ap.seqs = B.seqs;
+  ap.page_table = B.page_table;
+  ap.table_stride = B.table_stride;
+  ap.inv_freq = inv_freq;
+  ap.dtype = EMOE_BF16;
+  ap.n_heads = H;
+  ap.n_seqs = B.n_seqs;
+  ap.table_width = B.table_width;
+  ap.rotary_dim = Dh;
+  if ((st = emoe_paged_append(&kv[0], &ap, stream))) return st;  // no tokens yet: checks only
+  ap.tokens = T;
+  emoe_paged_attention_args at_args{};
+  at_args.q = qkv;
+  at_args.out = attn;
+  at_args.q_stride = 3 * (int64_t)d;
+  at_args.out_stride = d;
+  at_args.lengths = lengths;
+  at_args.seqs = B.seqs;
+  at_args.page_table = B.page_table;
+  at_args.table_stride = B.table_stride;
+  at_args.scale = 1.0f / std::sqrt((float)Dh);
+  at_args.dtype = EMOE_BF16;
+  at_args.rows = T;
+  at_args.n_heads = H;
+  at_args.n_seqs = B.n_seqs;
+  at_args.table_width = B.table_width;
+  at_args.max_keys = B.max_keys;
+  emoe_logits_args lg{};
+  if (process) lg = *process;
+  lg.logits = lg.out = logits;
+  lg.next_token = next_token;
+  lg.logits_stride = lg.out_stride = D.vocab;
+  lg.dtype = EMOE_F32;
+  lg.rows = n_out;
+  lg.vocab = D.vocab;
+  if ((st = check_process_logits(lg, ws + P.shared, P.shared_bytes))) return st;
+
+  const rocblas_status rs = rocblas_set_stream(dec->blas, stream);
+  if (rs != rocblas_status_success)
+    return report_error(EMOE_EHIP, "rocblas_set_stream: %s", rocblas_name(rs));
+  PagedStart start;
+  start.tokens = B.tokens;
+  start.positions = B.positions;
+  start.seqs = B.seqs;
+  start.lengths = lengths;
+  start.inv_freq = inv_freq;
+  start.tickets = reinterpret_cast<uint4*>(ws + P.shared);
+  start.n_tokens = T;
+  start.n_seqs = B.n_seqs;
+  start.half = Dh / 2;
+  constexpr int kClear = (EMOE_SERVING_TICKET_BYTES / 16 + kThreads - 1) / kThreads;
+  static_assert(kMaxHeadDim / 2 <= kThreads, "a thread per frequency");
+  DEC_LAUNCH(paged_start_kernel, dim3(T + kClear), dim3(kThreads), 0, stream, D.vocab, d, start,
+             dec->rope, dec->embed, xa);
+  const uint16_t* delta = nullptr;
+  const bool norm_in_gemv = T <= kDenseMaxTokens && d <= kNormMaxInputs;
+  for (int l = 0; l < D.n_layers; ++l) {
+    if (norm_in_gemv) {
+      const NormInput nm{delta, dec->attn_norm[l], delta ? xb : nullptr, D.rms_eps};
+      if ((st = dense_gemv<true>(T, 3 * d, d, xa, dec->wqkv[l], nullptr, qkv, false, nm, stream)))
+        return st;
+      if (delta) std::swap(xa, xb);  // xa is x + delta
+    } else {
+      DEC_LAUNCH(add_rmsnorm_kernel<false>, dim3(T), dim3(kThreads), 0, stream, d, xa, delta,
+                 dec->attn_norm[l], D.rms_eps, n, PickRows());
+      if ((st = dense(dec, T, 3 * d, d, n, dec->wqkv[l], nullptr, qkv, false, stream))) return st;
+    }
+    if ((st = emoe_paged_append(&kv[l], &ap, stream))) return st;
+    if ((st = emoe_paged_attention(&kv[l], &at_args, ws + P.shared, P.shared_bytes, stream))) return st;
+    if ((st = dense(dec, T, d, d, attn, dec->wo[l], xa, xb, false, stream))) return st;  // x += attn Wo^T
+    std::swap(xa, xb);
+    DEC_LAUNCH(add_rmsnorm_kernel<false>, dim3(T), dim3(kThreads), 0, stream, d, xa, nullptr,
+               dec->moe_norm[l], D.rms_eps, n, PickRows());
+    if ((st = emoe_moe_forward(dec->caches[l], T, n, dec->w_router[l], nullptr, D.renormalize,
+                               EMOE_PATH_AUTO, moe_y, ws + P.base + L.moe_ws, L.moe_ws_bytes, stream,
+                               stats)))
+      return st;
+    delta = moe_y;
+  }
+  DEC_LAUNCH(add_rmsnorm_kernel<true>, dim3(n_out), dim3(kThreads), 0, stream, d, xa, delta,
+             dec->final_norm, D.rms_eps, n, PickRows{B.out_rows, T});
+  if ((st = dense(dec, n_out, D.vocab, d, n, dec->lm_head, nullptr, logits, true, stream))) return st;
+  return emoe_process_logits(&lg, ws + P.shared, P.shared_bytes, stream);
 }
 
 }  // extern "C"

@@ -414,18 +414,8 @@ void launch_type(const LogitsArg& a, const LogitsPlan& p, unsigned blocks, hipSt
 
 }  // namespace
 
-extern "C" {
-
-size_t emoe_process_logits_workspace_bytes(int32_t rows, int32_t vocab) {
-  if (rows < 0 || vocab < 1) return 0;
-  const size_t held = rows < kTickets ? rows : kTickets;  // rows of one launch
-  return EMOE_SERVING_TICKET_BYTES + held * (((size_t)vocab + 1023) / 1024) * kTicketLine;  // the smallest chunks
-}
-
-int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_t workspace_bytes,
-                            hipStream_t stream) {
-  if (!args) return report_error(EMOE_EINVAL, "args is NULL");
-  const emoe_logits_args& A = *args;
+int32_t emoe::check_process_logits(const emoe_logits_args& A, const void* workspace,
+                                   size_t workspace_bytes) {
   if (A.dtype != EMOE_F32 && A.dtype != EMOE_BF16 && A.dtype != EMOE_F16)
     return report_error(EMOE_EINVAL, "type %d: need f32, bf16 or fp16", A.dtype);
   if (A.rows < 0 || A.vocab < 1)
@@ -459,8 +449,6 @@ int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_
   } else if (A.mask_rows) {
     return report_error(EMOE_EINVAL, "mask_rows without a mask");
   }
-  const int per = A.dtype == EMOE_F32 ? 4 : 8;
-  const LogitsPlan plan = logits_plan(A.rows, A.vocab, per, A.history ? A.history_width : 0);
   if (A.next_token) {
     const size_t need = emoe_process_logits_workspace_bytes(A.rows, A.vocab);
     if (!workspace || workspace_bytes < need)
@@ -468,6 +456,25 @@ int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_
                           workspace ? workspace_bytes : 0, need);
     if (!aligned16(workspace)) return report_error(EMOE_EINVAL, "workspace: need 16-byte alignment");
   }
+  return EMOE_OK;
+}
+
+extern "C" {
+
+size_t emoe_process_logits_workspace_bytes(int32_t rows, int32_t vocab) {
+  if (rows < 0 || vocab < 1) return 0;
+  const size_t held = rows < kTickets ? rows : kTickets;  // rows of one launch
+  return EMOE_SERVING_TICKET_BYTES + held * (((size_t)vocab + 1023) / 1024) * kTicketLine;  // the smallest chunks
+}
+
+int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_t workspace_bytes,
+                            hipStream_t stream) {
+  if (!args) return report_error(EMOE_EINVAL, "args is NULL");
+  const emoe_logits_args& A = *args;
+  const int32_t st = check_process_logits(A, workspace, workspace_bytes);
+  if (st || A.rows == 0) return st;
+  const int per = A.dtype == EMOE_F32 ? 4 : 8;
+  const LogitsPlan plan = logits_plan(A.rows, A.vocab, per, A.history ? A.history_width : 0);
   LogitsArg a;
   a.logits = A.logits;
   a.out = A.out;

@@ -58,6 +58,10 @@ __device__ __forceinline__ uint2 down8_e4m3(const float (&v)[8]) {
 constexpr int kTicketLine = 128, kTicketStride = kTicketLine / 4;
 constexpr int kTickets = EMOE_SERVING_TICKET_BYTES / kTicketLine;
 
+// The argument checks of emoe_process_logits.
+int32_t check_process_logits(const emoe_logits_args& args, const void* workspace,
+                             size_t workspace_bytes);
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 }  // namespace emoe
