@@ -164,6 +164,7 @@ KERNEL_NAMES = ["router", "topk", "group", "gateup_gemv", "down_gemv", "gateup_m
                 "combine", "decode_fused", "row_bias", "group_count"]
 
 _lib = None
+_binding = None
 
 
 class ExactMoEError(RuntimeError):
@@ -185,6 +186,22 @@ def lib() -> C.CDLL:
             fn.argtypes = args
         _lib = h
     return _lib
+
+
+def binding():
+    """Load the binding's compiled half (csrc/binding.cpp) once; raises if it has not been built."""
+    global _binding
+    if _binding is None:
+        import torch  # noqa: F401  (its libraries are the binding's)
+        if not os.path.exists(os.path.join(_HERE, "_binding.so")):
+            raise RuntimeError("_binding.so is missing: run `python -m paper_2608_15383_amd.build`")
+        from . import _binding as b
+        h = lib()
+        b.init(ExactMoEError, *[C.cast(getattr(h, n), C.c_void_p).value for n in
+                                ("emoe_last_error", "emoe_paged_append", "emoe_paged_attention",
+                                 "emoe_process_logits", "emoe_decoder_forward_paged")])
+        _binding = b
+    return _binding
 
 
 def check(status: int) -> None:

@@ -7,14 +7,12 @@ torch.bfloat16 or int16/uint16 bit patterns; they are passed by data_ptr().
 from __future__ import annotations
 
 import ctypes as C
-import math
 
 import numpy as np
 
 from . import _lib
-from ._lib import (DecoderBatch, DecoderDims, DecoderWeights, Dims, LogitsArgs, PagedAppendArgs,
-                   PagedAttentionArgs, PagedKVView, Stats, WsLayout, check, lib,
-                   EMOE_BF16, EMOE_E4M3, EMOE_EINVAL, EMOE_F16, EMOE_F32, EMOE_PATH_AUTO, EMOE_PATH_GEMV, EMOE_PATH_MFMA, EMOE_PATH_MIXED,
+from ._lib import (DecoderDims, DecoderWeights, Dims, PagedKVView, Stats, WsLayout, binding, check,
+                   lib, EMOE_BF16, EMOE_E4M3, EMOE_EINVAL, EMOE_F16, EMOE_PATH_AUTO, EMOE_PATH_GEMV, EMOE_PATH_MFMA, EMOE_PATH_MIXED,
                    EMOE_MIXED_MFMA_ROWS, ExactMoEError)
 
 
@@ -269,108 +267,49 @@ class Decoder:
 
     def forward_paged(self, kvs, tokens, positions, page_table, logits, workspace, max_keys: int,
                       seqs=None, out_rows=None, next_token=None, stream=None,
-                      stats: Stats | None = None, **processing) -> None:
+                      stats: Stats | None = None, history=None, history_lengths=None,
+                      prompt_lengths=None, repetition=None, presence=None, frequency=None,
+                      bias_ids=None, bias_values=None, bias_counts=None, mask=None,
+                      mask_rows=None) -> None:
         """emoe_decoder_forward_paged: tokens, positions (device int32 [n], of sequences seqs [n] or
-        0 .. n-1) over one PagedKV per layer; logits f32 [n or len(out_rows)][V], after the
-        `processing` (process_logits' history, penalties, biases and mask) of their rows."""
-        dev, n = tokens.device, tokens.shape[0]
-        rows = n if out_rows is None else out_rows.shape[0]
-        if len(kvs) != self.dims.n_layers or any(kv.device != dev for kv in kvs):
-            _refuse(f"need {self.dims.n_layers} caches on {dev}")
-        vocab = self.dims.vocab
-        lp = _array(logits, "logits", EMOE_F32, (rows, vocab), dev)
-        if rows > 1 and logits.stride(0) != vocab:
-            _refuse("logits must be contiguous")
-        batch = DecoderBatch(_array(tokens, "tokens", -1, (n,), dev),
-                             _array(positions, "positions", -1, (n,), dev),
-                             _array(seqs, "seqs", -1, (n,), dev),
-                             _array(page_table, "page_table", -1, (None, None), dev),
-                             _array(out_rows, "out_rows", -1, (rows,), dev), page_table.stride(0), n,
-                             page_table.shape[0], page_table.shape[1], rows, max_keys)
-        process = _processing(dev, rows, vocab, **processing)
-        nt = _array(next_token, "next_token", -1, (rows,), dev)
+        0 .. n-1) over one PagedKV per layer; logits f32 [n or len(out_rows)][V], processed as by
+        process_logits with the last eleven arguments (of the logits' rows)."""
+        if len(kvs) != self.dims.n_layers or any(kv.device != kvs[0].device for kv in kvs):
+            _refuse(f"need {self.dims.n_layers} caches on one device")
         views = (PagedKVView * len(kvs))(*[kv.view for kv in kvs])
-        wp, wn = _workspace(workspace, dev)
-        fn, tail = lib().emoe_decoder_forward_paged, C.byref(stats) if stats is not None else None
-        _call(lambda *a: fn(*a, tail), dev, stream, self.handle, views, C.byref(batch), lp,
-              C.byref(process), nt, wp, wn)
+        device = kvs[0].index
+        binding().decoder_forward_paged(
+            self.handle.value, C.addressof(views), self.dims.vocab, device, tokens, positions,
+            page_table, logits, workspace, max_keys, seqs, out_rows, next_token,
+            0 if stats is None else C.addressof(stats), history, history_lengths, prompt_lengths,
+            repetition, presence, frequency, bias_ids, bias_values, bias_counts, mask, mask_rows,
+            _stream_on(device, stream))
 
 
 # ---------------------------------------------------------------- many sequences at once
-# The calls of exactmoe_serving.h.  A pointer says nothing about its tensor, so
-# what the library cannot see (types, shapes, strides, devices) is checked here.
-_codes = None
-
-
-def _type_of(t, name: str) -> int:
-    global _codes
-    if _codes is None:
-        import torch
-        _codes = {torch.float32: EMOE_F32, torch.bfloat16: EMOE_BF16, torch.int16: EMOE_BF16,
-                  torch.uint16: EMOE_BF16, torch.float16: EMOE_F16,
-                  torch.float8_e4m3fn: EMOE_E4M3, torch.int32: -1, torch.uint32: -1,
-                  torch.float64: -2}
-    code = _codes.get(t.dtype)
-    if code is None:
-        _refuse(f"{name}: type {t.dtype} is not supported")
-    return code
-
-
+# The calls of exactmoe_serving.h.  A pointer says nothing about its tensor: what
+# the library cannot see (types, shapes, strides, devices) is checked in
+# csrc/binding.cpp, and here for a new cache.
 def _refuse(message: str):
     raise ExactMoEError(EMOE_EINVAL, message)
 
 
-def _array(t, name: str, code: int, shape: tuple, device):
-    """Pointer of an optional tensor of this type, shape (None: any size) and device, dense along
-    its last axis."""
-    if t is None:
-        return None
-    sh = t.shape
-    if _type_of(t, name) != code:
-        _refuse(f"{name}: type {t.dtype} does not fit")
-    if t.device != device:
-        _refuse(f"{name} is on {t.device}, not on {device}")
-    if len(sh) != len(shape):
-        _refuse(f"{name}: need {len(shape)} axes, got shape {tuple(sh)}")
-    for have, want in zip(sh, shape):
-        if want is not None and have != want:
-            _refuse(f"{name}: shape {tuple(sh)}, need {shape}")
-    if sh[-1] > 1 and t.stride(-1) != 1 and t.numel():
-        _refuse(f"{name}: the last axis must be dense")
-    return t.data_ptr()
-
-
-def _head_rows(t, name: str, code: int, shape: tuple, device):
-    """Pointer and row stride of a [rows][heads][dim] tensor whose rows are dense."""
-    ptr = _array(t, name, code, shape, device)
-    st = t.stride()
-    if shape[1] > 1 and st[1] != shape[2] and shape[0]:
-        _refuse(f"{name}: the heads of a row must be dense")
-    return ptr, st[0]
-
-
-def _call(fn, device, stream, *args) -> None:
-    """fn(*args, stream) with `device` current; the default stream is that device's current one."""
-    import torch
+def _stream_on(device: int, stream) -> int:
+    """Handle of a stream, by default of that device's current one."""
     if stream is None:
-        stream = torch._C._cuda_getCurrentRawStream(device.index)  # 1.8 us less than a Stream object
-    elif not isinstance(stream, int):
-        if stream.device != device:
-            _refuse(f"stream of {stream.device} for tensors on {device}")
-        stream = stream.cuda_stream
-    if torch.cuda.current_device() == device.index:
-        check(fn(*args, stream))
-    else:
-        with torch.cuda.device(device):
-            check(fn(*args, stream))
+        import torch
+        return torch._C._cuda_getCurrentRawStream(device)  # 1.8 us less than by a Stream object
+    if isinstance(stream, int):
+        return stream
+    if stream.device.index != device:
+        _refuse(f"stream of {stream.device} for tensors on cuda:{device}")
+    return stream.cuda_stream
 
 
-def _workspace(t, device):
-    if t is None:
-        return None, 0
-    if t.device != device or not t.is_contiguous():
-        _refuse(f"workspace must be contiguous and on {device}")
-    return t.data_ptr(), t.numel() * t.element_size()
+def _cache_types() -> dict:
+    import torch
+    return {torch.bfloat16: EMOE_BF16, torch.int16: EMOE_BF16, torch.uint16: EMOE_BF16,
+            torch.float16: EMOE_F16, torch.float8_e4m3fn: EMOE_E4M3}
 
 
 class PagedKV:
@@ -379,24 +318,27 @@ class PagedKV:
     hold their heads outside their slots does too).  k_scale, v_scale: f32 [kv heads], E4M3 only."""
 
     def __init__(self, k_pages, v_pages, k_scale=None, v_scale=None):
+        import torch
         if k_pages.device.type != "cuda":
             _refuse(f"k_pages is on {k_pages.device}")
-        self.device = k_pages.device
-        if k_pages.dim() != 4:
-            _refuse(f"k_pages: need 4 axes, got shape {tuple(k_pages.shape)}")
-        self.dtype = _type_of(k_pages, "k_pages")
-        shape, st = tuple(k_pages.shape), k_pages.stride()
-        kp = _array(k_pages, "k_pages", self.dtype, shape, self.device)
-        vp = _array(v_pages, "v_pages", self.dtype, shape, self.device)
-        if v_pages.dtype != k_pages.dtype or v_pages.stride() != st:
-            _refuse("v_pages: type or strides differ from those of k_pages")
-        ks = _array(k_scale, "k_scale", EMOE_F32, (shape[2],), self.device)
-        vs = _array(v_scale, "v_scale", EMOE_F32, (shape[2],), self.device)
-        self.n_kv_heads, self.head_dim = shape[2], shape[3]
+        if k_pages.dim() != 4 or k_pages.dtype not in _cache_types() or k_pages.stride(3) != 1:
+            _refuse(f"k_pages: shape {tuple(k_pages.shape)}, type {k_pages.dtype}: need 4 axes of "
+                    "bf16, fp16 or e4m3, the last one dense")
+        for what in ("device", "dtype", "shape"):
+            if getattr(v_pages, what) != getattr(k_pages, what):
+                _refuse(f"v_pages: another {what} than k_pages")
+        if v_pages.stride() != k_pages.stride():
+            _refuse("v_pages: other strides than k_pages")
+        for name, s in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if s is not None and (s.device != k_pages.device or s.dtype != torch.float32
+                                  or tuple(s.shape) != (k_pages.shape[2],) or not s.is_contiguous()):
+                _refuse(f"{name}: need f32 [{k_pages.shape[2]}] on {k_pages.device}")
+        self.device, self.index = k_pages.device, k_pages.device.index
         self._keep = (k_pages, v_pages, k_scale, v_scale)
-        self.view = PagedKVView(kp, vp, ks, vs, st[0], st[1], st[2], self.dtype, *shape)
-        self.ref = C.byref(self.view)
-        check(lib().emoe_check_paged_kv(self.ref))
+        self.view = PagedKVView(*[_ptr(t) for t in self._keep], *k_pages.stride()[:3],
+                                _cache_types()[k_pages.dtype], *k_pages.shape)
+        self.address = C.addressof(self.view)
+        check(lib().emoe_check_paged_kv(C.byref(self.view)))
 
 
 def rope_frequencies(rotary_dim: int, base: float = 10000.0, device="cuda"):
@@ -411,30 +353,13 @@ def paged_append(kv: PagedKV, q, k, v, positions, page_table, inv_freq, seqs=Non
     """emoe_paged_append: q_out (q itself when None) = the rotated q; the rotated k and v go to the
     pages of each token's position.  q [n][heads][dim] or None, k, v [n][kv heads][dim]; positions,
     seqs i32 [n]; page_table i32 [sequences][pages]; inv_freq f64 [rotary_dim / 2] or None."""
-    dev, n, hk, d = kv.device, k.shape[0], kv.n_kv_heads, kv.head_dim
-    code = _type_of(k, "k")
-    kp, ks = _head_rows(k, "k", code, (n, hk, d), dev)
-    vp, vs = _head_rows(v, "v", code, (n, hk, d), dev)
-    qp = op = None
-    qs = os = heads = 0
-    if q is not None:
-        heads = q.shape[1] if q.dim() == 3 else 0
-        qp, qs = op, os = _head_rows(q, "q", code, (n, heads, d), dev)
-        if q_out is not None:
-            op, os = _head_rows(q_out, "q_out", code, (n, heads, d), dev)
-    pp = _array(positions, "positions", -1, (n,), dev)
-    sp = _array(seqs, "seqs", -1, (n,), dev)
-    tp = _array(page_table, "page_table", -1, (None, None), dev)
-    fp = _array(inv_freq, "inv_freq", -2, (None,), dev)
-    n_seqs, width = page_table.shape
-    args = PagedAppendArgs(qp, kp, vp, op, pp, sp, tp, fp, qs, ks, vs, os, page_table.stride(0),
-                           code, n, heads, n_seqs, width,
-                           0 if inv_freq is None else 2 * inv_freq.shape[0], int(bool(interleaved)))
-    _call(lib().emoe_paged_append, dev, stream, kv.ref, C.byref(args))
+    binding().paged_append(kv.address, kv.index, q, k, v, positions, page_table, inv_freq, seqs, q_out,
+                           interleaved, _stream_on(kv.index, stream))
 
 
 def paged_attention_workspace_bytes(kv: PagedKV, rows: int, n_heads: int, max_keys: int) -> int:
-    return int(lib().emoe_paged_attention_workspace_bytes(kv.ref, rows, n_heads, max_keys))
+    return int(lib().emoe_paged_attention_workspace_bytes(C.byref(kv.view), rows, n_heads,
+                                                          max_keys))
 
 
 def paged_attention(kv: PagedKV, q, page_table, lengths, out, workspace, max_keys: int, seqs=None,
@@ -443,59 +368,14 @@ def paged_attention(kv: PagedKV, q, page_table, lengths, out, workspace, max_key
     its sequence.  q, out [rows][heads][dim]; lengths, seqs i32 [rows]; page_table i32 [sequences]
     [pages]; lse f32 [rows][heads] or None; scale 1 / sqrt(dim) when None.  workspace: zeroed once
     (paged_attention_workspace_bytes)."""
-    dev, (rows, heads, d) = kv.device, q.shape
-    code = _type_of(q, "q")
-    if d != kv.head_dim:
-        _refuse(f"q: head size {d}, the cache's is {kv.head_dim}")
-    qp, qs = _head_rows(q, "q", code, (rows, heads, d), dev)
-    op, os = _head_rows(out, "out", code, (rows, heads, d), dev)
-    if lse is not None and not lse.is_contiguous():
-        _refuse("lse must be contiguous")
-    lp = _array(lse, "lse", EMOE_F32, (rows, heads), dev)
-    np_ = _array(lengths, "lengths", -1, (rows,), dev)
-    sp = _array(seqs, "seqs", -1, (rows,), dev)
-    tp = _array(page_table, "page_table", -1, (None, None), dev)
-    wp, wn = _workspace(workspace, dev)
-    n_seqs, width = page_table.shape
-    args = PagedAttentionArgs(qp, op, lp, np_, sp, tp, qs, os, page_table.stride(0),
-                              1.0 / math.sqrt(d) if scale is None else scale, code, rows, heads,
-                              n_seqs, width, max_keys, window)
-    _call(lib().emoe_paged_attention, dev, stream, kv.ref, C.byref(args), wp, wn)
+    if scale is None:
+        scale = kv.view.head_dim ** -0.5
+    binding().paged_attention(kv.address, kv.index, q, page_table, lengths, out, workspace, max_keys,
+                              seqs, scale, window, lse, _stream_on(kv.index, stream))
 
 
 def process_logits_workspace_bytes(rows: int, vocab: int) -> int:
     return int(lib().emoe_process_logits_workspace_bytes(rows, vocab))
-
-
-def _processing(dev, rows: int, vocab: int, history=None, history_lengths=None,
-                prompt_lengths=None, repetition=None, presence=None, frequency=None, bias_ids=None,
-                bias_values=None, bias_counts=None, mask=None, mask_rows=None) -> LogitsArgs:
-    """The penalties, biases and masks of `rows` rows of logits, checked."""
-    args, row = LogitsArgs(), (rows,)
-    if history is not None:
-        args.history = _array(history, "history", -1, (rows, None), dev)
-        args.history_stride, args.history_width = history.stride(0), history.shape[1]
-    args.history_lengths = _array(history_lengths, "history_lengths", -1, row, dev)
-    args.prompt_lengths = _array(prompt_lengths, "prompt_lengths", -1, row, dev)
-    args.repetition = _array(repetition, "repetition", EMOE_F32, row, dev)
-    args.presence = _array(presence, "presence", EMOE_F32, row, dev)
-    args.frequency = _array(frequency, "frequency", EMOE_F32, row, dev)
-    if bias_ids is not None or bias_values is not None:
-        if bias_ids is None or bias_values is None:
-            _refuse("one of bias_ids and bias_values is missing")
-        args.bias_ids = _array(bias_ids, "bias_ids", -1, (rows, None), dev)
-        args.bias_values = _array(bias_values, "bias_values", EMOE_F32, tuple(bias_ids.shape), dev)
-        if rows > 1 and bias_ids.stride(0) != bias_values.stride(0):
-            _refuse("bias_ids and bias_values have different row strides")
-        args.bias_counts = _array(bias_counts, "bias_counts", -1, row, dev)
-        args.bias_stride, args.bias_width = bias_ids.stride(0), bias_ids.shape[1]
-    if mask is not None:
-        args.mask = _array(mask, "mask", -1, (None, None), dev)
-        if mask.shape[1] * 32 < vocab:
-            _refuse(f"mask: {mask.shape[1]} words for a vocabulary of {vocab}")
-        args.mask_stride, args.n_masks = mask.stride(0), mask.shape[0]
-    args.mask_rows = _array(mask_rows, "mask_rows", -1, row, dev)
-    return args
 
 
 def process_logits(logits, out=None, workspace=None, history=None, history_lengths=None,
@@ -507,22 +387,12 @@ def process_logits(logits, out=None, workspace=None, history=None, history_lengt
     [width], lengths i32 [rows]; repetition, presence, frequency f32 [rows]; bias_ids i32 and
     bias_values f32 [rows][width]; mask i32 words [masks][>= vocab / 32], mask_rows i32 [rows].
     workspace: zeroed once (process_logits_workspace_bytes), needed with next_token."""
-    dev, (rows, vocab) = logits.device, logits.shape
-    if dev.type != "cuda":
-        _refuse(f"logits is on {dev}")
-    code = _type_of(logits, "logits")
-    lp = _array(logits, "logits", code, (rows, vocab), dev)
-    op, os = lp, logits.stride(0)
-    if out is not None:
-        op, os = _array(out, "out", code, (rows, vocab), dev), out.stride(0)
-    args = _processing(dev, rows, vocab, history, history_lengths, prompt_lengths, repetition,
-                       presence, frequency, bias_ids, bias_values, bias_counts, mask, mask_rows)
-    args.logits, args.out = lp, op
-    args.next_token = _array(next_token, "next_token", -1, (rows,), dev)
-    args.logits_stride, args.out_stride = logits.stride(0), os
-    args.dtype, args.rows, args.vocab = code, rows, vocab
-    wp, wn = _workspace(workspace, dev)
-    _call(lib().emoe_process_logits, dev, stream, C.byref(args), wp, wn)
+    if not logits.is_cuda:
+        _refuse(f"logits is on {logits.device}")
+    binding().process_logits(logits, out, workspace, next_token, history, history_lengths,
+                             prompt_lengths, repetition, presence, frequency, bias_ids, bias_values,
+                             bias_counts, mask, mask_rows,
+                             _stream_on(logits.device.index, stream))
 
 
 def decoder_paged_workspace_bytes(dd: DecoderDims, n_tokens: int, n_out: int, max_keys: int) -> int:
