@@ -139,9 +139,8 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t c) {
 }
 
 // A workgroup takes one chunk of one row: its logits are on their way while
-// the row's history (and biases) is counted into words of LDS, one per token
-// id of the chunk (bit 31: in the prompt; low bits: times generated), with a
-// bit per touched id.  Counting again for every chunk costs L2 reads of the
+// the row's history (and biases) is counted into LDS, a counter per token id
+// of the chunk.  Counting again for every chunk costs L2 reads of the
 // history, but needs no table in memory as long as the vocabulary, which would
 // have to be cleared and read as well.  Then one pass: the few touched elements
 // are taken out of their registers one by one, the mask replaces words, and
@@ -157,15 +156,16 @@ __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
   constexpr int kChunk = kThreads * kPer * kLoads;
   constexpr uint32_t kAll = (1u << kPer) - 1;
   typedef typename F::Raw Raw;
-  // Counters of 16 bits (bit 15: in the prompt) where the history is short, so
-  // that twice the workgroups fit a CU, else of 32.
+  // A counter per id: 16 bits where the history is short, so that twice the
+  // workgroups fit a CU, else 32.  Low part: times generated; above it, that the
+  // prompt has the id: a bit, or how often where both numbers fit their half of
+  // 32 bits, so that one addition does.  64 words more take the additions of
+  // the ids that lie in other chunks, which costs less than to skip them.
   constexpr bool kShort = kThreads == 256;
-  constexpr uint32_t kPrompt = kShort ? 0x8000u : 0x80000000u;
   static_assert(kLongHistory <= 0x8000, "15 bits hold a short history's counts");
   constexpr int kSeenWords = kShort ? kChunk / 2 : kChunk;
-  __shared__ __attribute__((aligned(16))) uint32_t seen[kSeenWords];
+  __shared__ __attribute__((aligned(16))) uint32_t seen[kSeenWords + 64];
   __shared__ __attribute__((aligned(16))) int32_t bias[kBias ? kChunk : 4];
-  __shared__ uint32_t touched[kChunk / 32];
   __shared__ uint64_t red[kThreads / 64];
   const int tid = threadIdx.x;
   const int lr = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
@@ -211,6 +211,8 @@ __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
   n_hist = max(0, min(n_hist, a.history_width));
   n_bias = max(0, min(n_bias, a.bias_width));
   const bool count = a.history && !(rep == 1.f && pres == 0.f && freq == 0.f);
+  const bool both = !kShort && a.history_width < 0x10000;
+  const uint32_t made_bits = kShort ? 0x7fffu : both ? 0xffffu : 0x7fffffffu;
   if (count || kBias) {
     if (count)
       for (int i = tid; i < kSeenWords / 4; i += kThreads)
@@ -218,29 +220,22 @@ __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
     if constexpr (kBias)
       for (int i = tid; i < kChunk / 4; i += kThreads)
         reinterpret_cast<uint4*>(bias)[i] = make_uint4(0, 0, 0, 0);
-    for (int i = tid; i < kChunk / 32; i += kThreads) touched[i] = 0;
     __syncthreads();
     if (count) {
-      // LDS takes atomics on one word one after the other, and a text has words
-      // of which every tenth token is one: what is set already is not set again.
-      auto add4 = [&](int i, const int4& id4) __attribute__((always_inline)) {
-        const int id[4] = {id4.x, id4.y, id4.z, id4.w};
-        uint32_t at[4], was[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          at[k] = (uint32_t)id[k] - (uint32_t)c0;
-          if (at[k] >= (uint32_t)kChunk || id[k] >= V || i + k >= n_hist) at[k] = ~0u;
-          was[k] = at[k] == ~0u ? 0 : seen[kShort ? at[k] >> 1 : at[k]];
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (at[k] == ~0u) continue;
-          const int sh = kShort ? 16 * (at[k] & 1) : 0;
-          uint32_t* word = &seen[kShort ? at[k] >> 1 : at[k]];
-          const uint32_t now = kShort ? was[k] >> sh & 0xffffu : was[k];
-          if (i + k >= prompt) atomicAdd(word, 1u << sh);
-          else if (!(now & kPrompt)) atomicOr(word, kPrompt << sh);
-          if (now == 0) atomicOr(&touched[at[k] >> 5], 1u << (at[k] & 31));
+      const uint32_t here = (uint32_t)min(kChunk, V - c0);
+      auto add = [&](int i, int id) __attribute__((always_inline)) {
+        const uint32_t at = (uint32_t)id - (uint32_t)c0;
+        const bool hit = at < here && i < n_hist, old = i < prompt;
+        if constexpr (kShort) {
+          uint32_t* word = &seen[hit ? at >> 1 : kSeenWords + (tid & 63)];
+          const int sh = 16 * (at & 1);
+          atomicAdd(word, old ? 0u : 1u << sh);
+          if (old) atomicOr(word, 0x8000u << sh);
+        } else {
+          uint32_t* word = &seen[hit ? at : kSeenWords + (tid & 63)];
+          if (both) atomicAdd(word, old ? 0x10000u : 1u);
+          else if (old) atomicOr(word, 0x80000000u);
+          else atomicAdd(word, 1u);
         }
       };
       for (int i0 = 0; i0 < n_hist; i0 += 4 * kThreads * kAhead) {
@@ -250,7 +245,13 @@ __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
             ids[k] = load_ids(hist, i0 + 4 * (k * kThreads + tid), a.history_width);
         }
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) add4(i0 + 4 * (k * kThreads + tid), ids[k]);
+        for (int k = 0; k < kAhead; ++k) {
+          const int i = i0 + 4 * (k * kThreads + tid);
+          add(i, ids[k].x);
+          add(i + 1, ids[k].y);
+          add(i + 2, ids[k].z);
+          add(i + 3, ids[k].w);
+        }
       }
     }
     if constexpr (kBias) {
@@ -267,7 +268,6 @@ __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
         const uint32_t at = place(i < kThreads ? bias_id : more_ids[i]);
         if (at == ~0u) continue;
         atomicMax(&bias[at], i + 1);
-        atomicOr(&touched[at >> 5], 1u << (at & 31));
       }
       __syncthreads();
       for (int i = tid; i < n_bias; i += kThreads) {
@@ -289,7 +289,26 @@ __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
     if (allowed != kAll)
       w = make_uint4(masked<F>(w.x, allowed, 0), masked<F>(w.y, allowed, 1),
                      masked<F>(w.z, allowed, 2), masked<F>(w.w, allowed, 3));
-    uint32_t todo = count || kBias ? touched[at >> 5] >> (at & 31) & allowed : 0;
+    uint32_t todo = 0;  // the touched elements
+    if (count) {
+      constexpr int kWords = kShort ? kPer / 2 : kPer;
+      uint32_t c[kWords], any = 0;
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) {
+        c[i] = seen[(kShort ? at >> 1 : at) + i];
+        any |= c[i];
+      }
+      if (any) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          todo |= ((kShort ? c[i >> 1] >> (16 * (i & 1)) & 0xffffu : c[i]) != 0 ? 1u : 0u) << i;
+      }
+    }
+    if constexpr (kBias) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) todo |= (bias[at + i] != 0 ? 1u : 0u) << i;
+    }
+    todo &= allowed;
     if (a.next_token) {
       // The elements that stay as they are first: among equals the lower id.
       float x[kPer];
@@ -319,8 +338,8 @@ __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
       }
       if (c) {
         x = x > 0.f ? x / rep : x * rep;
-        if (c & (kPrompt - 1)) {
-          const float f = freq * (float)(c & (kPrompt - 1));
+        if (c & made_bits) {
+          const float f = freq * (float)(c & made_bits);
           x = x - f;
           x = x - pres;
         }
@@ -433,6 +452,8 @@ int32_t emoe::check_process_logits(const emoe_logits_args& A, const void* worksp
   const bool many = A.rows > 1;
   if (many && (A.logits_stride < A.vocab || A.out_stride < A.vocab))
     return report_error(EMOE_EINVAL, "logits or out: row stride below vocab %d", A.vocab);
+  if (A.history_width > (1 << 30))
+    return report_error(EMOE_ESHAPE, "history_width %d above 2^30", A.history_width);
   if (A.history && many && A.history_stride < A.history_width)
     return report_error(EMOE_EINVAL, "history_stride below history_width %d", A.history_width);
   if (!A.history && (A.repetition || A.presence || A.frequency))
