@@ -412,7 +412,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
   __shared__ __attribute__((aligned(16))) float os[kAttnWaves][16][kRow];
   __shared__ float4 striped[kThreads];
   __shared__ float striped_m[kThreads], striped_l[kThreads];
-  __shared__ int last, first_row;
+  __shared__ int last[2], shared_row[2], first_row;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
   const uint32_t k_off = Tl::k_offset(lane, a.kv.slot_bytes);
@@ -467,6 +467,23 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
   const int u_end = min((w + 1) * run, total);
   int u = w * run, row = first_row;
   bool first_segment = true;
+  int waiting = 0;  // outputs of this run that other workers share
+  const int hk = y / a.q_tiles, qt = y % a.q_tiles;
+  const int head0 = hk * a.group + qt * 16;
+  const int heads = min(16, a.group - qt * 16);
+  float scale = a.scale * 1.4426950408889634f;
+  if (kE4M3 && a.kv.k_scale) scale *= a.kv.k_scale[hk];
+  const float vs = kE4M3 && a.kv.v_scale ? a.kv.v_scale[hk] : 1.f;
+  auto store_out = [&](int64_t grow, int h, int d, float4 o, float M, float L) {
+    const float inv = L == 0.f ? 0.f : vs / L;
+    uint2 r;
+    r.x = T::down(o.x * inv) | (T::down(o.y * inv) << 16);
+    r.y = T::down(o.z * inv) | (T::down(o.w * inv) << 16);
+    *reinterpret_cast<uint2*>(a.out + grow * a.out_stride + (int64_t)(head0 + h) * kDh + d) = r;
+    if (d == 0 && a.lse)
+      a.lse[grow * a.n_heads + head0 + h] =
+          L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+  };
   for (; u < u_end; ++row) {
     row = __builtin_amdgcn_readfirstlane(row);
     const int base = __builtin_amdgcn_readfirstlane(pre[row]);
@@ -476,9 +493,6 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
     const int c0 = u - base;
     const int c1 = min(units, c0 + (u_end - u));
     const int first = a.window > 0 ? max(0, n - a.window) : 0;
-    const int hk = y / a.q_tiles, qt = y % a.q_tiles;
-    const int head0 = hk * a.group + qt * 16;
-    const int heads = min(16, a.group - qt * 16);
     const int64_t grow = a.row0 + row;
 
     uint4 q[Tl::kSteps];
@@ -489,9 +503,6 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
         q[c] = *reinterpret_cast<const uint4*>(a.q + grow * a.q_stride +
                                                (int64_t)(head0 + l16) * kDh + Tl::q_dim(c, g));
     }
-    float scale = a.scale * 1.4426950408889634f;
-    if (kE4M3 && a.kv.k_scale) scale *= a.kv.k_scale[hk];
-
     f32x4 acc[Tl::kDims];
 #pragma unroll
     for (int c = 0; c < Tl::kDims; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -629,17 +640,6 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
       for (int i = 0; i < kAttnWaves; ++i)
         L += ls[i][h] * part_weight(ms[i][h], M);
     };
-    const float vs = kE4M3 && a.kv.v_scale ? a.kv.v_scale[hk] : 1.f;
-    auto store_out = [&](int h, int d, float4 o, float M, float L) {
-      const float inv = L == 0.f ? 0.f : vs / L;
-      uint2 r;
-      r.x = T::down(o.x * inv) | (T::down(o.y * inv) << 16);
-      r.y = T::down(o.z * inv) | (T::down(o.w * inv) << 16);
-      *reinterpret_cast<uint2*>(a.out + grow * a.out_stride + (int64_t)(head0 + h) * kDh + d) = r;
-      if (d == 0 && a.lse)
-        a.lse[grow * a.n_heads + head0 + h] =
-            L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
-    };
     float* part = a.parts + (int64_t)(2 * blockIdx.x + (first_segment ? 0 : 1)) * a.part_floats;
     for (int x = tid; x < heads * (kDh / 4); x += kThreads) {
       const int h = x / (kDh / 4), d = 4 * (x % (kDh / 4));
@@ -652,7 +652,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
       float M, L;
       if (full || d == 0) join(h, M, L);
       if (full) {
-        store_out(h, d, o, M, L);
+        store_out(grow, h, d, o, M, L);
       } else {
         uint64_t* p = reinterpret_cast<uint64_t*>(part + 32 + h * kDh + d);
         const uint64_t a0 = (uint64_t)__float_as_uint(o.x) | ((uint64_t)__float_as_uint(o.y) << 32);
@@ -666,93 +666,108 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
       }
     }
     if (!full) {
-      // The workers that share this output; the first one's ticket is theirs.
-      const int wa = base / run, wb = (base + units - 1) / run;
-      uint32_t* ticket = &a.tickets[(wa * Y + y) * kTicketStride];
-      wait_memory();
-      __syncthreads();
-      if (tid == 0) {
-        last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED,
-                                      __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(wb - wa);
-        wait_memory();
-      }
-      __syncthreads();
-      if (last) {
-        const int parts = wb - wa + 1;
-        const int lead = base % run ? 1 : 0;  // the first one's last segment, or its first
-        auto part_at = [&](int i) {
-          return a.parts + (int64_t)(2 * ((wa + i) * Y + y) + (i == 0 ? lead : 0)) * a.part_floats;
-        };
-        // Eight parts at a time, everything of theirs in flight at once; the
-        // parts are dealt over the threads that one part's outputs leave idle.
-        const int items = heads * (kDh / 4);
-        const int stripes = items < kThreads ? kThreads / items : 1;
-        for (int x = tid; x < items * stripes; x += kThreads) {
-          const int item = x % items, h = item / (kDh / 4), d = 4 * (item % (kDh / 4));
-          float M = -INFINITY, L = 0.f;
-          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-          constexpr int kAhead = 8;
-          for (int i0 = x / items; i0 < parts; i0 += kAhead * stripes) {
-            float m_of[kAhead], l_of[kAhead];
-            uint64_t lo[kAhead], hi[kAhead];
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-              const float* p = part_at(min(i0 + k * stripes, parts - 1));
-              const uint64_t* v = reinterpret_cast<const uint64_t*>(p + 32 + h * kDh + d);
-              m_of[k] = __uint_as_float(ld_u32<true>(p + h));
-              l_of[k] = __uint_as_float(ld_u32<true>(p + 16 + h));
-              lo[k] = __hip_atomic_load(v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-              hi[k] = __hip_atomic_load(v + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
-            float top = M;
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-              if (i0 + k * stripes >= parts) m_of[k] = -INFINITY;  // the last part again
-              top = fmaxf(top, m_of[k]);
-            }
-            const float shrink = part_weight(M, top);
-            M = top;
-            L *= shrink;
-            o.x *= shrink, o.y *= shrink, o.z *= shrink, o.w *= shrink;
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-              const float f = part_weight(m_of[k], M);
-              L = fmaf(f, l_of[k], L);
-              o.x = fmaf(f, __uint_as_float((uint32_t)lo[k]), o.x);
-              o.y = fmaf(f, __uint_as_float((uint32_t)(lo[k] >> 32)), o.y);
-              o.z = fmaf(f, __uint_as_float((uint32_t)hi[k]), o.z);
-              o.w = fmaf(f, __uint_as_float((uint32_t)(hi[k] >> 32)), o.w);
-            }
-          }
-          if (stripes == 1) {
-            store_out(h, d, o, M, L);
-          } else {
-            striped[x] = o;
-            striped_m[x] = M;
-            striped_l[x] = L;
-          }
-        }
-        if (stripes > 1) {
-          __syncthreads();
-          if (tid < items) {
-            float M = striped_m[tid], L = 0.f;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int i = 1; i < stripes; ++i) M = fmaxf(M, striped_m[tid + i * items]);
-            for (int x = tid; x < items * stripes; x += items) {
-              const float f = part_weight(striped_m[x], M);
-              const float4 e = striped[x];
-              L = fmaf(f, striped_l[x], L);
-              o.x = fmaf(f, e.x, o.x), o.y = fmaf(f, e.y, o.y);
-              o.z = fmaf(f, e.z, o.z), o.w = fmaf(f, e.w, o.w);
-            }
-            store_out(tid / (kDh / 4), 4 * (tid % (kDh / 4)), o, M, L);
-          }
-        }
-        if (tid == 0) st_u32<true>(ticket, 0);
-      }
+      if (tid == 0) shared_row[waiting] = row;
+      ++waiting;
     }
     u += c1 - c0;
     first_segment = false;
+  }
+  if (waiting == 0) return;
+
+  // The shared outputs, at most two: this worker's parts are in memory before
+  // it takes their tickets, and whose ticket is the last joins the parts.
+  wait_memory();
+  __syncthreads();
+  if (tid < waiting) {
+    const int base = pre[shared_row[tid]], units = pre[shared_row[tid] + 1] - base;
+    const int wa = base / run, wb = (base + units - 1) / run;  // the first and the last worker
+    last[tid] = __hip_atomic_fetch_add(&a.tickets[(wa * Y + y) * kTicketStride], 1u, __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(wb - wa);
+    wait_memory();
+  }
+  __syncthreads();
+  for (int turn = 0; turn < waiting; ++turn) {
+    if (!last[turn]) continue;
+    const int shared = __builtin_amdgcn_readfirstlane(shared_row[turn]);
+    const int base = __builtin_amdgcn_readfirstlane(pre[shared]);
+    const int units = __builtin_amdgcn_readfirstlane(pre[shared + 1]) - base;
+    const int wa = base / run, parts = (base + units - 1) / run - wa + 1;
+    const int lead = base % run ? 1 : 0;  // the first one's last segment, or its first
+    auto part_at = [&](int i) {
+      return a.parts + (int64_t)(2 * ((wa + i) * Y + y) + (i == 0 ? lead : 0)) * a.part_floats;
+    };
+    const int64_t grow = a.row0 + shared;
+    // Eight parts at a time, everything of theirs in flight at once; the parts
+    // are dealt over the threads that one part's outputs leave idle.
+    const int items = heads * (kDh / 4);
+    const int stripes = items < kThreads ? kThreads / items : 1;
+    for (int x = tid; x < items * stripes; x += kThreads) {
+      const int item = x % items, h = item / (kDh / 4), d = 4 * (item % (kDh / 4));
+      float M = -INFINITY, L = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      constexpr int kAhead = 8;
+      for (int i0 = x / items; i0 < parts; i0 += kAhead * stripes) {
+        float m_of[kAhead], l_of[kAhead];
+        uint64_t lo[kAhead], hi[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const float* p = part_at(min(i0 + k * stripes, parts - 1));
+          const uint64_t* v = reinterpret_cast<const uint64_t*>(p + 32 + h * kDh + d);
+          m_of[k] = __uint_as_float(ld_u32<true>(p + h));
+          l_of[k] = __uint_as_float(ld_u32<true>(p + 16 + h));
+          lo[k] = __hip_atomic_load(v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          hi[k] = __hip_atomic_load(v + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        float top = M;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          if (i0 + k * stripes >= parts) {  // past the end: nothing (an infinity times 0 is not)
+            m_of[k] = -INFINITY;
+            l_of[k] = 0.f;
+            lo[k] = hi[k] = 0;
+          }
+          top = fmaxf(top, m_of[k]);
+        }
+        const float shrink = part_weight(M, top);
+        M = top;
+        L *= shrink;
+        o.x *= shrink, o.y *= shrink, o.z *= shrink, o.w *= shrink;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const float f = part_weight(m_of[k], M);
+          L = fmaf(f, l_of[k], L);
+          o.x = fmaf(f, __uint_as_float((uint32_t)lo[k]), o.x);
+          o.y = fmaf(f, __uint_as_float((uint32_t)(lo[k] >> 32)), o.y);
+          o.z = fmaf(f, __uint_as_float((uint32_t)hi[k]), o.z);
+          o.w = fmaf(f, __uint_as_float((uint32_t)(hi[k] >> 32)), o.w);
+        }
+      }
+      if (stripes == 1) {
+        store_out(grow, h, d, o, M, L);
+      } else {
+        striped[x] = o;
+        striped_m[x] = M;
+        striped_l[x] = L;
+      }
+    }
+    if (stripes > 1) {
+      __syncthreads();
+      if (tid < items) {
+        float M = striped_m[tid], L = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 1; i < stripes; ++i) M = fmaxf(M, striped_m[tid + i * items]);
+        for (int x = tid; x < items * stripes; x += items) {
+          const float f = part_weight(striped_m[x], M);
+          const float4 e = striped[x];
+          L = fmaf(f, striped_l[x], L);
+          o.x = fmaf(f, e.x, o.x), o.y = fmaf(f, e.y, o.y);
+          o.z = fmaf(f, e.z, o.z), o.w = fmaf(f, e.w, o.w);
+        }
+        store_out(grow, tid / (kDh / 4), 4 * (tid % (kDh / 4)), o, M, L);
+      }
+      __syncthreads();  // the next output's
+    }
+    if (tid == 0) st_u32<true>(&a.tickets[(wa * Y + y) * kTicketStride], 0);
   }
 }
 

@@ -415,6 +415,30 @@ def test_attention_without_a_finite_score():
         assert torch.isnan(out).all()
 
 
+@pytest.mark.parametrize("n,at", [(6, 2), (128, 127), (700, 300), (3000, 5), (3000, 2999)])
+def test_attention_of_infinite_values(n, at):
+    """An infinite value that the row sees leaves nothing finite in its own dimension, and
+    everything as it is in the others, however the row is split."""
+    c = Cache("bf16", 400, 8, 1, 64, 0)
+    c.fill([(p, s) for p in range(400) for s in range(8)])
+    q = torch.randn(1, 2, 64, device="cuda:0").to(torch.bfloat16)
+    out, ok = torch.empty_like(q), torch.empty_like(q)
+    ws = torch.zeros(api.paged_attention_workspace_bytes(c.kv, 1, 2, n), dtype=torch.uint8, device="cuda:0")
+    args = (q, ids(np.arange(400)[None]), ids([n]))
+    api.paged_attention(c.kv, *args, ok, ws, n)
+    c.v[at // 8, at % 8, 0, 3], c.v[at // 8, at % 8, 0, 40] = math.inf, -math.inf
+    api.paged_attention(c.kv, *args, out, ws, n)
+    got = f64(out)[0]
+    assert not np.isfinite(got[:, [3, 40]]).any()
+    assert np.array_equal(np.delete(got, [3, 40], 1), np.delete(f64(ok)[0], [3, 40], 1))
+
+
+@pytest.mark.parametrize("rows,longest", [(1025, 40), (1100, 300), (2050, 1)])
+def test_attention_more_rows_than_one_launch(rows, longest):
+    rng = np.random.default_rng(rows)
+    run_attention("bf16", "bf16", rng.integers(0, longest + 1, rows).tolist(), 2, 1, 64, 16, seed=rows)
+
+
 @pytest.mark.parametrize("n", [5, 128, 3000])
 def test_attention_of_nan(n):
     """A query of NaN has NaN outputs, however its row is split; its neighbours do not notice."""
