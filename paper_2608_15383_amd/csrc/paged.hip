@@ -3,6 +3,7 @@
 #include <cmath>
 
 #include "device_rope.h"
+#include "device_route.h"
 #include "serving.h"
 
 using namespace emoe;
@@ -256,6 +257,8 @@ struct Tile {
   static constexpr int kPairs = kDh / (8 * kChunkDims);    // loads of an octet
   static constexpr int kDims = kDh / 16;                   // output dimensions of a lane
   static constexpr int kVWords = kDims * kItem / 4;
+  // Units of all lines that memory (6 TB/s) takes in the time of one worker's unit.
+  static constexpr int kBusyUnits = 160 * 512 / (2 * kDh * kItem);
   static constexpr bool kSplitV = !kE4M3 && kDh == 256;    // two 16-byte loads, 256 bytes apart
 
   uint32_t k[4][kPairs][kChunkWords];
@@ -393,81 +396,179 @@ __device__ __forceinline__ Octets octets_of(const AttendArg& a, ConstI32 table, 
   return o;
 }
 
-// Split over the caches' lengths: all rows' units of 128 keys, times key heads
-// (and tiles of 16 query heads), stand in one line; each of up to `workers`
-// workgroups takes an equal run of it, whatever the rows' lengths are, and its
-// four wavefronts every fourth tile.  The outputs that a run covers whole it
-// writes; of the others (at most its first and its last) it leaves maximum,
-// sum and unscaled output in the workspace, and the last of such an output's
-// workgroups to finish joins them in the order of the line.  Bound by HBM: per
-// tile and wavefront 16 KB (16-bit, 128 dimensions) against about 130 vector
-// and 24 matrix instructions.
+// Inclusive sum over the wavefront by DPP moves (8 cycles each; a shuffle
+// through LDS takes a hundred).
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast:15
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast:31
+  return v;
+}
+
+// How the rows of a launch are cut for the workers (workgroups) of a line: rows
+// stand behind each other, each in a number of slots, and a worker takes `run`
+// slots.  Either slots are units and every worker takes the same number of them,
+// wherever rows begin and end: best where a worker has many.  Or a row has at
+// most ceil(units / target) slots and every worker one, so that its run never
+// spans two rows, which costs a run about four units more.
+// To join a shared row costs 3 to 8 us, a unit of a worker's own 1.4 us, and no
+// cut makes the launch faster than memory: rows stay whole unless the longest
+// gives up kPays units or more over what a part, or memory, still takes.  Whole
+// against cut, 128 dimensions, 8 key heads of 16 bits: 4 rows of 1,024 keys
+// 19.0 and 12.2 us, 16 of 512 13.4 and 15.3, 16 of 2,048 33.8 and 31.1, 32 of
+// 1,024 26.5 and 31.1, 32 of 2,048 47.1 and 53.8.
+constexpr int kPays = 4, kSlackUnits = 6;
+__device__ __forceinline__ int slot_units(int units, int target) {
+  if (target == 0) return 1;
+  const uint32_t parts = (uint32_t)(units + target - 1) / (uint32_t)target;
+  return (int)((uint32_t)(units + parts - 1) / parts);
+}
+__device__ __forceinline__ int slots_of(int units, int target) {
+  if (target == 0 || units == 0) return units;
+  const int each = slot_units(units, target);
+  return (int)((uint32_t)(units + each - 1) / (uint32_t)each);
+}
+
+// Split over the caches' lengths (Cut); a worker's four wavefronts take every
+// fourth tile of its units.  Outputs that it covers whole it writes; of the
+// others (at most its first and its last) it leaves maximum, sum and unscaled
+// output in the workspace, and the last of such an output's workers to finish
+// joins them in the rows' order.  Key heads (times tiles of 16 query heads) are
+// the lines: workgroups next to each other take the same keys of different
+// heads, which lie next to each other in memory.  Bound by HBM: per tile and
+// wavefront 16 KB (16-bit, 128 dimensions) against about 250 vector and 24
+// matrix instructions.
 template <class T, bool kE4M3, int kDh>
 __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) {
   typedef Tile<T, kE4M3, kDh> Tl;
   constexpr int kRow = kDh + 4;  // padded: lanes 16 apart in dimensions, 1 in queries
   __shared__ int pre[kMaxRows + 1], len[kMaxRows], seq[kMaxRows];
-  __shared__ int wave_sum[kThreads / 64];
+  __shared__ int wave_sum[kAttnWaves], wave_most[kAttnWaves];
   __shared__ float ms[kAttnWaves][16], ls[kAttnWaves][16];
   __shared__ __attribute__((aligned(16))) float os[kAttnWaves][16][kRow];
   __shared__ float4 striped[kThreads];
   __shared__ float striped_m[kThreads], striped_l[kThreads];
-  __shared__ int last[2], shared_row[2], first_row;
+  __shared__ int last[2], first_row;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
   const uint32_t k_off = Tl::k_offset(lane, a.kv.slot_bytes);
   const uint32_t v_off = Tl::v_offset(lane, a.kv.slot_bytes);
 
-  // Units before each row, and where this worker's run of them begins.
+  // How the rows are cut, and where this worker's run of slots begins.  Up to
+  // 64 rows every wavefront finds out by itself, a row per lane, and keeps them
+  // in its lanes; more rows take the workgroup and LDS.
   const int Y = a.kv.n_kv_heads * a.q_tiles;
   const int w = blockIdx.x / Y, y = blockIdx.x % Y;
-  int total = 0;
-  {
-    const int per = (a.rows + kThreads - 1) / kThreads, r0 = tid * per;
-    int cnt[kMaxRows / kThreads], sum = 0;
+  const bool few = a.rows <= 64;
+  const int per = few ? 1 : (a.rows + kThreads - 1) / kThreads, r0 = few ? lane : tid * per;
+  constexpr int kPer = kMaxRows / kThreads;
+  int units_[kPer], n_lane = 0, seq_lane = 0, total = 0, most = 0;
 #pragma unroll
-    for (int i = 0; i < kMaxRows / kThreads; ++i) {
-      cnt[i] = 0;
-      if (i < per && r0 + i < a.rows) {
-        const Span s = span_of(a, a.row0 + r0 + i);
+  for (int i = 0; i < kPer; ++i) {
+    units_[i] = 0;
+    if (i < per && r0 + i < a.rows) {
+      const Span s = span_of(a, a.row0 + r0 + i);
+      if (few) {
+        n_lane = s.n;
+        seq_lane = s.seq;
+      } else {
         len[r0 + i] = s.n;
         seq[r0 + i] = s.seq;
-        cnt[i] = units_of(s.first, s.n);
       }
-      sum += cnt[i];
+      units_[i] = units_of(s.first, s.n);
     }
-    int incl = sum;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int t = __shfl_up(incl, d);
-      if (lane >= d) incl += t;
-    }
-    if (lane == 63) wave_sum[wave] = incl;
-    __syncthreads();
-    int at = incl - sum;
-    for (int i = 0; i < kAttnWaves; ++i) {
-      at += i < wave ? wave_sum[i] : 0;
-      total += wave_sum[i];
-    }
-    const int start = w * ((total + a.workers - 1) / a.workers);
-#pragma unroll
-    for (int i = 0; i < kMaxRows / kThreads; ++i) {
-      if (i < per && r0 + i < a.rows) {
-        pre[r0 + i] = at;
-        if (start >= at && start < at + cnt[i]) first_row = r0 + i;
-      }
-      at += cnt[i];
-    }
-    if (tid == kThreads - 1) pre[a.rows] = total;
-    __syncthreads();
+    total += units_[i];
+    most = max(most, units_[i]);
   }
-  total = __builtin_amdgcn_readfirstlane(total);
-  const int run = (total + a.workers - 1) / a.workers;  // units per worker
-  if ((int64_t)w * run >= total) return;
-  const int u_end = min((w + 1) * run, total);
-  int u = w * run, row = first_row;
+  // Sums over the rows; `before` is what the rows before this thread's have.
+  auto sum_rows = [&](int v, int& before) -> int {
+    const int incl = wave_scan(v);
+    before = incl - v;
+    const int all = __builtin_amdgcn_readlane(incl, 63);
+    if (few) return all;
+    __syncthreads();
+    if (lane == 0) wave_sum[wave] = all;
+    __syncthreads();
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < kAttnWaves; ++i) {
+      before += i < wave ? wave_sum[i] : 0;
+      sum += wave_sum[i];
+    }
+    return __builtin_amdgcn_readfirstlane(sum);
+  };
+  int before;
+  total = sum_rows(total, before);
+  most = (int)wave_reduce_u32<true>((uint32_t)most);
+  if (!few) {
+    if (lane == 0) wave_most[wave] = most;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kAttnWaves; ++i) most = max(most, wave_most[i]);
+  }
+  most = __builtin_amdgcn_readfirstlane(most);
+  int run = (total + a.workers - 1) / a.workers, target = 0, all = total;
+  if (a.rows < a.workers) {
+    // The smallest target tried for which the workers suffice; they do for the
+    // last one, since the sum of ceil(units / target) <= total / target + rows.
+    const int spare = a.workers - a.rows, enough = (total + spare - 1) / spare;
+    const int busy = (int)min((int64_t)INT32_MAX, (int64_t)total * Y / Tl::kBusyUnits + 1);
+    int t = most - max(run, busy) < kPays ? most : run;
+    while (true) {
+      int mine = 0;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) mine += i < per ? slots_of(units_[i], t) : 0;
+      const int sum = sum_rows(mine, before);
+      if (t < most && t > run + kSlackUnits) break;  // equal runs, then
+      if (sum <= a.workers || t >= enough) {
+        target = t;
+        all = sum;
+        run = (sum + a.workers - 1) / a.workers;
+        break;
+      }
+      t = min(t + max(1, t / 4), max(enough, t + 1));
+    }
+  }
+  if (target == 0) {
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) mine += units_[i];
+    all = sum_rows(mine, before);
+  }
+  if ((int64_t)w * run >= all) return;  // the same for the whole workgroup
+  const int u_end = min((w + 1) * run, all);
+  int u = w * run, row = 0;
+  const int before_lane = before, slots_lane = slots_of(units_[0], target);
+  if (few) {
+    row = (int)__builtin_ctzll(__ballot(u >= before && u < before + slots_lane));
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if (i < per && r0 + i < a.rows) {
+        const int n = slots_of(units_[i], target);
+        pre[r0 + i] = before;
+        if (u >= before && u < before + n) first_row = r0 + i;
+        before += n;
+      }
+    }
+    if (tid == 0) pre[a.rows] = all;
+    __syncthreads();
+    row = first_row;
+  }
+  // A row's first slot and slots.
+  auto slots_at = [&](int r, int& base) -> int {
+    if (few) {
+      base = __builtin_amdgcn_readlane(before_lane, r);
+      return __builtin_amdgcn_readlane(slots_lane, r);
+    }
+    base = __builtin_amdgcn_readfirstlane(pre[r]);
+    return __builtin_amdgcn_readfirstlane(pre[r + 1]) - base;
+  };
   bool first_segment = true;
-  int waiting = 0;  // outputs of this run that other workers share
+  int waiting = 0, shared0 = 0, shared1 = 0;  // this run's outputs that other workers share
   const int hk = y / a.q_tiles, qt = y % a.q_tiles;
   const int head0 = hk * a.group + qt * 16;
   const int heads = min(16, a.group - qt * 16);
@@ -486,13 +587,14 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
   };
   for (; u < u_end; ++row) {
     row = __builtin_amdgcn_readfirstlane(row);
-    const int base = __builtin_amdgcn_readfirstlane(pre[row]);
-    const int units = __builtin_amdgcn_readfirstlane(pre[row + 1]) - base;
-    const int n = __builtin_amdgcn_readfirstlane(len[row]);
-    const int sq = __builtin_amdgcn_readfirstlane(seq[row]);
-    const int c0 = u - base;
-    const int c1 = min(units, c0 + (u_end - u));
+    int base;
+    const int row_slots = slots_at(row, base);
+    const int n = few ? __builtin_amdgcn_readlane(n_lane, row) : __builtin_amdgcn_readfirstlane(len[row]);
+    const int sq = few ? __builtin_amdgcn_readlane(seq_lane, row) : __builtin_amdgcn_readfirstlane(seq[row]);
     const int first = a.window > 0 ? max(0, n - a.window) : 0;
+    const int units = units_of(first, n), each = slot_units(units, target);
+    const int s0 = u - base, s1 = min(row_slots, s0 + (u_end - u));
+    const int c0 = s0 * each, c1 = min(units, s1 * each);
     const int64_t grow = a.row0 + row;
 
     uint4 q[Tl::kSteps];
@@ -631,7 +733,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
                           acc[c + 3][i] * mine);
     }
     __syncthreads();
-    const bool full = c0 == 0 && c1 == units;
+    const bool full = s0 == 0 && s1 == row_slots;
     // Maximum and sum of query h over the wavefronts.
     auto join = [&](int h, float& M, float& L) {
       M = ms[0][h];
@@ -666,10 +768,11 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
       }
     }
     if (!full) {
-      if (tid == 0) shared_row[waiting] = row;
+      if (waiting == 0) shared0 = row;
+      else shared1 = row;
       ++waiting;
     }
-    u += c1 - c0;
+    u += s1 - s0;
     first_segment = false;
   }
   if (waiting == 0) return;
@@ -678,9 +781,11 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
   // it takes their tickets, and whose ticket is the last joins the parts.
   wait_memory();
   __syncthreads();
+  int base0, base1;
+  const int end0 = slots_at(shared0, base0) + base0, end1 = slots_at(shared1, base1) + base1;
   if (tid < waiting) {
-    const int base = pre[shared_row[tid]], units = pre[shared_row[tid] + 1] - base;
-    const int wa = base / run, wb = (base + units - 1) / run;  // the first and the last worker
+    const int base = tid ? base1 : base0, end = tid ? end1 : end0;
+    const int wa = base / run, wb = (end - 1) / run;  // the first and the last worker
     last[tid] = __hip_atomic_fetch_add(&a.tickets[(wa * Y + y) * kTicketStride], 1u, __ATOMIC_RELAXED,
                                        __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(wb - wa);
     wait_memory();
@@ -688,10 +793,8 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
   __syncthreads();
   for (int turn = 0; turn < waiting; ++turn) {
     if (!last[turn]) continue;
-    const int shared = __builtin_amdgcn_readfirstlane(shared_row[turn]);
-    const int base = __builtin_amdgcn_readfirstlane(pre[shared]);
-    const int units = __builtin_amdgcn_readfirstlane(pre[shared + 1]) - base;
-    const int wa = base / run, parts = (base + units - 1) / run - wa + 1;
+    const int shared = turn ? shared1 : shared0, base = turn ? base1 : base0, end = turn ? end1 : end0;
+    const int wa = base / run, parts = (end - 1) / run - wa + 1;
     const int lead = base % run ? 1 : 0;  // the first one's last segment, or its first
     auto part_at = [&](int i) {
       return a.parts + (int64_t)(2 * ((wa + i) * Y + y) + (i == 0 ? lead : 0)) * a.part_floats;
