@@ -187,8 +187,6 @@ struct Half16<Fp16> {
 };
 
 constexpr int kTileKeys = 32;   // keys of one wavefront's step
-constexpr int kAttnWaves = 4;
-constexpr int kUnitKeys = kTileKeys * kAttnWaves;
 constexpr int kMaxRows = 1024;  // rows of one launch
 
 typedef const __attribute__((address_space(4))) int32_t* ConstI32;
@@ -218,11 +216,12 @@ __device__ __forceinline__ Span span_of(const AttendArg& a, int row) {
   s.first = a.window > 0 ? max(0, n - a.window) : 0;
   return s;
 }
-// Its units of kUnitKeys keys, from the tile of its first key on; a row
-// without keys has one, which writes its zeros.
+// Its units, of a tile for each of kWaves wavefronts, from the tile of its first
+// key on; a row without keys has one, which writes its zeros.
+template <int kWaves>
 __device__ __forceinline__ int units_of(int first, int n) {
   const int t0 = first / kTileKeys, t1 = (n + kTileKeys - 1) / kTileKeys;
-  return max(1, (t1 - t0 + kAttnWaves - 1) / kAttnWaves);
+  return max(1, (t1 - t0 + kWaves - 1) / kWaves);
 }
 
 // One tile of 32 keys of one key head, as the matrix instructions take it: two
@@ -257,8 +256,8 @@ struct Tile {
   static constexpr int kPairs = kDh / (8 * kChunkDims);    // loads of an octet
   static constexpr int kDims = kDh / 16;                   // output dimensions of a lane
   static constexpr int kVWords = kDims * kItem / 4;
-  // Units of all lines that memory (6 TB/s) takes in the time of one worker's unit.
-  static constexpr int kBusyUnits = 160 * 512 / (2 * kDh * kItem);
+  // Tiles of all lines that memory (6 TB/s) takes in the time of one wavefront's tile.
+  static constexpr int kBusyTiles = 640 * 512 / (2 * kDh * kItem);
   static constexpr bool kSplitV = !kE4M3 && kDh == 256;    // two 16-byte loads, 256 bytes apart
 
   uint32_t k[4][kPairs][kChunkWords];
@@ -441,14 +440,15 @@ __device__ __forceinline__ int slots_of(int units, int target) {
 // heads, which lie next to each other in memory.  Bound by HBM: per tile and
 // wavefront 16 KB (16-bit, 128 dimensions) against about 250 vector and 24
 // matrix instructions.
-template <class T, bool kE4M3, int kDh>
-__global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) {
+template <class T, bool kE4M3, int kDh, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attention_kernel(AttendArg a) {
+  constexpr int kThreads = 64 * kWaves;
   typedef Tile<T, kE4M3, kDh> Tl;
   constexpr int kRow = kDh + 4;  // padded: lanes 16 apart in dimensions, 1 in queries
   __shared__ int pre[kMaxRows + 1], len[kMaxRows], seq[kMaxRows];
-  __shared__ int wave_sum[kAttnWaves], wave_most[kAttnWaves];
-  __shared__ float ms[kAttnWaves][16], ls[kAttnWaves][16];
-  __shared__ __attribute__((aligned(16))) float os[kAttnWaves][16][kRow];
+  __shared__ int wave_sum[kWaves], wave_most[kWaves];
+  __shared__ float ms[kWaves][16], ls[kWaves][16];
+  __shared__ __attribute__((aligned(16))) float os[kWaves][16][kRow];
   __shared__ float4 striped[kThreads];
   __shared__ float striped_m[kThreads], striped_l[kThreads];
   __shared__ int last[2], first_row;
@@ -478,7 +478,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
         len[r0 + i] = s.n;
         seq[r0 + i] = s.seq;
       }
-      units_[i] = units_of(s.first, s.n);
+      units_[i] = units_of<kWaves>(s.first, s.n);
     }
     total += units_[i];
     most = max(most, units_[i]);
@@ -494,7 +494,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
     __syncthreads();
     int sum = 0;
 #pragma unroll
-    for (int i = 0; i < kAttnWaves; ++i) {
+    for (int i = 0; i < kWaves; ++i) {
       before += i < wave ? wave_sum[i] : 0;
       sum += wave_sum[i];
     }
@@ -507,7 +507,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
     if (lane == 0) wave_most[wave] = most;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kAttnWaves; ++i) most = max(most, wave_most[i]);
+    for (int i = 0; i < kWaves; ++i) most = max(most, wave_most[i]);
   }
   most = __builtin_amdgcn_readfirstlane(most);
   int run = (total + a.workers - 1) / a.workers, target = 0, all = total;
@@ -515,7 +515,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
     // The smallest target tried for which the workers suffice; they do for the
     // last one, since the sum of ceil(units / target) <= total / target + rows.
     const int spare = a.workers - a.rows, enough = (total + spare - 1) / spare;
-    const int busy = (int)min((int64_t)INT32_MAX, (int64_t)total * Y / Tl::kBusyUnits + 1);
+    const int busy = (int)min((int64_t)INT32_MAX, (int64_t)total * Y / (Tl::kBusyTiles / kWaves) + 1);
     int t = most - max(run, busy) < kPays ? most : run;
     while (true) {
       int mine = 0;
@@ -592,7 +592,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
     const int n = few ? __builtin_amdgcn_readlane(n_lane, row) : __builtin_amdgcn_readfirstlane(len[row]);
     const int sq = few ? __builtin_amdgcn_readlane(seq_lane, row) : __builtin_amdgcn_readfirstlane(seq[row]);
     const int first = a.window > 0 ? max(0, n - a.window) : 0;
-    const int units = units_of(first, n), each = slot_units(units, target);
+    const int units = units_of<kWaves>(first, n), each = slot_units(units, target);
     const int s0 = u - base, s1 = min(row_slots, s0 + (u_end - u));
     const int c0 = s0 * each, c1 = min(units, s1 * each);
     const int64_t grow = a.row0 + row;
@@ -611,8 +611,8 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
     float m = -INFINITY, l = 0.f;
 
     const int t0 = first / kTileKeys;
-    const int t_end = min(t0 + c1 * kAttnWaves, (n + kTileKeys - 1) / kTileKeys);
-    int t = t0 + c0 * kAttnWaves + wave;
+    const int t_end = min(t0 + c1 * kWaves, (n + kTileKeys - 1) / kTileKeys);
+    int t = t0 + c0 * kWaves + wave;
     const ConstI32 table = (ConstI32)(a.table + (int64_t)sq * a.table_stride);
     const uint8_t* kbase = a.kv.k + (int64_t)hk * a.kv.head_bytes;
     const uint8_t* vbase = a.kv.v + (int64_t)hk * a.kv.head_bytes;
@@ -644,10 +644,10 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
       place(now, t * kTileKeys, off);
       load_k(off);
       load_v(off);
-      if (t + kAttnWaves < t_end) next = octets_of(a, table, (t + kAttnWaves) * kTileKeys, n);
+      if (t + kWaves < t_end) next = octets_of(a, table, (t + kWaves) * kTileKeys, n);
     }
     while (t < t_end) {
-      const int key0 = t * kTileKeys, tn = t + kAttnWaves;
+      const int key0 = t * kTileKeys, tn = t + kWaves;
       const bool more = tn < t_end;
       f32x4 s[2];
       tile.scores(q, (lane & 2) != 0, s);
@@ -705,7 +705,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
       if (more) {
         load_v(off);
         now = next;
-        if (tn + kAttnWaves < t_end) next = octets_of(a, table, (tn + kAttnWaves) * kTileKeys, n);
+        if (tn + kWaves < t_end) next = octets_of(a, table, (tn + kWaves) * kTileKeys, n);
       }
       t = tn;
     }
@@ -721,7 +721,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
     __syncthreads();
     float M = ms[0][l16];
 #pragma unroll
-    for (int i = 1; i < kAttnWaves; ++i) M = fmaxf(M, ms[i][l16]);
+    for (int i = 1; i < kWaves; ++i) M = fmaxf(M, ms[i][l16]);
     const float mine = part_weight(m, M);
     if (l16 < heads) {
 #pragma unroll
@@ -737,9 +737,9 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
     // Maximum and sum of query h over the wavefronts.
     auto join = [&](int h, float& M, float& L) {
       M = ms[0][h];
-      for (int i = 1; i < kAttnWaves; ++i) M = fmaxf(M, ms[i][h]);
+      for (int i = 1; i < kWaves; ++i) M = fmaxf(M, ms[i][h]);
       L = 0.f;
-      for (int i = 0; i < kAttnWaves; ++i)
+      for (int i = 0; i < kWaves; ++i)
         L += ls[i][h] * part_weight(ms[i][h], M);
     };
     float* part = a.parts + (int64_t)(2 * blockIdx.x + (first_segment ? 0 : 1)) * a.part_floats;
@@ -747,7 +747,7 @@ __global__ __launch_bounds__(kThreads) void paged_attention_kernel(AttendArg a) 
       const int h = x / (kDh / 4), d = 4 * (x % (kDh / 4));
       float4 o = *reinterpret_cast<const float4*>(&os[0][h][d]);
 #pragma unroll
-      for (int i = 1; i < kAttnWaves; ++i) {
+      for (int i = 1; i < kWaves; ++i) {
         const float4 e = *reinterpret_cast<const float4*>(&os[i][h][d]);
         o.x += e.x, o.y += e.y, o.z += e.z, o.w += e.w;
       }
@@ -976,14 +976,25 @@ void launch_append(const AppendArg& a, int head_dim, bool inter, dim3 grid, hipS
 }
 
 template <class T, bool kE4M3>
-void launch_attend(const AttendArg& a, int head_dim, hipStream_t stream) {
-  const dim3 grid((unsigned)(a.workers * a.kv.n_kv_heads * a.q_tiles));
-  if (head_dim == 64)
-    hipLaunchKernelGGL((paged_attention_kernel<T, kE4M3, 64>), grid, dim3(kThreads), 0, stream, a);
-  else if (head_dim == 128)
-    hipLaunchKernelGGL((paged_attention_kernel<T, kE4M3, 128>), grid, dim3(kThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL((paged_attention_kernel<T, kE4M3, 256>), grid, dim3(kThreads), 0, stream, a);
+void launch_attend(const AttendArg& a, int head_dim, int waves, hipStream_t stream) {
+  const dim3 grid((unsigned)(a.workers * a.kv.n_kv_heads * a.q_tiles)), block(64 * waves);
+#define ATTEND_CASE(D, W) \
+  hipLaunchKernelGGL((paged_attention_kernel<T, kE4M3, D, W>), grid, block, 0, stream, a)
+  if (head_dim == 256) {
+    ATTEND_CASE(256, 4);
+  } else if (head_dim == 128) {
+    if constexpr (kE4M3) {
+      if (waves == 8) {
+        ATTEND_CASE(128, 8);
+        return;
+      }
+    }
+    ATTEND_CASE(128, 4);
+  } else {
+    if (waves == 8) ATTEND_CASE(64, 8);
+    else ATTEND_CASE(64, 4);
+  }
+#undef ATTEND_CASE
 }
 
 // How a call is launched: rows per launch (their units stay below 2^31), the
@@ -991,21 +1002,26 @@ void launch_attend(const AttendArg& a, int head_dim, hipStream_t stream) {
 // and the floats of one workgroup's record for a split output.
 struct AttendPlan {
   int64_t rows_per_launch;
-  int workers, lines, part_floats;
+  int waves, workers, lines, part_floats;
+  int64_t most_parts;  // workgroups of any plan with these rows, heads and max_keys
 };
-constexpr int kWorkers = 512;
-AttendPlan attend_plan(const emoe_paged_kv& kv, int32_t rows, int32_t n_heads, int32_t max_keys) {
+AttendPlan attend_plan(const emoe_paged_kv& kv, int32_t rows, int32_t n_heads, int32_t max_keys,
+                       int32_t window) {
   const int group = n_heads / kv.n_kv_heads;
-  const int64_t most = (int64_t)max_keys / kUnitKeys + 2;  // units of one row
+  const int64_t keys = window > 0 && window < max_keys ? window : max_keys;
+  const int row_bytes = kv.head_dim * (kv.dtype == EMOE_E4M3 ? 1 : 2);
   AttendPlan p;
   p.lines = kv.n_kv_heads * ((group + 15) / 16);
+  p.waves = row_bytes <= 128 && keys > 256 && (int64_t)rows * p.lines <= 512 ? 8 : 4;
+  const int64_t most = keys / (kTileKeys * p.waves) + 2;  // units of one row
   p.rows_per_launch = (((int64_t)1 << 31) - 1 - kTickets) / most;
   if (p.rows_per_launch > kMaxRows) p.rows_per_launch = kMaxRows;
   const int64_t held = rows < p.rows_per_launch ? rows : p.rows_per_launch;
-  int64_t workers = kWorkers / p.lines;
+  int64_t workers = (kv.head_dim == 256 ? 256 : 512) / p.lines;
   if (workers < 1) workers = 1;
   p.workers = (int)(held * most < workers ? held * most : workers);
   p.part_floats = 32 + (group < 16 ? group : 16) * kv.head_dim;
+  p.most_parts = p.lines > 512 ? p.lines : 512;
   return p;
 }
 
@@ -1080,8 +1096,8 @@ int32_t emoe_paged_append(const emoe_paged_kv* kv, const emoe_paged_append_args*
 size_t emoe_paged_attention_workspace_bytes(const emoe_paged_kv* kv, int32_t rows, int32_t n_heads,
                                             int32_t max_keys) {
   if (check_kv(kv) || rows < 0 || n_heads < 1 || n_heads % kv->n_kv_heads || max_keys < 0) return 0;
-  const AttendPlan p = attend_plan(*kv, rows, n_heads, max_keys);
-  return EMOE_SERVING_TICKET_BYTES + (size_t)2 * p.workers * p.lines * p.part_floats * 4;
+  const AttendPlan p = attend_plan(*kv, rows, n_heads, max_keys, 0);
+  return EMOE_SERVING_TICKET_BYTES + (size_t)2 * p.most_parts * p.part_floats * 4;
 }
 
 int32_t emoe_paged_attention(const emoe_paged_kv* kv, const emoe_paged_attention_args* args,
@@ -1108,7 +1124,7 @@ int32_t emoe_paged_attention(const emoe_paged_kv* kv, const emoe_paged_attention
     return report_error(EMOE_EINVAL, "workspace of %zu bytes < %zu needed", workspace ? workspace_bytes : 0,
                         need);
   if (!aligned16(workspace)) return report_error(EMOE_EINVAL, "workspace: need 16-byte alignment");
-  const AttendPlan plan = attend_plan(*kv, A.rows, A.n_heads, A.max_keys);
+  const AttendPlan plan = attend_plan(*kv, A.rows, A.n_heads, A.max_keys, A.window);
   AttendArg a;
   a.kv = view_of(*kv);
   a.q = static_cast<const uint16_t*>(A.q);
@@ -1137,11 +1153,11 @@ int32_t emoe_paged_attention(const emoe_paged_kv* kv, const emoe_paged_attention
     a.row0 = (int32_t)r0;
     a.rows = (int32_t)(A.rows - r0 < plan.rows_per_launch ? A.rows - r0 : plan.rows_per_launch);
     if (A.dtype == EMOE_BF16) {
-      if (e4m3) launch_attend<Bf16, true>(a, kv->head_dim, stream);
-      else launch_attend<Bf16, false>(a, kv->head_dim, stream);
+      if (e4m3) launch_attend<Bf16, true>(a, kv->head_dim, plan.waves, stream);
+      else launch_attend<Bf16, false>(a, kv->head_dim, plan.waves, stream);
     } else {
-      if (e4m3) launch_attend<Fp16, true>(a, kv->head_dim, stream);
-      else launch_attend<Fp16, false>(a, kv->head_dim, stream);
+      if (e4m3) launch_attend<Fp16, true>(a, kv->head_dim, plan.waves, stream);
+      else launch_attend<Fp16, false>(a, kv->head_dim, plan.waves, stream);
     }
     if ((st = launched("paged_attention_kernel"))) return st;
   }
