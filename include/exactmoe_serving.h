@@ -126,8 +126,8 @@ typedef struct emoe_paged_attention_args {
 /* Workspace of the attention.  Its first EMOE_SERVING_TICKET_BYTES count
  * finished workgroups: zero them once, before the workspace's first call; every
  * call leaves them zero.  The rest needs no initial value.  One workspace may
- * serve calls of any sizes and both kinds (attention and logits), captured or
- * not, as long as no two of them overlap in time. */
+ * serve attention calls of any sizes, captured or not, as long as no two of them
+ * overlap in time, and no other use. */
 #define EMOE_SERVING_TICKET_BYTES 131072
 size_t emoe_paged_attention_workspace_bytes(const emoe_paged_kv* kv, int32_t rows, int32_t n_heads,
                                             int32_t max_keys);
@@ -171,7 +171,10 @@ typedef struct emoe_logits_args {
   int32_t history_width, bias_width, n_masks;  /* bias_width below 2^23 */
 } emoe_logits_args;
 
-/* Workspace (needed with next_token only); its beginning as the attention's. */
+/* Workspace (needed with next_token only): what the workgroups of a row hand
+ * over to each other.  Zero it once, before its first call; every call leaves it
+ * zero.  It may serve calls of any sizes, captured or not, as long as no two of
+ * them overlap in time, and no other use. */
 size_t emoe_process_logits_workspace_bytes(int32_t rows, int32_t vocab);
 
 int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_t workspace_bytes,
@@ -194,7 +197,7 @@ typedef struct emoe_decoder_batch {
 } emoe_decoder_batch;
 
 /* Workspace of emoe_decoder_forward_paged; needs no initial value, since the
- * call clears its tickets itself. */
+ * call clears what has to be zero. */
 size_t emoe_decoder_paged_workspace_bytes(const emoe_decoder_dims* dims, int32_t n_tokens,
                                           int32_t n_out, int32_t max_keys);
 

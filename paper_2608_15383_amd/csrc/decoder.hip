@@ -201,22 +201,26 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(int V, int d, const int
 
 // The beginning of a call over paged caches: embed_kernel's rows, each token's
 // number of keys (its own position included; 0 for padding), the rotation's
-// frequencies in memory, and the attention's tickets cleared (by the
-// workgroups from n_tokens on).
+// frequencies in memory, and what has to be zero of the attention's and the
+// logits' workspaces cleared (by the workgroups from n_tokens on).
 struct PagedStart {
   const int32_t *tokens, *positions, *seqs;
   int32_t* lengths;
   double* inv_freq;
-  uint4* tickets;
-  int32_t n_tokens, n_seqs, half;
+  uint4 *tickets, *logit_words;
+  int32_t n_logit_words, n_tokens, n_seqs, half;  // words of 16 bytes
 };
+constexpr int kClearGroups = 32;
 __global__ __launch_bounds__(kThreads) void paged_start_kernel(int V, int d, PagedStart a,
                                                                RopeTable rope, const uint16_t* embed,
                                                                uint16_t* x) {
   const int t = blockIdx.x;
   if (t >= a.n_tokens) {
-    const int i = (t - a.n_tokens) * kThreads + threadIdx.x;
-    if (i < EMOE_SERVING_TICKET_BYTES / 16) a.tickets[i] = make_uint4(0, 0, 0, 0);
+    const int i0 = (t - a.n_tokens) * kThreads + threadIdx.x;
+    for (int i = i0; i < EMOE_SERVING_TICKET_BYTES / 16; i += kClearGroups * kThreads)
+      a.tickets[i] = make_uint4(0, 0, 0, 0);
+    for (int i = i0; i < a.n_logit_words; i += kClearGroups * kThreads)
+      a.logit_words[i] = make_uint4(0, 0, 0, 0);
     if (t == a.n_tokens && threadIdx.x < a.half) a.inv_freq[threadIdx.x] = rope.inv[threadIdx.x];
     return;
   }
@@ -683,10 +687,10 @@ struct WsLayout {
   size_t x0, x1, n, qkv, attn, moe_y, moe_ws, moe_ws_bytes, total;
 };
 
-// What a call over paged caches has besides: tickets first, as the attention's
-// and the logits' workspace begins, which `shared` serves.
+// What a call over paged caches has besides: the attention's and the logits'
+// workspaces, the rows' lengths and the rotation's frequencies.
 struct PagedLayout {
-  size_t shared, shared_bytes, lengths, inv_freq, base, total;
+  size_t attn, attn_bytes, logits, logits_bytes, lengths, inv_freq, base, total;
 };
 
 WsLayout decoder_ws_layout(const emoe_decoder_dims& dd, int T);
@@ -709,10 +713,10 @@ PagedLayout paged_layout(const emoe_decoder_dims& dd, int T, int n_out, int max_
     off += align_up(bytes);
     return at;
   };
-  const size_t attn = emoe_paged_attention_workspace_bytes(&kv, T, dd.n_heads, max_keys);
-  const size_t logits = emoe_process_logits_workspace_bytes(n_out, dd.vocab);
-  L.shared_bytes = attn > logits ? attn : logits;
-  L.shared = take(L.shared_bytes);
+  L.attn_bytes = emoe_paged_attention_workspace_bytes(&kv, T, dd.n_heads, max_keys);
+  L.attn = take(L.attn_bytes);
+  L.logits_bytes = emoe_process_logits_workspace_bytes(n_out, dd.vocab);
+  L.logits = take(L.logits_bytes);
   L.lengths = take((size_t)T * 4);
   L.inv_freq = take(sizeof(RopeTable));
   L.base = take(decoder_ws_layout(dd, T).total);
@@ -1065,7 +1069,7 @@ int32_t emoe_decoder_forward_paged(emoe_decoder* dec, const emoe_paged_kv* kv,
   lg.dtype = EMOE_F32;
   lg.rows = n_out;
   lg.vocab = D.vocab;
-  if ((st = check_process_logits(lg, ws + P.shared, P.shared_bytes))) return st;
+  if ((st = check_process_logits(lg, ws + P.logits, P.logits_bytes))) return st;
 
   const rocblas_status rs = rocblas_set_stream(dec->blas, stream);
   if (rs != rocblas_status_success)
@@ -1076,13 +1080,14 @@ int32_t emoe_decoder_forward_paged(emoe_decoder* dec, const emoe_paged_kv* kv,
   start.seqs = B.seqs;
   start.lengths = lengths;
   start.inv_freq = inv_freq;
-  start.tickets = reinterpret_cast<uint4*>(ws + P.shared);
+  start.tickets = reinterpret_cast<uint4*>(ws + P.attn);
+  start.logit_words = reinterpret_cast<uint4*>(ws + P.logits);
+  start.n_logit_words = (int32_t)(align_up(P.logits_bytes) / 16);
   start.n_tokens = T;
   start.n_seqs = B.n_seqs;
   start.half = Dh / 2;
-  constexpr int kClear = (EMOE_SERVING_TICKET_BYTES / 16 + kThreads - 1) / kThreads;
   static_assert(kMaxHeadDim / 2 <= kThreads, "a thread per frequency");
-  DEC_LAUNCH(paged_start_kernel, dim3(T + kClear), dim3(kThreads), 0, stream, D.vocab, d, start,
+  DEC_LAUNCH(paged_start_kernel, dim3(T + kClearGroups), dim3(kThreads), 0, stream, D.vocab, d, start,
              dec->rope, dec->embed, xa);
   const uint16_t* delta = nullptr;
   const bool norm_in_gemv = T <= kDenseMaxTokens && d <= kNormMaxInputs;
@@ -1098,7 +1103,7 @@ int32_t emoe_decoder_forward_paged(emoe_decoder* dec, const emoe_paged_kv* kv,
       if ((st = dense(dec, T, 3 * d, d, n, dec->wqkv[l], nullptr, qkv, false, stream))) return st;
     }
     if ((st = emoe_paged_append(&kv[l], &ap, stream))) return st;
-    if ((st = emoe_paged_attention(&kv[l], &at_args, ws + P.shared, P.shared_bytes, stream))) return st;
+    if ((st = emoe_paged_attention(&kv[l], &at_args, ws + P.attn, P.attn_bytes, stream))) return st;
     if ((st = dense(dec, T, d, d, attn, dec->wo[l], xa, xb, false, stream))) return st;  // x += attn Wo^T
     std::swap(xa, xb);
     DEC_LAUNCH(add_rmsnorm_kernel<false>, dim3(T), dim3(kThreads), 0, stream, d, xa, nullptr,
@@ -1112,7 +1117,7 @@ int32_t emoe_decoder_forward_paged(emoe_decoder* dec, const emoe_paged_kv* kv,
   DEC_LAUNCH(add_rmsnorm_kernel<true>, dim3(n_out), dim3(kThreads), 0, stream, d, xa, delta,
              dec->final_norm, D.rms_eps, n, PickRows{B.out_rows, T});
   if ((st = dense(dec, n_out, D.vocab, d, n, dec->lm_head, nullptr, logits, true, stream))) return st;
-  return emoe_process_logits(&lg, ws + P.shared, P.shared_bytes, stream);
+  return emoe_process_logits(&lg, ws + P.logits, P.logits_bytes, stream);
 }
 
 }  // extern "C"

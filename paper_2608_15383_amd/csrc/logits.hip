@@ -6,7 +6,7 @@ using namespace emoe;
 
 namespace {
 
-constexpr int kBestStride = kTicketLine / 8;  // a chunk's best has a line of its own, too
+constexpr int kMaxRows = 4096;  // rows of one launch
 constexpr int kLongHistory = 4096;
 constexpr uint32_t kBiasIndices = 1u << 23;  // bits of the smallest normal number
 
@@ -21,8 +21,7 @@ struct LogitsArg {
   const int32_t* bias_counts;
   const uint32_t* mask;
   const int32_t* mask_rows;
-  uint32_t* tickets;
-  uint64_t* best;  // [row of the launch][chunk], a line each
+  uint64_t* best;  // [row of the launch][chunk]: the chunks' best choices, handed over
   int64_t logits_stride, out_stride, history_stride, bias_stride, mask_stride;
   int32_t row0, vocab, history_width, bias_width, n_masks, chunks;
 };
@@ -129,6 +128,15 @@ __device__ __forceinline__ uint64_t choice(float x, int v) {
   const uint32_t o = (b & 0x80000000u) ? ~b : b | 0x80000000u;
   return ((uint64_t)o << 32) | (uint32_t)~v;
 }
+// Hand-over between the workgroups of a row: a chunk's word is 0 until its
+// workgroup stores its best choice, device-coherently, and 0 again when the
+// row's last workgroup has read it; kNoChoice stands for 0 meanwhile.  Counting
+// finished workgroups instead takes one trip to memory more, 0.8 us of the 5 that
+// a row of 50,304 logits takes.  The wait is for workgroups of lower index only,
+// which were dispatched before, and bounded (kSpinLimit polls, about a second):
+// one that gives up makes the token -1, and the workspace has to be zeroed again.
+constexpr uint64_t kNoChoice = 1;
+constexpr int kSpinLimit = 1 << 19;
 __device__ __forceinline__ int chosen(uint64_t c) { return c ? (int)~(uint32_t)c : -1; }
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
@@ -146,8 +154,8 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t c) {
 // are taken out of their registers one by one, the mask replaces words, and
 // everything else goes from load to store as it came (a 16-bit logit is its
 // own rounding); the greedy choice needs one comparison per chunk of 16 bytes
-// unless that holds a new best.  The row's last workgroup to finish (a ticket
-// in the workspace) takes the best of its chunks' best.  Rows start at any
+// unless that holds a new best.  The workgroup of the row's last chunk takes the
+// best of the chunks' best, which the others hand over.  Rows start at any
 // element: the chunks of 16 bytes are loaded unaligned.
 template <class F, int kThreads, int kLoads, bool kBias>
 __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
@@ -361,22 +369,16 @@ __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
   // The choice goes out before the row does: its hand-over takes two trips to
   // memory, which the stores then do not stand in front of.
   const bool choose = a.next_token != nullptr;
-  uint32_t before = 0;
+  uint64_t top = 0;
   if (choose) {
-    uint64_t top = wave_max(choice(best, best_at));
+    top = wave_max(choice(best, best_at));
     if ((tid & 63) == 0) red[tid >> 6] = top;
     __syncthreads();
     if (tid == 0) {
       for (int i = 1; i < kThreads / 64; ++i) top = max64(top, red[i]);
-      if (a.chunks == 1) {
-        a.next_token[row] = chosen(top);
-      } else {
-        __hip_atomic_store(&a.best[((int64_t)lr * a.chunks + chunk) * kBestStride], top,
+      if (chunk < a.chunks - 1)
+        __hip_atomic_store(&a.best[(int64_t)lr * a.chunks + chunk], top ? top : kNoChoice,
                            __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        wait_memory();
-        before = __hip_atomic_fetch_add(&a.tickets[lr * kTicketStride], 1u, __ATOMIC_RELAXED,
-                                        __HIP_MEMORY_SCOPE_AGENT);
-      }
     }
   }
 #pragma unroll
@@ -384,18 +386,27 @@ __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
     const int v = c0 + (u * kThreads + tid) * kPer;
     if (v < V) store_chunk<F>(dst, v, V, raw[u]);
   }
-  if (!choose || a.chunks == 1 || tid >= 64) return;
-  if (__builtin_amdgcn_readfirstlane(before) != (uint32_t)a.chunks - 1) return;
-  wait_memory();
-  uint64_t top = 0;
-  for (int i = tid; i < a.chunks; i += 64)
-    top = max64(top, __hip_atomic_load(&a.best[((int64_t)lr * a.chunks + i) * kBestStride],
-                                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-  top = wave_max(top);
-  if (tid == 0) {
-    a.next_token[row] = chosen(top);
-    st_u32<true>(&a.tickets[lr * kTicketStride], 0);
+  // The row's last workgroup waits for the others' words.
+  if (!choose || chunk < a.chunks - 1 || tid >= 64) return;
+  top = tid == 0 ? top : 0;
+  bool gave_up = false;
+  for (int i = tid; i < a.chunks - 1; i += 64) {
+    uint64_t* word = &a.best[(int64_t)lr * a.chunks + i];
+    uint64_t other = 0;
+    for (int spin = 0; !other; ++spin) {
+      other = __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (!other && spin == kSpinLimit) {
+        gave_up = true;
+        break;
+      }
+      if (!other) __builtin_amdgcn_s_sleep(4);
+    }
+    __hip_atomic_store(word, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (other != kNoChoice) top = max64(top, other);
   }
+  top = wave_max(top);
+  const bool failed = __any(gave_up);
+  if (tid == 0) a.next_token[row] = failed ? -1 : chosen(top);
 }
 
 // How a call is cut: threads and 16-byte loads of a workgroup.
@@ -486,8 +497,8 @@ extern "C" {
 
 size_t emoe_process_logits_workspace_bytes(int32_t rows, int32_t vocab) {
   if (rows < 0 || vocab < 1) return 0;
-  const size_t held = rows < kTickets ? rows : kTickets;  // rows of one launch
-  return EMOE_SERVING_TICKET_BYTES + held * (((size_t)vocab + 1023) / 1024) * kTicketLine;  // the smallest chunks
+  const size_t held = rows < kMaxRows ? rows : kMaxRows;
+  return held * (((size_t)vocab + 1023) / 1024) * 8;  // the smallest chunks
 }
 
 int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_t workspace_bytes,
@@ -513,9 +524,7 @@ int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_
   a.bias_counts = A.bias_counts;
   a.mask = A.mask;
   a.mask_rows = A.mask_rows;
-  a.tickets = static_cast<uint32_t*>(workspace);
-  a.best = reinterpret_cast<uint64_t*>(static_cast<uint8_t*>(workspace) + EMOE_SERVING_TICKET_BYTES);
-  if (!A.next_token) a.tickets = nullptr, a.best = nullptr;
+  a.best = static_cast<uint64_t*>(workspace);
   a.logits_stride = A.logits_stride;
   a.out_stride = A.out_stride;
   a.history_stride = A.history_stride;
@@ -526,9 +535,9 @@ int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_
   a.bias_width = A.bias_width;
   a.n_masks = A.n_masks;
   a.chunks = plan.chunks;
-  // Rows of one launch: a ticket each, and a grid below 2^31 workgroups.
+  // Rows of one launch: a grid below 2^31 workgroups.
   int64_t step = ((int64_t)1 << 30) / plan.chunks;
-  if (step > kTickets) step = kTickets;
+  if (step > kMaxRows) step = kMaxRows;
   for (int64_t r0 = 0; r0 < A.rows; r0 += step) {
     a.row0 = (int32_t)r0;
     const int64_t n = A.rows - r0 < step ? A.rows - r0 : step;

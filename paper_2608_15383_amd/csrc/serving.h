@@ -1,5 +1,5 @@
 // Shared by the kernels of exactmoe_serving.h: the 16-bit and 8-bit element
-// types and the workspace's ticket words.
+// types and the attention's tickets.
 #pragma once
 
 #include "common.h"
@@ -52,9 +52,9 @@ __device__ __forceinline__ uint2 down8_e4m3(const float (&v)[8]) {
   return w;
 }
 
-// The workspace's tickets, each in a line of its own: device-coherent atomics
+// The attention's tickets, each in a line of its own: device-coherent atomics
 // on one line come one after the other, whatever the word (19 rows' tickets in
-// one line kept process_logits_kernel busy for 10 us).
+// one line kept a launch busy for 10 us).
 constexpr int kTicketLine = 128, kTicketStride = kTicketLine / 4;
 constexpr int kTickets = EMOE_SERVING_TICKET_BYTES / kTicketLine;
 

@@ -548,7 +548,7 @@ def run_logits(kind, rows, vocab, width, seed, in_place=False, token=True, **kw)
     api.process_logits(out=None if in_place else out[:rows], workspace=ws if token else None,
                        next_token=None if nt is None else nt[:rows], **dev)
     torch.cuda.synchronize()
-    assert not ws[:EMOE_SERVING_TICKET_BYTES].any()
+    assert not ws.any()
     if not in_place:
         assert bool((out[rows:] == 7).all())
         whole = out._base if out._base is not None else out
@@ -578,8 +578,8 @@ def test_logits_large(kind, rows, vocab):
     run_logits(kind, rows, vocab, 300, seed=rows, biases=20, mask="rows")
 
 
-def test_logits_more_rows_than_tickets():
-    rows, vocab = 4099 + 300, 1500
+def test_logits_more_rows_than_one_launch():
+    rows, vocab = 4096 + 300, 1500
     x = torch.randn(rows, vocab, device="cuda:0")
     nt = torch.empty(rows, dtype=torch.int32, device="cuda:0")
     ws = torch.zeros(api.process_logits_workspace_bytes(rows, vocab), dtype=torch.uint8, device="cuda:0")
@@ -642,9 +642,9 @@ class Step:
         self.hist = ids(rng.integers(0, vocab, (rows, 64)))
         self.rep = gpu((1 + rng.random(rows)).astype(np.float32))
         self.next = torch.empty(rows, dtype=torch.int32, device="cuda:0")
-        need = max(api.paged_attention_workspace_bytes(self.kv, rows, heads, 1024),
-                   api.process_logits_workspace_bytes(rows, vocab))
-        self.ws = torch.zeros(need, dtype=torch.uint8, device="cuda:0")
+        zeros = lambda n: torch.zeros(n, dtype=torch.uint8, device="cuda:0")
+        self.ws = zeros(api.paged_attention_workspace_bytes(self.kv, rows, heads, 1024))
+        self.logits_ws = zeros(api.process_logits_workspace_bytes(rows, vocab))
 
     def run(self, stream=None):
         api.paged_append(self.kv, self.q, self.new_k, self.new_v, self.pos, self.table, self.freq,
@@ -652,7 +652,7 @@ class Step:
         api.paged_attention(self.kv, self.qr, self.table, self.n, self.out, self.ws, 1024, stream=stream)
 
     def finish(self, stream=None):
-        api.process_logits(self.x, self.x, self.ws, history=self.hist, repetition=self.rep,
+        api.process_logits(self.x, self.x, self.logits_ws, history=self.hist, repetition=self.rep,
                            next_token=self.next, stream=stream)
 
     def all(self):
@@ -685,11 +685,12 @@ def test_step_against_the_oracle():
 
 
 def test_two_graphs_share_a_workspace():
-    """Captured calls of different sizes over one workspace, replayed in turn with eager ones."""
+    """Captured calls of different sizes over one workspace of each kind, replayed in turn with
+    eager ones."""
     a, b = Step(1), Step(2, rows=9, heads=4, hk=4, vocab=5000)
-    if b.ws.numel() > a.ws.numel():
-        a.ws = b.ws
-    b.ws = a.ws
+    for name in ("ws", "logits_ws"):
+        larger = max((getattr(a, name), getattr(b, name)), key=lambda t: t.numel())
+        setattr(a, name, larger), setattr(b, name, larger)
     want = [[t.clone() for t in s.all()[:2:2]] + [s.next.clone()] for s in (a, b)]
     raw = [torch.mm(s.out.flatten(1), s.head) for s in (a, b)]
     side, graphs = torch.cuda.Stream(), []
@@ -708,7 +709,7 @@ def test_two_graphs_share_a_workspace():
             graphs[i].replay()
             torch.cuda.synchronize()
             assert torch.equal(s.out, want[i][0]) and torch.equal(s.next, want[i][-1]), (turn, i)
-        assert not a.ws[:EMOE_SERVING_TICKET_BYTES].any()
+        assert not a.ws[:EMOE_SERVING_TICKET_BYTES].any() and not a.logits_ws.any()
         a.all()
 
 

