@@ -21,7 +21,8 @@ struct LogitsArg {
   const int32_t* bias_counts;
   const uint32_t* mask;
   const int32_t* mask_rows;
-  uint64_t* best;  // [row of the launch][chunk]: the chunks' best choices, handed over
+  uint32_t* tickets;  // [row of the launch], a line each: workgroups that have started
+  uint64_t* best;     // [row of the launch][chunk]: the chunks' best choices, handed over
   int64_t logits_stride, out_stride, history_stride, bias_stride, mask_stride;
   int32_t row0, vocab, history_width, bias_width, n_masks, chunks;
 };
@@ -128,13 +129,15 @@ __device__ __forceinline__ uint64_t choice(float x, int v) {
   const uint32_t o = (b & 0x80000000u) ? ~b : b | 0x80000000u;
   return ((uint64_t)o << 32) | (uint32_t)~v;
 }
-// Hand-over between the workgroups of a row: a chunk's word is 0 until its
-// workgroup stores its best choice, device-coherently, and 0 again when the
-// row's last workgroup has read it; kNoChoice stands for 0 meanwhile.  Counting
-// finished workgroups instead takes one trip to memory more, 0.8 us of the 5 that
-// a row of 50,304 logits takes.  The wait is for workgroups of lower index only,
-// which were dispatched before, and bounded (kSpinLimit polls, about a second):
-// one that gives up makes the token -1, and the workspace has to be zeroed again.
+// Hand-over between the workgroups of a row.  Each takes a ticket of the row when
+// it starts, on the way with its loads; the one that starts last collects the
+// row's choice.  A chunk's word is 0 until its workgroup stores its best, device-
+// coherently, and 0 again when the collector has read it; kNoChoice stands for 0
+// meanwhile.  The collector waits only for workgroups that run already and wait
+// for nobody, so every wait ends, whatever else the device runs.  To count
+// workgroups as they finish instead takes one trip to memory more, 0.6 us of the
+// 5.8 that a row of 50,304 logits took so.  The bound on the wait (kSpinLimit polls,
+// about a second) is for a workspace that was not zeroed: the token is -1 then.
 constexpr uint64_t kNoChoice = 1;
 constexpr int kSpinLimit = 1 << 19;
 __device__ __forceinline__ int chosen(uint64_t c) { return c ? (int)~(uint32_t)c : -1; }
@@ -154,8 +157,8 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t c) {
 // are taken out of their registers one by one, the mask replaces words, and
 // everything else goes from load to store as it came (a 16-bit logit is its
 // own rounding); the greedy choice needs one comparison per chunk of 16 bytes
-// unless that holds a new best.  The workgroup of the row's last chunk takes the
-// best of the chunks' best, which the others hand over.  Rows start at any
+// unless that holds a new best.  One workgroup of the row takes the best of the
+// chunks' best, which the others hand over.  Rows start at any
 // element: the chunks of 16 bytes are loaded unaligned.
 template <class F, int kThreads, int kLoads, bool kBias>
 __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
@@ -216,6 +219,12 @@ __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
       bias_value = a.bias_values[row * a.bias_stride + tid];
     }
   }
+  // After the loads, which return in order.
+  const bool choose = a.next_token != nullptr;
+  uint32_t* ticket = a.tickets + (int64_t)lr * kTicketStride;
+  uint32_t order = 0;
+  if (choose && a.chunks > 1 && tid == 0)
+    order = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   n_hist = max(0, min(n_hist, a.history_width));
   n_bias = max(0, min(n_bias, a.bias_width));
   const bool count = a.history && !(rep == 1.f && pres == 0.f && freq == 0.f);
@@ -368,15 +377,16 @@ __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
   for (int u = 0; u < kLoads; ++u) step(raw[u], allow[u], (u * kThreads + tid) * kPer);
   // The choice goes out before the row does: its hand-over takes two trips to
   // memory, which the stores then do not stand in front of.
-  const bool choose = a.next_token != nullptr;
   uint64_t top = 0;
+  bool collects = false;
   if (choose) {
     top = wave_max(choice(best, best_at));
     if ((tid & 63) == 0) red[tid >> 6] = top;
     __syncthreads();
+    collects = __builtin_amdgcn_readfirstlane(order) == (uint32_t)a.chunks - 1 && tid < 64;
     if (tid == 0) {
       for (int i = 1; i < kThreads / 64; ++i) top = max64(top, red[i]);
-      if (chunk < a.chunks - 1)
+      if (!collects)
         __hip_atomic_store(&a.best[(int64_t)lr * a.chunks + chunk], top ? top : kNoChoice,
                            __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
@@ -386,11 +396,11 @@ __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
     const int v = c0 + (u * kThreads + tid) * kPer;
     if (v < V) store_chunk<F>(dst, v, V, raw[u]);
   }
-  // The row's last workgroup waits for the others' words.
-  if (!choose || chunk < a.chunks - 1 || tid >= 64) return;
+  if (!collects) return;
   top = tid == 0 ? top : 0;
   bool gave_up = false;
-  for (int i = tid; i < a.chunks - 1; i += 64) {
+  for (int i = tid; i < a.chunks; i += 64) {
+    if (i == chunk) continue;
     uint64_t* word = &a.best[(int64_t)lr * a.chunks + i];
     uint64_t other = 0;
     for (int spin = 0; !other; ++spin) {
@@ -406,7 +416,10 @@ __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
   }
   top = wave_max(top);
   const bool failed = __any(gave_up);
-  if (tid == 0) a.next_token[row] = failed ? -1 : chosen(top);
+  if (tid == 0) {
+    if (a.chunks > 1) st_u32<true>(ticket, 0);
+    a.next_token[row] = failed ? -1 : chosen(top);
+  }
 }
 
 // How a call is cut: threads and 16-byte loads of a workgroup.
@@ -498,7 +511,7 @@ extern "C" {
 size_t emoe_process_logits_workspace_bytes(int32_t rows, int32_t vocab) {
   if (rows < 0 || vocab < 1) return 0;
   const size_t held = rows < kMaxRows ? rows : kMaxRows;
-  return held * (((size_t)vocab + 1023) / 1024) * 8;  // the smallest chunks
+  return held * (kTicketLine + (((size_t)vocab + 1023) / 1024) * 8);  // the smallest chunks
 }
 
 int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_t workspace_bytes,
@@ -524,7 +537,6 @@ int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_
   a.bias_counts = A.bias_counts;
   a.mask = A.mask;
   a.mask_rows = A.mask_rows;
-  a.best = static_cast<uint64_t*>(workspace);
   a.logits_stride = A.logits_stride;
   a.out_stride = A.out_stride;
   a.history_stride = A.history_stride;
@@ -535,9 +547,13 @@ int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_
   a.bias_width = A.bias_width;
   a.n_masks = A.n_masks;
   a.chunks = plan.chunks;
-  // Rows of one launch: a grid below 2^31 workgroups.
-  int64_t step = ((int64_t)1 << 30) / plan.chunks;
+  // Rows of one launch: a grid of at most 2^31 threads (plan.chunks is below 2^18,
+  // and below 2^9 with the smallest chunks).
+  int64_t step = ((int64_t)1 << 21) / plan.chunks;
   if (step > kMaxRows) step = kMaxRows;
+  if (step > A.rows) step = A.rows;
+  a.tickets = static_cast<uint32_t*>(workspace);
+  a.best = reinterpret_cast<uint64_t*>(a.tickets + step * kTicketStride);
   for (int64_t r0 = 0; r0 < A.rows; r0 += step) {
     a.row0 = (int32_t)r0;
     const int64_t n = A.rows - r0 < step ? A.rows - r0 : step;

@@ -1,5 +1,5 @@
 // Shared by the kernels of exactmoe_serving.h: the 16-bit and 8-bit element
-// types and the attention's tickets.
+// types and the tickets of outputs that several workgroups share.
 #pragma once
 
 #include "common.h"
@@ -52,7 +52,7 @@ __device__ __forceinline__ uint2 down8_e4m3(const float (&v)[8]) {
   return w;
 }
 
-// The attention's tickets, each in a line of its own: device-coherent atomics
+// Tickets, each in a line of its own: device-coherent atomics
 // on one line come one after the other, whatever the word (19 rows' tickets in
 // one line kept a launch busy for 10 us).
 constexpr int kTicketLine = 128, kTicketStride = kTicketLine / 4;

@@ -588,6 +588,28 @@ def test_logits_more_rows_than_one_launch():
     assert torch.equal(out, x) and torch.equal(nt.long(), x.argmax(1))
 
 
+def test_logits_of_two_streams_at_once():
+    """Calls with their own workspaces, each with more rows of two chunks than the device holds
+    workgroups: a row's workgroups wait for none that has no place yet."""
+    rows, vocab = 4096, 8000
+    jobs = []
+    for i in range(2):
+        x = torch.randn(rows, vocab, device="cuda:0")
+        nt = torch.empty(rows, dtype=torch.int32, device="cuda:0")
+        ws = torch.zeros(api.process_logits_workspace_bytes(rows, vocab), dtype=torch.uint8, device="cuda:0")
+        jobs.append((x, torch.empty_like(x), ws, nt, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for turn in range(3):
+        for x, out, ws, nt, stream in jobs:
+            api.process_logits(x, out, ws, next_token=nt, stream=stream)
+        torch.cuda.synchronize()
+        for x, out, ws, nt, _ in jobs:
+            assert torch.equal(out, x) and torch.equal(nt.long(), x.argmax(1)) and not ws.any()
+            nt.fill_(-7)
+            out.zero_()
+        torch.cuda.synchronize()
+
+
 def test_logits_special_values():
     """Ties to the lower id (also -0 with +0), NaN never chosen, infinities as they come."""
     V = 5000
