@@ -114,12 +114,12 @@ typedef struct emoe_paged_attention_args {
   const int32_t* page_table;  /* device [n_seqs][table_width] */
   int64_t q_stride, out_stride; /* between rows, elements, multiples of 8 */
   int64_t table_stride;
-  float scale;                /* of the scores, e.g. 1 / sqrt(head_dim); finite */
+  float scale;                /* of the scores, e.g. 1 / sqrt(head_dim); within +-2e38 */
   int32_t dtype;              /* of q and out: EMOE_BF16 or EMOE_F16; a 16-bit cache has the same */
   int32_t rows;               /* >= 0 */
-  int32_t n_heads;            /* a multiple of n_kv_heads */
+  int32_t n_heads;            /* a multiple of n_kv_heads, at most 2^20 */
   int32_t n_seqs, table_width;
-  int32_t max_keys;           /* bound of lengths[], >= 0: how finely the call is split */
+  int32_t max_keys;           /* bound of lengths[], 0 .. 2^30: how finely the call is split */
   int32_t window;             /* >= 0 */
 } emoe_paged_attention_args;
 
@@ -193,7 +193,7 @@ typedef struct emoe_decoder_batch {
   int64_t table_stride;
   int32_t n_tokens, n_seqs, table_width;
   int32_t n_out;              /* 1 .. n_tokens */
-  int32_t max_keys;           /* bound of positions[] + 1 */
+  int32_t max_keys;           /* bound of positions[] + 1, 0 .. 2^30 */
 } emoe_decoder_batch;
 
 /* Workspace of emoe_decoder_forward_paged; needs no initial value, since the

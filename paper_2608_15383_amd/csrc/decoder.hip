@@ -985,7 +985,8 @@ int32_t emoe_decoder_forward(emoe_decoder* dec, const int32_t* tokens, int32_t T
 
 size_t emoe_decoder_paged_workspace_bytes(const emoe_decoder_dims* dims, int32_t n_tokens,
                                           int32_t n_out, int32_t max_keys) {
-  if (check_decoder_dims(dims) != EMOE_OK || n_tokens < 1 || n_out < 1 || n_out > n_tokens || max_keys < 0)
+  if (check_decoder_dims(dims) != EMOE_OK || n_tokens < 1 || n_out < 1 || n_out > n_tokens || max_keys < 0 ||
+      max_keys > 1 << 30)
     return 0;
   return paged_layout(*dims, n_tokens, n_out, max_keys).total;
 }
@@ -1001,7 +1002,7 @@ int32_t emoe_decoder_forward_paged(emoe_decoder* dec, const emoe_paged_kv* kv,
   const emoe_decoder_dims& D = dec->dims;
   const emoe_decoder_batch& B = *batch;
   const int T = B.n_tokens, n_out = B.n_out;
-  if (T < 1 || n_out < 1 || B.max_keys < 0)
+  if (T < 1 || n_out < 1 || B.max_keys < 0 || B.max_keys > 1 << 30)
     return report_error(EMOE_EINVAL, "n_tokens %d, n_out %d, max_keys %d", T, n_out, B.max_keys);
   if (B.out_rows ? n_out > T : n_out != T)
     return report_error(EMOE_EINVAL, "n_out %d of n_tokens %d: need at most as many, all without out_rows",

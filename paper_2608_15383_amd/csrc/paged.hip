@@ -29,7 +29,8 @@ struct AppendArg {
   const int32_t *positions, *seqs, *table;
   const double* inv_freq;
   int64_t q_stride, k_stride, v_stride, qo_stride, table_stride;
-  int32_t tokens, n_heads, n_seqs, table_width, rotary_dim;
+  int64_t token0;
+  int32_t n_heads, n_seqs, table_width, rotary_dim;
 };
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -52,7 +53,7 @@ template <class T, bool kE4M3, bool kInter, int kDh>
 __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArg a) {
   __shared__ float2 cs[kDh / 2];
   constexpr int kPieces = kDh / 16;
-  const int64_t t = blockIdx.x;
+  const int64_t t = a.token0 + blockIdx.x;
   const int p = a.positions[t], s = a.seqs ? a.seqs[t] : (int)t;
   if (p < 0 || (uint32_t)s >= (uint32_t)a.n_seqs) return;
   int64_t slot_at = -1;  // byte offset of the token's slot, -1: none
@@ -1025,6 +1026,10 @@ AttendPlan attend_plan(const emoe_paged_kv& kv, int32_t rows, int32_t n_heads, i
   return p;
 }
 
+// Bounds of the attention's integers: keys of a row and what a tile adds to them
+// stay within 32 bits, and lines times threads within a grid.
+constexpr int32_t kMostKeys = 1 << 30, kMostHeads = 1 << 20;
+
 }  // namespace
 
 extern "C" {
@@ -1070,7 +1075,6 @@ int32_t emoe_paged_append(const emoe_paged_kv* kv, const emoe_paged_append_args*
   a.v_stride = A.v_stride;
   a.qo_stride = A.q_out_stride;
   a.table_stride = A.table_stride;
-  a.tokens = A.tokens;
   a.n_heads = A.n_heads;
   a.n_seqs = A.n_seqs;
   a.table_width = A.table_width;
@@ -1078,24 +1082,30 @@ int32_t emoe_paged_append(const emoe_paged_kv* kv, const emoe_paged_append_args*
   const int64_t heads = (A.q ? A.n_heads : 0) + 2 * (int64_t)kv->n_kv_heads;
   const int64_t items = heads * (dh / 16);
   if (items >= (int64_t)1 << 31) return report_error(EMOE_ESHAPE, "%lld heads", (long long)heads);
-  const int64_t gx = A.tokens;
   int64_t gy = 1;  // small calls: up to an item per thread
-  while (gx * gy < 512 && gy * kThreads < items) ++gy;
-  const dim3 grid((unsigned)gx, (unsigned)gy);
+  while (A.tokens * gy < 512 && gy * kThreads < items) ++gy;
   const bool e4m3 = kv->dtype == EMOE_E4M3, inter = A.interleaved != 0;
-  if (A.dtype == EMOE_BF16) {
-    if (e4m3) launch_append<Bf16, true>(a, kv->head_dim, inter, grid, stream);
-    else launch_append<Bf16, false>(a, kv->head_dim, inter, grid, stream);
-  } else {
-    if (e4m3) launch_append<Fp16, true>(a, kv->head_dim, inter, grid, stream);
-    else launch_append<Fp16, false>(a, kv->head_dim, inter, grid, stream);
+  constexpr int64_t kTokens = 1 << 22;  // of one launch: a grid has fewer than 2^32 threads
+  for (a.token0 = 0; a.token0 < A.tokens; a.token0 += kTokens) {
+    const int64_t gx = A.tokens - a.token0 < kTokens ? A.tokens - a.token0 : kTokens;
+    const dim3 grid((unsigned)gx, (unsigned)gy);
+    if (A.dtype == EMOE_BF16) {
+      if (e4m3) launch_append<Bf16, true>(a, kv->head_dim, inter, grid, stream);
+      else launch_append<Bf16, false>(a, kv->head_dim, inter, grid, stream);
+    } else {
+      if (e4m3) launch_append<Fp16, true>(a, kv->head_dim, inter, grid, stream);
+      else launch_append<Fp16, false>(a, kv->head_dim, inter, grid, stream);
+    }
+    if ((st = launched("paged_append_kernel"))) return st;
   }
-  return launched("paged_append_kernel");
+  return EMOE_OK;
 }
 
 size_t emoe_paged_attention_workspace_bytes(const emoe_paged_kv* kv, int32_t rows, int32_t n_heads,
                                             int32_t max_keys) {
-  if (check_kv(kv) || rows < 0 || n_heads < 1 || n_heads % kv->n_kv_heads || max_keys < 0) return 0;
+  if (check_kv(kv) || rows < 0 || n_heads < 1 || n_heads % kv->n_kv_heads || max_keys < 0 ||
+      max_keys > kMostKeys || n_heads > kMostHeads)
+    return 0;
   const AttendPlan p = attend_plan(*kv, rows, n_heads, max_keys, 0);
   return EMOE_SERVING_TICKET_BYTES + (size_t)2 * p.most_parts * p.part_floats * 4;
 }
@@ -1113,7 +1123,11 @@ int32_t emoe_paged_attention(const emoe_paged_kv* kv, const emoe_paged_attention
   if (A.n_heads < 1 || A.n_heads % kv->n_kv_heads)
     return report_error(EMOE_ESHAPE, "n_heads %d is no multiple of n_kv_heads %d", A.n_heads,
                         kv->n_kv_heads);
-  if (!std::isfinite(A.scale)) return report_error(EMOE_EINVAL, "scale is not finite");
+  if (A.max_keys > kMostKeys || A.n_heads > kMostHeads)
+    return report_error(EMOE_ESHAPE, "max_keys %d or n_heads %d: need at most 2^30 and 2^20", A.max_keys,
+                        A.n_heads);
+  if (!std::isfinite(A.scale * 1.4426950408889634f))  // as the kernel takes it
+    return report_error(EMOE_EINVAL, "scale %g is not finite, or near the largest number", A.scale);
   if (A.rows == 0) return EMOE_OK;
   const int64_t qw = (int64_t)A.n_heads * kv->head_dim;
   if ((st = check_rows("q", A.q, A.q_stride, A.rows, qw))) return st;

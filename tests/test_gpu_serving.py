@@ -241,6 +241,27 @@ def test_append_ties_to_even_in_8_bits():
     assert f64(c.v.float())[0, 0, 0, :len(x)].tolist() == want
 
 
+def test_append_more_tokens_than_one_launch():
+    """All but a few of 2^24 + 5 tokens are padding; the others are what a call of them alone gives."""
+    n, d = (1 << 24) + 5, 64
+    at = torch.tensor([0, (1 << 22) - 1, 1 << 22, n - 1], device="cuda:0")
+    k = torch.empty(n, 1, d, device="cuda:0", dtype=torch.bfloat16)
+    v = torch.empty_like(k)
+    k[at], v[at] = (torch.randn(4, 1, d, device="cuda:0").to(k.dtype) for _ in "kv")
+    seqs = torch.full((n,), -1, dtype=torch.int32, device="cuda:0")
+    positions = torch.zeros_like(seqs)
+    seqs[at] = 0
+    positions[at] = ids([3, 4, 5, 7])
+    caches = []
+    for pick in (slice(None), at):
+        pages = torch.zeros(2, 1, 8, 1, d, device="cuda:0", dtype=k.dtype)
+        api.paged_append(api.PagedKV(pages[0], pages[1]), None, k[pick], v[pick], positions[pick],
+                         ids([[0]]), api.rope_frequencies(d), seqs=seqs[pick])
+        caches.append(pages)
+    assert torch.equal(*caches)
+    assert all(bool(caches[0][:, 0, slot].any()) == (slot in (3, 4, 5, 7)) for slot in range(8))
+
+
 def test_append_nothing():
     c = Cache("bf16", 1, 8, 1, 64, 2)
     e = torch.empty(0, 1, 64, device="cuda:0", dtype=torch.bfloat16)

@@ -124,6 +124,10 @@ def test_append_checks(change, want):
     (dict(n_heads=6), EMOE_ESHAPE),
     (dict(scale=float("nan")), EMOE_EINVAL),
     (dict(scale=float("inf")), EMOE_EINVAL),
+    (dict(scale=-3e38), EMOE_EINVAL),                   # infinite once it is one of powers of two
+    (dict(max_keys=(1 << 30) + 1), EMOE_ESHAPE),
+    (dict(max_keys=2 ** 31 - 1), EMOE_ESHAPE),
+    (dict(n_heads=1 << 21, q_stride=1 << 28, out_stride=1 << 28), EMOE_ESHAPE),
     (dict(dtype=EMOE_F16), EMOE_EINVAL),
     (dict(dtype=EMOE_F32), EMOE_EINVAL),
     (dict(q=None), EMOE_EINVAL),
@@ -146,7 +150,7 @@ def test_attention_needs_its_workspace():
     args = (C.byref(kv()), C.byref(attention()))
     assert status("emoe_paged_attention", *args, None, need, None) == EMOE_EINVAL
     assert status("emoe_paged_attention", *args, P, need - 1, None) == EMOE_EINVAL
-    for bad in ((-1, 16, 9), (1, 0, 9), (1, 6, 9), (1, 16, -1)):
+    for bad in ((-1, 16, 9), (1, 0, 9), (1, 6, 9), (1, 16, -1), (1, 16, 2 ** 31 - 1), (1, 1 << 21, 9)):
         assert _lib.lib().emoe_paged_attention_workspace_bytes(C.byref(kv()), *bad) == 0
 
 
