@@ -223,7 +223,11 @@ PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     A.n_seqs = i32(table.size(0), "sequences");
     A.table_width = i32(table.size(1), "page_table");
     A.rotary_dim = freq ? i32(2 * freq->size(0), "inv_freq") : 0;
-    A.interleaved = PyObject_IsTrue(a[10]) ? 1 : 0;
+    A.interleaved = PyObject_IsTrue(a[10]);
+    if (A.interleaved < 0) {
+      PyErr_Clear();
+      refuse("interleaved: need True or False");
+    }
     return on_device(kv.device, g_append, kv.view, &A, stream_of(a[11]));
   });
 }

@@ -789,7 +789,8 @@ def test_binding_checks_tensors():
     ok = dict(kv=c.kv, q=q, k=k, v=k, positions=p, page_table=t, inv_freq=api.rope_frequencies(64))
     api.paged_append(**ok)
     for change in (dict(k=k.half()), dict(v=k[:1]), dict(v=k[:, :1]), dict(positions=p.float()),
-                   dict(inv_freq=torch.zeros(32, device="cuda:0")), dict(q_out=q.float())):
+                   dict(inv_freq=torch.zeros(32, device="cuda:0")), dict(q_out=q.float()),
+                   dict(interleaved=np.zeros(2))):
         with pytest.raises(ExactMoEError):
             api.paged_append(**{**ok, **change})
     x = torch.zeros(2, 100, device="cuda:0")
