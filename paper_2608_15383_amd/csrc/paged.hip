@@ -257,8 +257,6 @@ struct Tile {
   static constexpr int kPairs = kDh / (8 * kChunkDims);    // loads of an octet
   static constexpr int kDims = kDh / 16;                   // output dimensions of a lane
   static constexpr int kVWords = kDims * kItem / 4;
-  // Tiles of all lines that memory (6 TB/s) takes in the time of one wavefront's tile.
-  static constexpr int kBusyTiles = 640 * 512 / (2 * kDh * kItem);
   static constexpr bool kSplitV = !kE4M3 && kDh == 256;    // two 16-byte loads, 256 bytes apart
 
   uint32_t k[4][kPairs][kChunkWords];
@@ -414,13 +412,14 @@ __device__ __forceinline__ int wave_scan(int v) {
 // wherever rows begin and end: best where a worker has many.  Or a row has at
 // most ceil(units / target) slots and every worker one, so that its run never
 // spans two rows, which costs a run about four units more.
-// To join a shared row costs 3 to 8 us, a unit of a worker's own 1.4 us, and no
-// cut makes the launch faster than memory: rows stay whole unless the longest
-// gives up kPays units or more over what a part, or memory, still takes.  Whole
-// against cut, 128 dimensions, 8 key heads of 16 bits: 4 rows of 1,024 keys
-// 19.0 and 12.2 us, 16 of 512 13.4 and 15.3, 16 of 2,048 33.8 and 31.1, 32 of
-// 1,024 26.5 and 31.1, 32 of 2,048 47.1 and 53.8.
-constexpr int kPays = 4, kSlackUnits = 6;
+// To join a shared row costs 3 to 8 us, a unit of a worker's own about 1.4 us per
+// 64 KB (what a CU keeps in flight; smaller units 1 us): rows stay whole unless
+// the longest gives up pays_units or more.  Whole against cut, 8 key heads, 16
+// bits: 4 rows of 1,024 keys of 128 dimensions 19.0 and 11.1 us, 16 of 512 13.4
+// and 15.3, 4 of 1,024 of 64 dimensions 14.0 and 9.7; 4 key heads of 256
+// dimensions, 16 rows of 512 17.8 and 14.2, of 2,048 54.0 and 28.4.
+constexpr int kSlackUnits = 6;
+constexpr int pays_units(int unit_bytes) { return unit_bytes > 65536 ? 2 : 4; }
 __device__ __forceinline__ int slot_units(int units, int target) {
   if (target == 0) return 1;
   const uint32_t parts = (uint32_t)(units + target - 1) / (uint32_t)target;
@@ -432,19 +431,25 @@ __device__ __forceinline__ int slots_of(int units, int target) {
   return (int)((uint32_t)(units + each - 1) / (uint32_t)each);
 }
 
-// Split over the caches' lengths (Cut); a worker's four wavefronts take every
-// fourth tile of its units.  Outputs that it covers whole it writes; of the
-// others (at most its first and its last) it leaves maximum, sum and unscaled
+// Split over the caches' lengths, as above; a worker's kWaves wavefronts take
+// every kWaves-th tile of its units.  Outputs that it covers whole it writes; of
+// the others (at most its first and its last) it leaves maximum, sum and unscaled
 // output in the workspace, and the last of such an output's workers to finish
-// joins them in the rows' order.  Key heads (times tiles of 16 query heads) are
-// the lines: workgroups next to each other take the same keys of different
-// heads, which lie next to each other in memory.  Bound by HBM: per tile and
-// wavefront 16 KB (16-bit, 128 dimensions) against about 250 vector and 24
-// matrix instructions.
+// joins them in the rows' order (nobody waits).  Key heads (times tiles of 16
+// query heads) are the lines: workgroups next to each other take the same keys of
+// different heads, which lie next to each other in memory.
+// Bound by HBM where there are keys enough: per tile and wavefront 16 KB (16
+// bits, 128 dimensions) against about 250 vector and 24 matrix instructions.
+// 131,072 keys of 8 heads of 128 take 91 us, 5.9 TB/s, of the 6.0 that this
+// pattern of reads reaches without any arithmetic; 128 rows over 8 bits 277 us,
+// 5.2 TB/s (ragged rows; heads of one 128-byte line each).  Short calls are
+// bound by the chain of trips to memory (lengths, page table, keys, parts,
+// ticket, parts again): 302 keys take 9 us.
 template <class T, bool kE4M3, int kDh, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attention_kernel(AttendArg a) {
   constexpr int kThreads = 64 * kWaves;
   typedef Tile<T, kE4M3, kDh> Tl;
+  constexpr int kPays = pays_units(kWaves * kTileKeys * 2 * kDh * Tl::kItem);
   constexpr int kRow = kDh + 4;  // padded: lanes 16 apart in dimensions, 1 in queries
   __shared__ int pre[kMaxRows + 1], len[kMaxRows], seq[kMaxRows];
   __shared__ int wave_sum[kWaves], wave_most[kWaves];
@@ -512,12 +517,11 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
   }
   most = __builtin_amdgcn_readfirstlane(most);
   int run = (total + a.workers - 1) / a.workers, target = 0, all = total;
-  if (a.rows < a.workers) {
+  if (a.rows <= a.workers) {
     // The smallest target tried for which the workers suffice; they do for the
     // last one, since the sum of ceil(units / target) <= total / target + rows.
-    const int spare = a.workers - a.rows, enough = (total + spare - 1) / spare;
-    const int busy = (int)min((int64_t)INT32_MAX, (int64_t)total * Y / (Tl::kBusyTiles / kWaves) + 1);
-    int t = most - max(run, busy) < kPays ? most : run;
+    const int spare = a.workers - a.rows, enough = spare ? min(most, (total + spare - 1) / spare) : most;
+    int t = most - run < kPays ? most : run;
     while (true) {
       int mine = 0;
 #pragma unroll
@@ -984,13 +988,8 @@ void launch_attend(const AttendArg& a, int head_dim, int waves, hipStream_t stre
   if (head_dim == 256) {
     ATTEND_CASE(256, 4);
   } else if (head_dim == 128) {
-    if constexpr (kE4M3) {
-      if (waves == 8) {
-        ATTEND_CASE(128, 8);
-        return;
-      }
-    }
-    ATTEND_CASE(128, 4);
+    if (waves == 8) ATTEND_CASE(128, 8);
+    else ATTEND_CASE(128, 4);
   } else {
     if (waves == 8) ATTEND_CASE(64, 8);
     else ATTEND_CASE(64, 4);
@@ -1001,28 +1000,45 @@ void launch_attend(const AttendArg& a, int head_dim, int waves, hipStream_t stre
 // How a call is launched: rows per launch (their units stay below 2^31), the
 // workers of each line and the lines (key heads times tiles of 16 queries),
 // and the floats of one workgroup's record for a split output.
+// The device holds 512 workgroups of four wavefronts, two to a CU, or 256 of eight
+// (or of four at 256 dimensions: 65,536 keys of 4 heads 55 us, with 512 workers
+// 67).  Eight join twice the keys in LDS that four do, which pays in two cases:
+//  - with four, an output's parts would come to more than kWideJoin bytes, which
+//    one workgroup reads: 131,072 keys of 8 heads 94 against 91 us, 8,192 keys
+//    16.3 and 14.2, 4 rows of 4,000 keys of 4 heads with 8 queries each 17.4 and
+//    13.9; below it 4 rows of 3,000 keys 17.1 and 17.6;
+//  - there is a workgroup for every output, and what the idle ones could take
+//    off the longest row comes to less than two units: 47 windows of 1,024 keys
+//    14.5 and 12.7 us, 302 keys 9.6 and 9.0; above it 16 rows of up to 1,024 keys
+//    12.9 and 17.
 struct AttendPlan {
   int64_t rows_per_launch;
   int waves, workers, lines, part_floats;
   int64_t most_parts;  // workgroups of any plan with these rows, heads and max_keys
 };
+constexpr int kPlaces = 512, kWideJoin = 96 << 10;
 AttendPlan attend_plan(const emoe_paged_kv& kv, int32_t rows, int32_t n_heads, int32_t max_keys,
                        int32_t window) {
   const int group = n_heads / kv.n_kv_heads;
   const int64_t keys = window > 0 && window < max_keys ? window : max_keys;
-  const int row_bytes = kv.head_dim * (kv.dtype == EMOE_E4M3 ? 1 : 2);
   AttendPlan p;
   p.lines = kv.n_kv_heads * ((group + 15) / 16);
-  p.waves = row_bytes <= 128 && keys > 256 && (int64_t)rows * p.lines <= 512 ? 8 : 4;
+  const int record = 4 * (group < 16 ? group : 16) * kv.head_dim;
+  const int64_t outputs = (int64_t)rows * p.lines, four = 4 * kTileKeys, eight = 8 * kTileKeys;
+  int64_t parts = outputs > 0 ? kPlaces / outputs : 0;
+  if (parts > (keys + four - 1) / four) parts = (keys + four - 1) / four;
+  const int64_t idle = kPlaces / 2 - outputs;
+  const bool whole = idle >= 0 && (keys + eight - 1) / eight * idle < kPlaces;
+  p.waves = kv.head_dim < 256 && (whole || parts * record > kWideJoin) ? 8 : 4;
   const int64_t most = keys / (kTileKeys * p.waves) + 2;  // units of one row
   p.rows_per_launch = (((int64_t)1 << 31) - 1 - kTickets) / most;
   if (p.rows_per_launch > kMaxRows) p.rows_per_launch = kMaxRows;
   const int64_t held = rows < p.rows_per_launch ? rows : p.rows_per_launch;
-  int64_t workers = (kv.head_dim == 256 ? 256 : 512) / p.lines;
+  int64_t workers = (kv.head_dim == 256 || p.waves == 8 ? kPlaces / 2 : kPlaces) / p.lines;
   if (workers < 1) workers = 1;
   p.workers = (int)(held * most < workers ? held * most : workers);
   p.part_floats = 32 + (group < 16 ? group : 16) * kv.head_dim;
-  p.most_parts = p.lines > 512 ? p.lines : 512;
+  p.most_parts = p.lines > kPlaces ? p.lines : kPlaces;
   return p;
 }
 
