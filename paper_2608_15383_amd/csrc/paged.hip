@@ -417,8 +417,10 @@ __device__ __forceinline__ int wave_scan(int v) {
 // the longest gives up pays_units or more.  Whole against cut, 8 key heads, 16
 // bits: 4 rows of 1,024 keys of 128 dimensions 19.0 and 11.1 us, 16 of 512 13.4
 // and 15.3, 4 of 1,024 of 64 dimensions 14.0 and 9.7; 4 key heads of 256
-// dimensions, 16 rows of 512 17.8 and 14.2, of 2,048 54.0 and 28.4.
-constexpr int kSlackUnits = 6;
+// dimensions, 16 rows of 512 17.8 and 14.2, of 2,048 54.0 and 28.4.  A target of
+// more than slack_units above the equal runs' gives way to those: 32 rows of up to
+// 2,000 keys, eight wavefronts, 31.4 us with a slack of 6 and 27.0 with 1.
+constexpr int slack_units(int waves) { return waves == 8 ? 1 : 6; }
 constexpr int pays_units(int unit_bytes) { return unit_bytes > 65536 ? 2 : 4; }
 __device__ __forceinline__ int slot_units(int units, int target) {
   if (target == 0) return 1;
@@ -527,7 +529,7 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
 #pragma unroll
       for (int i = 0; i < kPer; ++i) mine += i < per ? slots_of(units_[i], t) : 0;
       const int sum = sum_rows(mine, before);
-      if (t < most && t > run + kSlackUnits) break;  // equal runs, then
+      if (t < most && t > run + slack_units(kWaves)) break;  // equal runs, then
       if (sum <= a.workers || t >= enough) {
         target = t;
         all = sum;
@@ -1009,8 +1011,8 @@ void launch_attend(const AttendArg& a, int head_dim, int waves, hipStream_t stre
 //    13.9; below it 4 rows of 3,000 keys 17.1 and 17.6;
 //  - there is a workgroup for every output, and what the idle ones could take
 //    off the longest row comes to less than two units: 47 windows of 1,024 keys
-//    14.5 and 12.7 us, 302 keys 9.6 and 9.0; above it 16 rows of up to 1,024 keys
-//    12.9 and 17.
+//    14.5 and 12.7 us, 302 keys 9.6 and 9.0, 32 rows of 2,000 keys 50 and 45.7 (of
+//    up to 2,000 25.4 and 27.0); above it 16 rows of up to 1,024 keys 12.9 and 17.
 struct AttendPlan {
   int64_t rows_per_launch;
   int waves, workers, lines, part_floats;
