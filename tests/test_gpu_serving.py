@@ -14,6 +14,7 @@ operation; half(t) = finfo(t).eps / 2, that of storing a 16-bit value):
   logits      at most six operations, each u of its intermediate values, the store.
 """
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -346,6 +347,10 @@ def test_attention_head_layouts(heads, hk, cache_kind):
     run_attention("bf16", cache_kind, [1, 70, 300, 0, 513], heads, hk, 128, 16, seed=heads)
 
 
+def test_attention_of_more_lines_than_workgroups():
+    run_attention("bf16", "bf16", [33, 0, 70], 1200, 600, 64, 8, seed=1)
+
+
 @pytest.mark.parametrize("lengths,heads,hk,d,page", [
     ([5000], 8, 2, 128, 16), ([4096, 1, 4097], 4, 4, 64, 64), ([20011], 4, 1, 256, 128),
     ([9000, 40, 7, 1200], 12, 2, 128, 8), ([1] * 40 + [3000], 4, 4, 64, 16),
@@ -648,6 +653,23 @@ def test_logits_of_two_streams_at_once():
         torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("rows,vocab", [(1, 1 << 30), (5, (1 << 29) + 1)])
+def test_logits_offsets_past_32_bits(rows, vocab):
+    x = torch.zeros(rows, vocab, device="cuda:0", dtype=torch.bfloat16)
+    at = [(vocab - 1 - 12345 * r) % vocab for r in range(rows)]
+    for r, v in enumerate(at):
+        x[r, v] = 2.0 + r
+    h = ids([[v, v // 2] for v in at])
+    nt = torch.empty(rows, dtype=torch.int32, device="cuda:0")
+    ws = torch.zeros(api.process_logits_workspace_bytes(rows, vocab), dtype=torch.uint8, device="cuda:0")
+    two, quarter = (torch.full((rows,), s, device="cuda:0") for s in (2.0, 0.25))
+    api.process_logits(x, workspace=ws, next_token=nt, history=h, repetition=two, presence=quarter)
+    assert nt.tolist() == at and not ws.any()
+    for r, v in enumerate(at):
+        assert float(x[r, v]) == (2 + r) / 2 - 0.25 and float(x[r, v // 2]) == -0.25
+    assert sum(int(x[r].count_nonzero()) for r in range(rows)) == 2 * rows
+
+
 def test_logits_special_values():
     """Ties to the lower id (also -0 with +0), NaN never chosen, infinities as they come."""
     V = 5000
@@ -784,6 +806,27 @@ def test_two_streams_with_their_own_workspaces():
         torch.cuda.synchronize()
         for s, w in zip(steps, want):
             assert torch.equal(s.out, w[0])
+
+
+def test_two_threads_call_at_once():
+    """Each with tensors, workspaces and a stream of its own."""
+    steps = [Step(7 + i) for i in range(4)]
+    want = [[t.clone() for t in s.all()] for s in steps]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in steps]
+
+    def work(i):
+        for _ in range(50):
+            steps[i].run(stream=streams[i])
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for s, w in zip(steps, want):
+        assert torch.equal(s.out, w[0])
 
 
 def test_binding_checks_tensors():
