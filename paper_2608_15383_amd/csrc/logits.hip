@@ -7,7 +7,7 @@ using namespace emoe;
 namespace {
 
 constexpr int kMaxRows = 4096;  // rows of one launch
-constexpr int kLongHistory = 4096;
+constexpr int kLongHistory = 6144;
 constexpr uint32_t kBiasIndices = 1u << 23;  // bits of the smallest normal number
 
 struct LogitsArg {
@@ -423,11 +423,18 @@ __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
 }
 
 // How a call is cut: threads and 16-byte loads of a workgroup.
+// Four loads (a chunk of 16 KB), one where that would leave fewer than 512
+// workgroups: 16 rows of 50,304 f32 logits 6.5 us with one and 8.1 with four, 64
+// rows 11.3 and 10.0.  Two for 16-bit logits with biases, whose words of LDS keep
+// all but three workgroups of four loads out of a CU: 90 rows of 68,149 11.0 and
+// 15.7.  From kLongHistory ids on 1,024 threads count: 19 rows of 50,304 and 8,000
+// ids 9.5 us and 10.6 with 256, 64 rows and 12,000 16.1 and 18.4; 132 rows of 64,066
+// and 4,756 ids 26.0 and 20.2, 64 rows and 6,000 14.5 and 14.1.
 struct LogitsPlan {
   int threads, loads, chunks;
 };
-LogitsPlan logits_plan(int32_t rows, int32_t vocab, int per, int32_t history_width) {
-  LogitsPlan p{256, 4, 0};
+LogitsPlan logits_plan(int32_t rows, int32_t vocab, int per, int32_t history_width, bool biases) {
+  LogitsPlan p{256, biases && per == 8 ? 2 : 4, 0};
   auto chunks = [&] {
     const int64_t c = (int64_t)p.threads * per * p.loads;
     return (int)((vocab + c - 1) / c);
@@ -442,10 +449,10 @@ LogitsPlan logits_plan(int32_t rows, int32_t vocab, int per, int32_t history_wid
   return p;
 }
 
-template <class F, int kThreads, int kLoads>
+template <class F, int kThreads, int kLoads, int kBiasLoads = kLoads>
 void launch_logits(const LogitsArg& a, unsigned blocks, hipStream_t stream) {
   if (a.bias_ids)
-    hipLaunchKernelGGL((process_logits_kernel<F, kThreads, kLoads, true>), dim3(blocks), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((process_logits_kernel<F, kThreads, kBiasLoads, true>), dim3(blocks), dim3(kThreads), 0, stream, a);
   else
     hipLaunchKernelGGL((process_logits_kernel<F, kThreads, kLoads, false>), dim3(blocks), dim3(kThreads), 0, stream, a);
 }
@@ -454,7 +461,7 @@ template <class F>
 void launch_type(const LogitsArg& a, const LogitsPlan& p, unsigned blocks, hipStream_t stream) {
   if (p.threads == 1024) launch_logits<F, 1024, 8 / F::kPer>(a, blocks, stream);
   else if (p.loads == 1) launch_logits<F, 256, 1>(a, blocks, stream);
-  else launch_logits<F, 256, 4>(a, blocks, stream);
+  else launch_logits<F, 256, 4, F::kPer == 8 ? 2 : 4>(a, blocks, stream);
 }
 
 }  // namespace
@@ -521,7 +528,7 @@ int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_
   const int32_t st = check_process_logits(A, workspace, workspace_bytes);
   if (st || A.rows == 0) return st;
   const int per = A.dtype == EMOE_F32 ? 4 : 8;
-  const LogitsPlan plan = logits_plan(A.rows, A.vocab, per, A.history ? A.history_width : 0);
+  const LogitsPlan plan = logits_plan(A.rows, A.vocab, per, A.history ? A.history_width : 0, A.bias_ids && A.bias_width > 0);
   LogitsArg a;
   a.logits = A.logits;
   a.out = A.out;
