@@ -453,120 +453,138 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
   typedef Tile<T, kE4M3, kDh> Tl;
   constexpr int kPays = pays_units(kWaves * kTileKeys * 2 * kDh * Tl::kItem);
   constexpr int kRow = kDh + 4;  // padded: lanes 16 apart in dimensions, 1 in queries
-  __shared__ int pre[kMaxRows + 1], len[kMaxRows], seq[kMaxRows];
+  constexpr bool kWhole = kWaves == 1;  // a row to a workgroup, nothing shared
+  constexpr int kRows = kWhole ? 1 : kMaxRows, kJoiners = kWhole ? 1 : kThreads;
+  __shared__ int pre[kRows + 1], len[kRows], seq[kRows];
   __shared__ int wave_sum[kWaves], wave_most[kWaves];
   __shared__ float ms[kWaves][16], ls[kWaves][16];
   __shared__ __attribute__((aligned(16))) float os[kWaves][16][kRow];
-  __shared__ float4 striped[kThreads];
-  __shared__ float striped_m[kThreads], striped_l[kThreads];
+  __shared__ float4 striped[kJoiners];
+  __shared__ float striped_m[kJoiners], striped_l[kJoiners];
   __shared__ int last[2], first_row;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
   const uint32_t k_off = Tl::k_offset(lane, a.kv.slot_bytes);
   const uint32_t v_off = Tl::v_offset(lane, a.kv.slot_bytes);
 
-  // How the rows are cut, and where this worker's run of slots begins.  Up to
-  // 64 rows every wavefront finds out by itself, a row per lane, and keeps them
-  // in its lanes; more rows take the workgroup and LDS.
-  const int Y = a.kv.n_kv_heads * a.q_tiles;
-  const int w = blockIdx.x / Y, y = blockIdx.x % Y;
+  // Workgroups of one key head's tiles of queries are 8 apart, on one die, so that
+  // its L2 serves what the second reads again (21 rows of up to 11,854 keys, 24
+  // queries to a key head: 40.5 -> 33 us).
+  const int chunk = blockIdx.x / (8 * a.q_tiles), at = blockIdx.x % (8 * a.q_tiles);
+  const int pairs = min(8, a.workers * a.kv.n_kv_heads - 8 * chunk);
+  const int pair = 8 * chunk + at % pairs, qt = at / pairs;
+  const int w = pair / a.kv.n_kv_heads, hk = pair % a.kv.n_kv_heads;
+  const int Y = a.kv.n_kv_heads * a.q_tiles, y = hk * a.q_tiles + qt;
   const bool few = a.rows <= 64;
-  const int per = few ? 1 : (a.rows + kThreads - 1) / kThreads, r0 = few ? lane : tid * per;
-  constexpr int kPer = kMaxRows / kThreads;
-  int units_[kPer], n_lane = 0, seq_lane = 0, total = 0, most = 0;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    units_[i] = 0;
-    if (i < per && r0 + i < a.rows) {
-      const Span s = span_of(a, a.row0 + r0 + i);
-      if (few) {
-        n_lane = s.n;
-        seq_lane = s.seq;
-      } else {
-        len[r0 + i] = s.n;
-        seq[r0 + i] = s.seq;
-      }
-      units_[i] = units_of<kWaves>(s.first, s.n);
-    }
-    total += units_[i];
-    most = max(most, units_[i]);
-  }
-  // Sums over the rows; `before` is what the rows before this thread's have.
-  auto sum_rows = [&](int v, int& before) -> int {
-    const int incl = wave_scan(v);
-    before = incl - v;
-    const int all = __builtin_amdgcn_readlane(incl, 63);
-    if (few) return all;
-    __syncthreads();
-    if (lane == 0) wave_sum[wave] = all;
-    __syncthreads();
-    int sum = 0;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-      before += i < wave ? wave_sum[i] : 0;
-      sum += wave_sum[i];
-    }
-    return __builtin_amdgcn_readfirstlane(sum);
-  };
-  int before;
-  total = sum_rows(total, before);
-  most = (int)wave_reduce_u32<true>((uint32_t)most);
-  if (!few) {
-    if (lane == 0) wave_most[wave] = most;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) most = max(most, wave_most[i]);
-  }
-  most = __builtin_amdgcn_readfirstlane(most);
-  int run = (total + a.workers - 1) / a.workers, target = 0, all = total;
-  if (a.rows <= a.workers) {
-    // The smallest target tried for which the workers suffice; they do for the
-    // last one, since the sum of ceil(units / target) <= total / target + rows.
-    const int spare = a.workers - a.rows, enough = spare ? min(most, (total + spare - 1) / spare) : most;
-    int t = most - run < kPays ? most : run;
-    while (true) {
-      int mine = 0;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) mine += i < per ? slots_of(units_[i], t) : 0;
-      const int sum = sum_rows(mine, before);
-      if (t < most && t > run + slack_units(kWaves)) break;  // equal runs, then
-      if (sum <= a.workers || t >= enough) {
-        target = t;
-        all = sum;
-        run = (sum + a.workers - 1) / a.workers;
-        break;
-      }
-      t = min(t + max(1, t / 4), max(enough, t + 1));
-    }
-  }
-  if (target == 0) {
-    int mine = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) mine += units_[i];
-    all = sum_rows(mine, before);
-  }
-  if ((int64_t)w * run >= all) return;  // the same for the whole workgroup
-  const int u_end = min((w + 1) * run, all);
-  int u = w * run, row = 0;
-  const int before_lane = before, slots_lane = slots_of(units_[0], target);
-  if (few) {
-    row = (int)__builtin_ctzll(__ballot(u >= before && u < before + slots_lane));
-  } else {
-#pragma unroll
+  int n_lane = 0, seq_lane = 0, before_lane = 0, slots_lane = 1;
+  int run = 1, target = kWhole ? INT32_MAX / 2 : 0, u = 0, u_end = 1, row = kWhole ? w : 0;
+  if constexpr (!kWhole) {
+    // How the rows are cut, and where this worker's run of slots begins.  Up to
+    // 64 rows every wavefront finds out by itself, a row per lane, and keeps them
+    // in its lanes; more rows take the workgroup and LDS.
+    const int per = few ? 1 : (a.rows + kThreads - 1) / kThreads, r0 = few ? lane : tid * per;
+    constexpr int kPer = kMaxRows / kThreads;
+    int units_[kPer], total = 0, most = 0;
+  #pragma unroll
     for (int i = 0; i < kPer; ++i) {
+      units_[i] = 0;
       if (i < per && r0 + i < a.rows) {
-        const int n = slots_of(units_[i], target);
-        pre[r0 + i] = before;
-        if (u >= before && u < before + n) first_row = r0 + i;
-        before += n;
+        const Span s = span_of(a, a.row0 + r0 + i);
+        if (few) {
+          n_lane = s.n;
+          seq_lane = s.seq;
+        } else {
+          len[r0 + i] = s.n;
+          seq[r0 + i] = s.seq;
+        }
+        units_[i] = units_of<kWaves>(s.first, s.n);
+      }
+      total += units_[i];
+      most = max(most, units_[i]);
+    }
+    // Sums over the rows; `before` is what the rows before this thread's have.
+    auto sum_rows = [&](int v, int& before) -> int {
+      const int incl = wave_scan(v);
+      before = incl - v;
+      const int all = __builtin_amdgcn_readlane(incl, 63);
+      if (few) return all;
+      __syncthreads();
+      if (lane == 0) wave_sum[wave] = all;
+      __syncthreads();
+      int sum = 0;
+  #pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        before += i < wave ? wave_sum[i] : 0;
+        sum += wave_sum[i];
+      }
+      return __builtin_amdgcn_readfirstlane(sum);
+    };
+    int before;
+    total = sum_rows(total, before);
+    most = (int)wave_reduce_u32<true>((uint32_t)most);
+    if (!few) {
+      if (lane == 0) wave_most[wave] = most;
+      __syncthreads();
+  #pragma unroll
+      for (int i = 0; i < kWaves; ++i) most = max(most, wave_most[i]);
+    }
+    most = __builtin_amdgcn_readfirstlane(most);
+    int all = total;
+    run = (total + a.workers - 1) / a.workers;
+    if (a.rows <= a.workers) {
+      // The smallest target tried for which the workers suffice; they do for the
+      // last one, since the sum of ceil(units / target) <= total / target + rows.
+      const int spare = a.workers - a.rows, enough = spare ? min(most, (total + spare - 1) / spare) : most;
+      int t = most - run < kPays ? most : run;
+      while (true) {
+        int mine = 0;
+  #pragma unroll
+        for (int i = 0; i < kPer; ++i) mine += i < per ? slots_of(units_[i], t) : 0;
+        const int sum = sum_rows(mine, before);
+        if (t < most && t > run + slack_units(kWaves)) break;  // equal runs, then
+        if (sum <= a.workers || t >= enough) {
+          target = t;
+          all = sum;
+          run = (sum + a.workers - 1) / a.workers;
+          break;
+        }
+        t = min(t + max(1, t / 4), max(enough, t + 1));
       }
     }
-    if (tid == 0) pre[a.rows] = all;
-    __syncthreads();
-    row = first_row;
+    if (target == 0) {
+      int mine = 0;
+  #pragma unroll
+      for (int i = 0; i < kPer; ++i) mine += units_[i];
+      all = sum_rows(mine, before);
+    }
+    if ((int64_t)w * run >= all) return;  // the same for the whole workgroup
+    u_end = min((w + 1) * run, all);
+    u = w * run;
+    before_lane = before;
+    slots_lane = slots_of(units_[0], target);
+    if (few) {
+      row = (int)__builtin_ctzll(__ballot(u >= before && u < before + slots_lane));
+    } else {
+  #pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        if (i < per && r0 + i < a.rows) {
+          const int n = slots_of(units_[i], target);
+          pre[r0 + i] = before;
+          if (u >= before && u < before + n) first_row = r0 + i;
+          before += n;
+        }
+      }
+      if (tid == 0) pre[a.rows] = all;
+      __syncthreads();
+      row = first_row;
+    }
   }
   // A row's first slot and slots.
   auto slots_at = [&](int r, int& base) -> int {
+    if constexpr (kWhole) {
+      base = 0;
+      return 1;
+    }
     if (few) {
       base = __builtin_amdgcn_readlane(before_lane, r);
       return __builtin_amdgcn_readlane(slots_lane, r);
@@ -576,7 +594,6 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
   };
   bool first_segment = true;
   int waiting = 0, shared0 = 0, shared1 = 0;  // this run's outputs that other workers share
-  const int hk = y / a.q_tiles, qt = y % a.q_tiles;
   const int head0 = hk * a.group + qt * 16;
   const int heads = min(16, a.group - qt * 16);
   float scale = a.scale * 1.4426950408889634f;
@@ -596,8 +613,15 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
     row = __builtin_amdgcn_readfirstlane(row);
     int base;
     const int row_slots = slots_at(row, base);
-    const int n = few ? __builtin_amdgcn_readlane(n_lane, row) : __builtin_amdgcn_readfirstlane(len[row]);
-    const int sq = few ? __builtin_amdgcn_readlane(seq_lane, row) : __builtin_amdgcn_readfirstlane(seq[row]);
+    int n, sq;
+    if constexpr (kWhole) {
+      const Span s = span_of(a, a.row0 + row);
+      n = __builtin_amdgcn_readfirstlane(s.n);
+      sq = __builtin_amdgcn_readfirstlane(s.seq);
+    } else {
+      n = few ? __builtin_amdgcn_readlane(n_lane, row) : __builtin_amdgcn_readfirstlane(len[row]);
+      sq = few ? __builtin_amdgcn_readlane(seq_lane, row) : __builtin_amdgcn_readfirstlane(seq[row]);
+    }
     const int first = a.window > 0 ? max(0, n - a.window) : 0;
     const int units = units_of<kWaves>(first, n), each = slot_units(units, target);
     const int s0 = u - base, s1 = min(row_slots, s0 + (u_end - u));
@@ -749,7 +773,7 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
       for (int i = 0; i < kWaves; ++i)
         L += ls[i][h] * part_weight(ms[i][h], M);
     };
-    float* part = a.parts + (int64_t)(2 * blockIdx.x + (first_segment ? 0 : 1)) * a.part_floats;
+    float* part = a.parts + (int64_t)(2 * (w * Y + y) + (first_segment ? 0 : 1)) * a.part_floats;
     for (int x = tid; x < heads * (kDh / 4); x += kThreads) {
       const int h = x / (kDh / 4), d = 4 * (x % (kDh / 4));
       float4 o = *reinterpret_cast<const float4*>(&os[0][h][d]);
@@ -782,7 +806,7 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
     u += s1 - s0;
     first_segment = false;
   }
-  if (waiting == 0) return;
+  if (kWhole || waiting == 0) return;
 
   // The shared outputs, at most two: this worker's parts are in memory before
   // it takes their tickets, and whose ticket is the last joins the parts.
@@ -987,21 +1011,25 @@ void launch_attend(const AttendArg& a, int head_dim, int waves, hipStream_t stre
   const dim3 grid((unsigned)(a.workers * a.kv.n_kv_heads * a.q_tiles)), block(64 * waves);
 #define ATTEND_CASE(D, W) \
   hipLaunchKernelGGL((paged_attention_kernel<T, kE4M3, D, W>), grid, block, 0, stream, a)
+#define ATTEND_WAVES(D)                  \
+  if (waves == 1) ATTEND_CASE(D, 1);     \
+  else if (waves == 8) ATTEND_CASE(D, 8); \
+  else ATTEND_CASE(D, 4)
   if (head_dim == 256) {
-    ATTEND_CASE(256, 4);
+    if (waves == 1) ATTEND_CASE(256, 1);
+    else ATTEND_CASE(256, 4);
   } else if (head_dim == 128) {
-    if (waves == 8) ATTEND_CASE(128, 8);
-    else ATTEND_CASE(128, 4);
+    ATTEND_WAVES(128);
   } else {
-    if (waves == 8) ATTEND_CASE(64, 8);
-    else ATTEND_CASE(64, 4);
+    ATTEND_WAVES(64);
   }
+#undef ATTEND_WAVES
 #undef ATTEND_CASE
 }
 
 // How a call is launched: rows per launch (their units stay below 2^31), the
-// workers of each line and the lines (key heads times tiles of 16 queries),
-// and the floats of one workgroup's record for a split output.
+// workers of each line (with one wavefront: its rows) and the lines (key heads
+// times tiles of 16 queries), and the floats of one workgroup's record for a split output.
 // The device holds 512 workgroups of four wavefronts, two to a CU, or 256 of eight
 // (or of four at 256 dimensions: 65,536 keys of 4 heads 55 us, with 512 workers
 // 67).  Eight join twice the keys in LDS that four do, which pays in two cases:
@@ -1018,7 +1046,15 @@ struct AttendPlan {
   int waves, workers, lines, part_floats;
   int64_t most_parts;  // workgroups of any plan with these rows, heads and max_keys
 };
-constexpr int kPlaces = 512, kWideJoin = 96 << 10;
+// One wavefront, a workgroup to every output, where a row has a tile or two (no
+// more than kShortKeys keys: one row of 10 6.3 -> 4.4 us, 282 of up to 30 21 ->
+// 7.9; above, 4 rows of 128 7.3 and 8.2), or up to kManyKeys with more outputs
+// than the device holds workgroups twice over (1,600 outputs of up to 250 keys
+// 29 -> 19.8 us, of up to 500 37.6 -> 34.7; of up to 1,000 62 and 65.5, 512
+// outputs of up to 250 11 and 13.6): the wavefronts that a short row leaves idle
+// take other rows, and nothing is planned.
+constexpr int kPlaces = 512, kWideJoin = 96 << 10, kShortKeys = 64, kManyKeys = 512;
+constexpr int kMostWhole = 1 << 20;  // outputs: a grid below 2^32 threads
 AttendPlan attend_plan(const emoe_paged_kv& kv, int32_t rows, int32_t n_heads, int32_t max_keys,
                        int32_t window) {
   const int group = n_heads / kv.n_kv_heads;
@@ -1031,7 +1067,10 @@ AttendPlan attend_plan(const emoe_paged_kv& kv, int32_t rows, int32_t n_heads, i
   if (parts > (keys + four - 1) / four) parts = (keys + four - 1) / four;
   const int64_t idle = kPlaces / 2 - outputs;
   const bool whole = idle >= 0 && (keys + eight - 1) / eight * idle < kPlaces;
-  p.waves = kv.head_dim < 256 && (whole || parts * record > kWideJoin) ? 8 : 4;
+  if (outputs <= kMostWhole && (keys <= kShortKeys || (keys <= kManyKeys && outputs > 2 * kPlaces)))
+    p.waves = 1;
+  else
+    p.waves = kv.head_dim < 256 && (whole || parts * record > kWideJoin) ? 8 : 4;
   const int64_t most = keys / (kTileKeys * p.waves) + 2;  // units of one row
   p.rows_per_launch = (((int64_t)1 << 31) - 1 - kTickets) / most;
   if (p.rows_per_launch > kMaxRows) p.rows_per_launch = kMaxRows;
@@ -1178,12 +1217,12 @@ int32_t emoe_paged_attention(const emoe_paged_kv* kv, const emoe_paged_attention
   a.table_width = A.table_width;
   a.max_keys = A.max_keys;
   a.window = A.window;
-  a.workers = plan.workers;
   a.part_floats = plan.part_floats;
   const bool e4m3 = kv->dtype == EMOE_E4M3;
   for (int64_t r0 = 0; r0 < A.rows; r0 += plan.rows_per_launch) {
     a.row0 = (int32_t)r0;
     a.rows = (int32_t)(A.rows - r0 < plan.rows_per_launch ? A.rows - r0 : plan.rows_per_launch);
+    a.workers = plan.waves == 1 ? a.rows : plan.workers;
     if (A.dtype == EMOE_BF16) {
       if (e4m3) launch_attend<Bf16, true>(a, kv->head_dim, plan.waves, stream);
       else launch_attend<Bf16, false>(a, kv->head_dim, plan.waves, stream);

@@ -369,7 +369,8 @@ def ragged(rows, longest):
     ([300], 16, 16, 128), ([900] * 47, 4, 4, 64), (ragged(200, 400), 2, 1, 128),      # an output a workgroup
     (ragged(32, 900), 8, 8, 128), (ragged(64, 400), 8, 8, 64), ([130] * 64, 8, 8, 64),  # a row a worker
     (ragged(31, 900), 8, 8, 128), ([600] * 16, 4, 4, 256), (ragged(16, 1100), 4, 4, 256),
-    (ragged(90, 300), 16, 8, 64)])
+    (ragged(90, 300), 16, 8, 64), (ragged(130, 200), 8, 8, 128), (ragged(300, 64), 4, 4, 256),  # one wavefront
+    (ragged(1100, 40), 2, 2, 64), ([64, 1, 33], 40, 2, 128), ([65, 700], 48, 2, 64)])
 @pytest.mark.parametrize("kind,cache_kind", [("bf16", "bf16"), ("fp16", "fp16"), ("bf16", "e4m3")])
 def test_attention_cuts(lengths, heads, hk, d, kind, cache_kind):
     """Rows whole, in parts of their own and in equal runs, with four and with eight wavefronts."""
@@ -608,6 +609,7 @@ def test_logits(kind, vocab):
 
 @pytest.mark.parametrize("kind", ["f32", "bf16", "fp16"])
 @pytest.mark.parametrize("opts", [dict(width=0), dict(width=1), dict(width=3001),
+                                  dict(width=6143), dict(width=6144, biases=3),
                                   dict(width=0, biases=300), dict(width=0, mask="own"),
                                   dict(width=40, in_place=True, biases=3, mask="own"),
                                   dict(width=40, token=False), dict(width=40, stride=5)])
@@ -616,7 +618,8 @@ def test_logits_parts(kind, opts):
 
 
 @pytest.mark.parametrize("kind,rows,vocab", [("f32", 200, 12001), ("bf16", 150, 32771),
-                                             ("fp16", 1, 50304)])
+                                             ("fp16", 1, 50304), ("fp16", 90, 50021),
+                                             ("f32", 3, 200001)])
 def test_logits_large(kind, rows, vocab):
     run_logits(kind, rows, vocab, 300, seed=rows, biases=20, mask="rows")
 
