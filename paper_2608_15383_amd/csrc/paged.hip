@@ -485,7 +485,7 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
     const int per = few ? 1 : (a.rows + kThreads - 1) / kThreads, r0 = few ? lane : tid * per;
     constexpr int kPer = kMaxRows / kThreads;
     int units_[kPer], total = 0, most = 0;
-  #pragma unroll
+#pragma unroll
     for (int i = 0; i < kPer; ++i) {
       units_[i] = 0;
       if (i < per && r0 + i < a.rows) {
@@ -512,7 +512,7 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
       if (lane == 0) wave_sum[wave] = all;
       __syncthreads();
       int sum = 0;
-  #pragma unroll
+#pragma unroll
       for (int i = 0; i < kWaves; ++i) {
         before += i < wave ? wave_sum[i] : 0;
         sum += wave_sum[i];
@@ -525,7 +525,7 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
     if (!few) {
       if (lane == 0) wave_most[wave] = most;
       __syncthreads();
-  #pragma unroll
+#pragma unroll
       for (int i = 0; i < kWaves; ++i) most = max(most, wave_most[i]);
     }
     most = __builtin_amdgcn_readfirstlane(most);
@@ -538,7 +538,7 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
       int t = most - run < kPays ? most : run;
       while (true) {
         int mine = 0;
-  #pragma unroll
+#pragma unroll
         for (int i = 0; i < kPer; ++i) mine += i < per ? slots_of(units_[i], t) : 0;
         const int sum = sum_rows(mine, before);
         if (t < most && t > run + slack_units(kWaves)) break;  // equal runs, then
@@ -553,7 +553,7 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
     }
     if (target == 0) {
       int mine = 0;
-  #pragma unroll
+#pragma unroll
       for (int i = 0; i < kPer; ++i) mine += units_[i];
       all = sum_rows(mine, before);
     }
@@ -565,7 +565,7 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
     if (few) {
       row = (int)__builtin_ctzll(__ballot(u >= before && u < before + slots_lane));
     } else {
-  #pragma unroll
+#pragma unroll
       for (int i = 0; i < kPer; ++i) {
         if (i < per && r0 + i < a.rows) {
           const int n = slots_of(units_[i], target);
