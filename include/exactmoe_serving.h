@@ -80,7 +80,7 @@ typedef struct emoe_paged_append_args {
   int64_t table_stride;       /* between the table's rows, elements */
   int32_t dtype;              /* of q, k, v and q_out: EMOE_BF16 or EMOE_F16; a 16-bit cache has the same */
   int32_t tokens;             /* >= 0 */
-  int32_t n_heads;
+  int32_t n_heads;            /* of q, 1 .. 2^20; without a q not read */
   int32_t n_seqs, table_width;
   int32_t rotary_dim;         /* a multiple of 16, 0 (no rotation) .. head_dim */
   int32_t interleaved;        /* 0 or 1 */

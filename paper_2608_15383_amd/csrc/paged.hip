@@ -1083,8 +1083,10 @@ AttendPlan attend_plan(const emoe_paged_kv& kv, int32_t rows, int32_t n_heads, i
   return p;
 }
 
-// Bounds of the attention's integers: keys of a row and what a tile adds to them
-// stay within 32 bits, and lines times threads within a grid.
+// Bounds of the calls' integers: keys of a row and what a tile adds to them stay
+// within 32 bits, and lines times threads within a grid; an appended token's
+// items (at most 2^24 of q and, as a page's slots are below 2^30 elements, 2^27 of
+// k and v) and what a step of its workgroups adds to them stay within 32 bits.
 constexpr int32_t kMostKeys = 1 << 30, kMostHeads = 1 << 20;
 
 }  // namespace
@@ -1106,7 +1108,8 @@ int32_t emoe_paged_append(const emoe_paged_kv* kv, const emoe_paged_append_args*
                         A.rotary_dim, kv->head_dim);
   if (A.interleaved != 0 && A.interleaved != 1)
     return report_error(EMOE_EINVAL, "interleaved %d: need 0 or 1", A.interleaved);
-  if (A.q && A.n_heads < 1) return report_error(EMOE_ESHAPE, "n_heads %d", A.n_heads);
+  if (A.q && (A.n_heads < 1 || A.n_heads > kMostHeads))
+    return report_error(EMOE_ESHAPE, "n_heads %d: need 1 to 2^20", A.n_heads);
   if (A.tokens == 0) return EMOE_OK;
   const int64_t dh = kv->head_dim, kw = kv->n_kv_heads * dh, qw = (int64_t)A.n_heads * dh;
   if (A.rotary_dim > 0 && !A.inv_freq) return report_error(EMOE_EINVAL, "inv_freq is NULL");
@@ -1138,7 +1141,6 @@ int32_t emoe_paged_append(const emoe_paged_kv* kv, const emoe_paged_append_args*
   a.rotary_dim = A.rotary_dim;
   const int64_t heads = (A.q ? A.n_heads : 0) + 2 * (int64_t)kv->n_kv_heads;
   const int64_t items = heads * (dh / 16);
-  if (items >= (int64_t)1 << 31) return report_error(EMOE_ESHAPE, "%lld heads", (long long)heads);
   int64_t gy = 1;  // small calls: up to an item per thread
   while (A.tokens * gy < 512 && gy * kThreads < items) ++gy;
   const bool e4m3 = kv->dtype == EMOE_E4M3, inter = A.interleaved != 0;

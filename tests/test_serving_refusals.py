@@ -115,6 +115,15 @@ def test_append_checks(change, want):
     assert status("emoe_paged_append", C.byref(kv()), None, None) == EMOE_EINVAL
 
 
+@pytest.mark.parametrize("heads", [(1 << 20) + 1, 1 << 27, (1 << 31) - 1])
+def test_append_bounds_its_heads(heads):
+    """A row's items and what a step of the workgroups adds to them stay within 32 bits (2^27
+    heads of 128 would have passed them)."""
+    for tokens in (0, 1):
+        a = append(n_heads=heads, tokens=tokens, q_stride=1 << 40, q_out_stride=1 << 40)
+        assert status("emoe_paged_append", C.byref(kv()), C.byref(a), None) == EMOE_ESHAPE
+
+
 @pytest.mark.parametrize("change,want", [
     (dict(rows=0, q=None), EMOE_OK),
     (dict(rows=-1), EMOE_EINVAL),
