@@ -97,8 +97,10 @@ int32_t emoe_paged_append(const emoe_paged_kv* kv, const emoe_paged_append_args*
  *   out[r][h] = v_scale[g] * sum_j w_j v_j, rounded once;
  *   lse[r][h] = log sum_j exp(z_j).
  * Products of 16-bit values are summed in fp32, the softmax is fp32, its
- * weights enter the second product as two 16-bit halves (an infinity among the
- * values that a row sees makes its dimension infinite or NaN).  A row without keys
+ * weights enter the second product as two 16-bit halves: to 2^-16 of each, over
+ * fp16 pages down to 2^-64 of the largest (an infinity among the values that a
+ * row sees makes its dimension infinite or NaN, and so may the sums of values
+ * above 2^88).  A row without keys
  * (n <= 0, s outside [0, n_seqs), no page) has out = 0 and lse = -inf.  n is
  * cut to max_keys and to the table.  What lies in slots without a key (never
  * written, NaN) has no effect.  The last token's own key is one of the n:

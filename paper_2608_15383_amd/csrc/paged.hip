@@ -1,6 +1,7 @@
 // The paged key-value cache (exactmoe_serving.h): append with the rotary
 // positions on the way, and the attention of one new token per row.
 #include <cmath>
+#include <type_traits>
 
 #include "device_rope.h"
 #include "device_route.h"
@@ -156,12 +157,10 @@ struct AttendArg {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 // The 16-bit type's matrix instruction (16 x 16 outputs, 32 products each) and
-// its pairs: of two floats, and of two E4M3 values (exact) of a dword's half.
+// its pairs of two E4M3 values (exact) of a dword's half.
 template <class T>
 struct Half16;
 template <>
@@ -245,9 +244,16 @@ __device__ __forceinline__ int units_of(int first, int n) {
 // dimensions), which keeps values out of LDS.  A query's running maximum, sum
 // and output columns all live in lanes l16 = query, so nothing is exchanged
 // between queries in the loop.
+// Its weights are two 16-bit halves each, what the first one's rounding leaves
+// being the second: with them a weight is known to 2^-16 of itself, in bf16
+// however small it is, in fp16 only from 2^-9 on.  E4M3 values are exact in bf16
+// and take bf16 weights under queries of either type.
 template <class T, bool kE4M3, int kDh>
 struct Tile {
   typedef Half16<T> H16;
+  static constexpr bool kF16Weights = !kE4M3 && T::kType == EMOE_F16;
+  typedef typename std::conditional<kF16Weights, Fp16, Bf16>::type W;
+  typedef Half16<W> HW;
   static constexpr int kSteps = kDh / 32;
   static constexpr int kItem = kE4M3 ? 1 : 2;
   static constexpr int kChunk = kE4M3 && kDh == 64 ? 8 : 16;  // bytes of a lane's load
@@ -356,10 +362,18 @@ struct Tile {
 #pragma unroll
       for (int w = 0; w < kVWords; ++w) v[j][w] = (there >> j) & 1 ? v[j][w] : 0u;
   }
+  // Lets the compiler know nothing of the values any more: a further add_pair would
+  // have it keep all transposed pairs, in 45 registers more.
+  __device__ __forceinline__ void transpose_again() {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int w = 0; w < kVWords; ++w) asm volatile("" : "+v"(v[j][w]));
+  }
   // The pair of dimensions (2w, 2w + 1) of key j.
   template <int kW>
   __device__ __forceinline__ uint32_t pair(int j) const {
-    if constexpr (kE4M3) return H16::template from_e4m3<(kW & 1) != 0>(v[j][kW >> 1]);
+    if constexpr (kE4M3) return HW::template from_e4m3<(kW & 1) != 0>(v[j][kW >> 1]);
     else return v[j][kW];
   }
   template <int kW>
@@ -372,10 +386,10 @@ struct Tile {
       o[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
     }
     const uint4 ve = make_uint4(e[0], e[1], e[2], e[3]), vo = make_uint4(o[0], o[1], o[2], o[3]);
-    acc[2 * kW] = H16::mfma(ve, hi, acc[2 * kW]);
-    acc[2 * kW + 1] = H16::mfma(vo, hi, acc[2 * kW + 1]);
-    acc[2 * kW] = H16::mfma(ve, lo, acc[2 * kW]);
-    acc[2 * kW + 1] = H16::mfma(vo, lo, acc[2 * kW + 1]);
+    acc[2 * kW] = HW::mfma(ve, hi, acc[2 * kW]);
+    acc[2 * kW + 1] = HW::mfma(vo, hi, acc[2 * kW + 1]);
+    acc[2 * kW] = HW::mfma(ve, lo, acc[2 * kW]);
+    acc[2 * kW + 1] = HW::mfma(vo, lo, acc[2 * kW + 1]);
     if constexpr (kW + 1 < kDims / 2) add_pair<kW + 1>(hi, lo, acc);
   }
 };
@@ -452,6 +466,8 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
   constexpr int kThreads = 64 * kWaves;
   typedef Tile<T, kE4M3, kDh> Tl;
   constexpr int kPays = pays_units(kWaves * kTileKeys * 2 * kDh * Tl::kItem);
+  // fp16 weights begin at 2^7: there is room above, but little below.
+  constexpr float kLead = Tl::kF16Weights ? 7.f : 0.f;
   constexpr int kRow = kDh + 4;  // padded: lanes 16 apart in dimensions, 1 in queries
   constexpr bool kWhole = kWaves == 1;  // a row to a workgroup, nothing shared
   constexpr int kRows = kWhole ? 1 : kMaxRows, kJoiners = kWhole ? 1 : kThreads;
@@ -703,15 +719,16 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
         }
         tile.clear_v(there);
       }
-      // The maximum that the weights refer to moves only when a score exceeds
-      // it by 2^8: until then they stay below 256, and nothing is rescaled.
+      // The exponent that the weights refer to follows the maximum only when a
+      // score exceeds it by 8: until then they stay below 2^(8 + kLead), and
+      // nothing is rescaled.
       float top = z[0];
 #pragma unroll
       for (int j = 1; j < 8; ++j) top = fmaxf(top, z[j]);
-      if (__any(top > m + 8.f)) {
+      if (__any(top > m + (8.f + kLead))) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float m2 = fmaxf(m, top);
+        const float m2 = fmaxf(m, top - kLead);
         const float shrink = m2 == -INFINITY ? 0.f : exp2_hw(m - m2);
         m = m2;
         l *= shrink;
@@ -719,20 +736,65 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
         for (int c = 0; c < Tl::kDims; ++c) acc[c] *= shrink;
       }
       const float ref = m == -INFINITY ? 0.f : m;
-      // Weights in two 16-bit halves: what the first one's rounding leaves is
-      // the second, so the products see 16 bits of bf16 weights instead of 8.
-      uint32_t hi[4], lo[4];
+      float p[8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float p0 = exp2_hw(z[2 * j] - ref), p1 = exp2_hw(z[2 * j + 1] - ref);
-        l += p0;
-        l += p1;
-        const uint32_t h0 = T::down(p0), h1 = T::down(p1);
-        hi[j] = h0 | (h1 << 16);
-        lo[j] = T::down(p0 - T::up(h0)) | (T::down(p1 - T::up(h1)) << 16);
+      for (int j = 0; j < 8; ++j) {
+        p[j] = exp2_hw(z[j] - ref);
+        l += p[j];
       }
-      tile.template add_pair<0>(make_uint4(hi[0], hi[1], hi[2], hi[3]),
-                                make_uint4(lo[0], lo[1], lo[2], lo[3]), acc);
+      // fp16 weights below 2^-9 (a key that draws most of the weight to itself
+      // leaves all others there) are added in turns of their own, 2^24 and 2^48
+      // times as large, to sums as much larger; the products by powers of two are
+      // exact.  Weights below 2^-57, 2^-64 of the largest, would not show: 2^20 of
+      // them times the largest value are 2^-28, below fp16's smallest half.  What
+      // asks for it costs 1% where no weight is small (131,072 keys 91.3 -> 91.9 us,
+      // 300 rows of up to 60 keys 10.6 -> 11.3), a turn more 0.5% to 20% (the same,
+      // one key 25 nats above the others, 91.7 -> 92.1; 302 keys 8.1 -> 9.8).
+      float lift = 1.f;
+      while (true) {
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = p[j];
+        bool rest = false;
+        if constexpr (Tl::kF16Weights) {
+          auto least = [&] {  // of the weights that are not 0, as bits less 1
+            uint32_t b = ~0u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) b = min(b, __float_as_uint(p[j]) - 1u);
+            return b;
+          };
+          constexpr uint32_t kLeast = (127 - 9) << 23;  // 2^-9
+          rest = __any(least() < kLeast - 1u);
+          if (rest) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const bool small = p[j] < 0x1p-9f;
+              y[j] = small ? 0.f : p[j];
+              p[j] = small ? p[j] * 0x1p24f : 0.f;
+            }
+          }
+        }
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          typedef typename Tl::W W;
+          const uint32_t h0 = W::down(y[2 * j]), h1 = W::down(y[2 * j + 1]);
+          hi[j] = h0 | (h1 << 16);
+          lo[j] = W::down(y[2 * j] - W::up(h0)) | (W::down(y[2 * j + 1] - W::up(h1)) << 16);
+        }
+        tile.template add_pair<0>(make_uint4(hi[0], hi[1], hi[2], hi[3]),
+                                  make_uint4(lo[0], lo[1], lo[2], lo[3]), acc);
+        if (!rest || lift == 0x1p48f) break;
+        tile.transpose_again();
+        lift *= 0x1p24f;
+#pragma unroll
+        for (int c = 0; c < Tl::kDims; ++c) acc[c] *= 0x1p24f;
+      }
+      if (lift != 1.f) {
+        const float back = lift == 0x1p24f ? 0x1p-24f : 0x1p-48f;
+#pragma unroll
+        for (int c = 0; c < Tl::kDims; ++c) acc[c] *= back;
+      }
       if (more) {
         load_v(off);
         now = next;
