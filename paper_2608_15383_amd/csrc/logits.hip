@@ -559,8 +559,8 @@ int32_t emoe_process_logits(const emoe_logits_args* args, void* workspace, size_
   a.bias_width = A.bias_width;
   a.n_masks = A.n_masks;
   a.chunks = plan.chunks;
-  // Rows of one launch: a grid of at most 2^31 threads (plan.chunks is below 2^18,
-  // and below 2^9 with the smallest chunks).
+  // Rows of one launch: a grid of at most 2^31 threads (plan.chunks is at most 2^18,
+  // and below 2^11 with the smallest chunks: fewer than 512 of up to four times their size).
   int64_t step = ((int64_t)1 << 21) / plan.chunks;
   if (step > kMaxRows) step = kMaxRows;
   if (step > A.rows) step = A.rows;
