@@ -175,7 +175,8 @@ typedef struct emoe_logits_args {
 
 /* Workspace (needed with next_token only): what the workgroups of a row hand
  * over to each other.  Zero it once, before its first call; every call leaves it
- * zero.  It may serve calls of any sizes, captured or not, as long as no two of
+ * zero.  Over one that was not zeroed calls end, but their tokens are undefined,
+ * and so are those of later calls until it is.  It may serve calls of any sizes, captured or not, as long as no two of
  * them overlap in time, and no other use. */
 size_t emoe_process_logits_workspace_bytes(int32_t rows, int32_t vocab);
 

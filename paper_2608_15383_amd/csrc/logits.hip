@@ -136,8 +136,10 @@ __device__ __forceinline__ uint64_t choice(float x, int v) {
 // meanwhile.  The collector waits only for workgroups that run already and wait
 // for nobody, so every wait ends, whatever else the device runs.  To count
 // workgroups as they finish instead takes one trip to memory more, 0.6 us of the
-// 5.8 that a row of 50,304 logits took so.  The bound on the wait (kSpinLimit polls,
-// about a second) is for a workspace that was not zeroed: the token is -1 then.
+// 5.8 that a row of 50,304 logits took so.  The wait is bounded (kSpinLimit polls,
+// about a second) so that a launch ends over a workspace that was not zeroed, too.
+// Its tokens are undefined: perhaps nobody starts last, or old words pass for
+// choices, and tickets and words may stay nonzero for later calls.
 constexpr uint64_t kNoChoice = 1;
 constexpr int kSpinLimit = 1 << 19;
 __device__ __forceinline__ int chosen(uint64_t c) { return c ? (int)~(uint32_t)c : -1; }
