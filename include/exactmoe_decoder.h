@@ -70,8 +70,9 @@ size_t emoe_decoder_workspace_bytes(const emoe_decoder_dims* dims, int32_t max_t
 
 /* Create a decoder over caller-owned weights, one slot cache per layer
  * (host array of n_layers emoe_cache*, each created with dims->moe and a slot
- * bank) and a KV cache (device, emoe_decoder_kv_bytes).  Creates a rocBLAS
- * handle for the dense projections of prompts (more than 4 tokens; decode
+ * bank) and a KV cache (device, emoe_decoder_kv_bytes; NULL for a decoder that
+ * only runs emoe_decoder_forward_paged: emoe_decoder_forward refuses then, with
+ * EMOE_ESTATE).  Creates a rocBLAS handle for the dense projections of prompts (more than 4 tokens; decode
  * steps use the library's own GEMV kernel).  EMOE_ESHAPE for unsupported
  * sizes. */
 int32_t emoe_decoder_create(const emoe_decoder_dims* dims, const emoe_decoder_weights* weights,
@@ -84,9 +85,9 @@ int32_t emoe_decoder_destroy(emoe_decoder* dec);
  * then the head on the last token: logits (device f32 [V]) and the greedy
  * next token (device int32 [1]; ties to the lower id).  A prompt is one call
  * with pos0 = 0; each decode step is a call with T = 1.  pos0 + T must not
- * exceed max_positions.  EMOE_ESTATE without a KV cache.  stats (nullable) accumulates the MoE layers'
- * counters.  Blocks the host when a layer's cache is not fully resident
- * (emoe_moe_forward's batched expert-id transfer). */
+ * exceed max_positions.  EMOE_ESTATE without a KV cache.  stats (nullable)
+ * accumulates the MoE layers' counters.  Blocks the host when a layer's cache
+ * is not fully resident (emoe_moe_forward's batched expert-id transfer). */
 int32_t emoe_decoder_forward(emoe_decoder* dec, const int32_t* tokens, int32_t T, int32_t pos0,
                              float* logits, int32_t* next_token, void* workspace,
                              size_t workspace_bytes, hipStream_t stream, emoe_stats* stats);
