@@ -234,6 +234,7 @@ class Decoder:
                            cast(self._arrays["moe_norm"]), cast(self._arrays["w_router"]))
         handles = (C.c_void_p * n)(*[c.handle.value for c in caches])
         self.dims = dd
+        self.device = weights["embed"].device
         self._keep = (weights, caches, kv, handles)
         h = C.c_void_p()
         check(lib().emoe_decoder_create(C.byref(dd), C.byref(w), C.cast(handles, C.POINTER(C.c_void_p)),
@@ -274,8 +275,8 @@ class Decoder:
         """emoe_decoder_forward_paged: tokens, positions (device int32 [n], of sequences seqs [n] or
         0 .. n-1) over one PagedKV per layer; logits f32 [n or len(out_rows)][V], processed as by
         process_logits with the last eleven arguments (of the logits' rows)."""
-        if len(kvs) != self.dims.n_layers or any(kv.device != kvs[0].device for kv in kvs):
-            _refuse(f"need {self.dims.n_layers} caches on one device")
+        if len(kvs) != self.dims.n_layers or any(kv.device != self.device for kv in kvs):
+            _refuse(f"need {self.dims.n_layers} caches on the decoder's device, {self.device}")
         views = (PagedKVView * len(kvs))(*[kv.view for kv in kvs])
         device = kvs[0].index
         binding().decoder_forward_paged(
