@@ -17,7 +17,7 @@ import pytest
 import torch
 
 from paper_2608_15383_amd import api
-from tests.test_gpu_serving import HALF, TYPES, U, check, f64, gpu, ids
+from tests.test_gpu_serving import HALF, TYPES, U, check, f64, gpu, ids, ragged, run_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -95,6 +95,17 @@ def test_weights_far_below_the_largest(kind, cache_kind, n, d, where, size):
         got, lse = attend(kv, table, q, [n])
         z = f64(q)[0] @ f64(k)[:, 0].T
         check_weights(kind, got[0], lse[0], z, f64(v)[:, 0])
+
+
+@pytest.mark.parametrize("cache_kind", ["fp16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("scale", [1.0, 4.0, -0.3, 0.0])
+def test_scores_far_apart(cache_kind, d, scale):
+    """Random scores of up to +-200: large and small weights in one tile, in tiles that a row, a
+    window or a missing page cuts, and a maximum that moves far."""
+    for lengths, more in (([700, 5, 64, 0, 3001], {}), (ragged(70, 500), dict(holes=30)),
+                          ([1000, 33, 2050], dict(window=300)), (ragged(300, 64), {})):
+        run_attention("fp16", cache_kind, lengths, 4, 2, d, 16, seed=d, scale=scale, **more)
 
 
 @pytest.mark.parametrize("gap", [33.0, 38.0, 43.0, 60.0])
