@@ -456,11 +456,11 @@ __device__ __forceinline__ int slots_of(int units, int target) {
 // different heads, which lie next to each other in memory.
 // Bound by HBM where there are keys enough: per tile and wavefront 16 KB (16
 // bits, 128 dimensions) against about 250 vector and 24 matrix instructions.
-// 131,072 keys of 8 heads of 128 take 91 us, 5.9 TB/s, of the 6.0 that this
-// pattern of reads reaches without any arithmetic; 128 rows over 8 bits 277 us,
-// 5.2 TB/s (ragged rows; heads of one 128-byte line each).  Short calls are
-// bound by the chain of trips to memory (lengths, page table, keys, parts,
-// ticket, parts again): 302 keys take 9 us.
+// 131,072 keys of 8 heads of 128 take 91.5 us, 5.9 TB/s, of the 6.5 that this
+// pattern of reads reaches without any arithmetic; 128 rows over 8 bits 279 us,
+// 5.3 TB/s of 6.0 (ragged rows; heads of one 128-byte line each).  Short calls
+// are bound by the chain of trips to memory (lengths, page table, keys, parts,
+// ticket, parts again): 302 keys take 8.2 us.
 template <class T, bool kE4M3, int kDh, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attention_kernel(AttendArg a) {
   constexpr int kThreads = 64 * kWaves;
