@@ -746,10 +746,10 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
       // leaves all others there) are added in turns of their own, 2^24 and 2^48
       // times as large, to sums as much larger; the products by powers of two are
       // exact.  Weights below 2^-57, 2^-64 of the largest, would not show: 2^20 of
-      // them times the largest value are 2^-28, below fp16's smallest half.  What
-      // asks for it costs 1% where no weight is small (131,072 keys 91.3 -> 91.9 us,
-      // 300 rows of up to 60 keys 10.6 -> 11.3), a turn more 0.5% to 20% (the same,
-      // one key 25 nats above the others, 91.7 -> 92.1; 302 keys 8.1 -> 9.8).
+      // them times the largest value are 2^-28, below fp16's smallest half.  To look
+      // for small weights costs 1% to 6% (131,072 keys 91.3 -> 91.9 us, 300 rows of
+      // up to 60 keys 10.6 -> 11.3), a turn more 0.5% to 20% (one key 25 nats above
+      // all others: 131,072 keys 91.7 -> 92.1, 302 keys 8.1 -> 9.8).
       float lift = 1.f;
       while (true) {
         float y[8];
@@ -757,14 +757,10 @@ __global__ __launch_bounds__(64 * kWaves, kDh == 256 ? 1 : 2) void paged_attenti
         for (int j = 0; j < 8; ++j) y[j] = p[j];
         bool rest = false;
         if constexpr (Tl::kF16Weights) {
-          auto least = [&] {  // of the weights that are not 0, as bits less 1
-            uint32_t b = ~0u;
+          uint32_t least = ~0u;  // the bits, less 1, of the smallest weight above 0
 #pragma unroll
-            for (int j = 0; j < 8; ++j) b = min(b, __float_as_uint(p[j]) - 1u);
-            return b;
-          };
-          constexpr uint32_t kLeast = (127 - 9) << 23;  // 2^-9
-          rest = __any(least() < kLeast - 1u);
+          for (int j = 0; j < 8; ++j) least = min(least, __float_as_uint(p[j]) - 1u);
+          rest = __any(least < __float_as_uint(0x1p-9f) - 1u);
           if (rest) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {

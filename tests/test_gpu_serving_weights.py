@@ -5,9 +5,10 @@ with u = 2^-24 (the rounding of an fp32 operation):
   scores      the scale, its log2 e and a key scale: 4 u |z| =: dz;
   weights     2 dz + 2^-15 of each (both exponents, exp2 itself, its two 16-bit halves);
   sums        no more than 1,024 additions one after another, of the products and of the
-              weights: a wavefront takes at most 4 tiles of 32 keys of a row of 131,072
-              (256 workgroups of 4 wavefronts at least), with 4 products per key; then the
-              wavefronts' and the workgroups' parts are joined;
+              weights: a wavefront takes at most 4 tiles of 32 keys of these rows (256
+              workgroups of 4 wavefronts at 256 dimensions, else of 8), with 6 products per
+              key at most (two halves in up to three turns); then the wavefronts' and the
+              workgroups' parts are joined;
   the store   half a step.
 """
 import math
