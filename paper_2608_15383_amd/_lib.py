@@ -21,6 +21,7 @@ EMOE_GEMV_MAX_TOKENS = 4
 EMOE_NOALLOC_SCRATCH_BYTES = 32 << 20
 EMOE_F32, EMOE_BF16, EMOE_F16, EMOE_E4M3 = 0, 1, 2, 3
 EMOE_SERVING_TICKET_BYTES = 131072
+EMOE_MAX_NODES = 64
 
 
 class Dims(C.Structure):
@@ -99,13 +100,47 @@ class DecoderBatch(C.Structure):
                                             "max_keys")])
 
 
+class PagedAxes(C.Structure):
+    _fields_ = [("angles", C.c_void_p), ("axes", C.c_void_p), ("angle_stride", C.c_int64),
+                ("n_axes", C.c_int32)]
+
+
+class PagedTreeArgs(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "out", "lse", "lengths", "starts", "seqs", "tree",
+                                           "slopes", "page_table")]
+                + [(n, C.c_int64) for n in ("q_stride", "out_stride", "table_stride")]
+                + [("scale", C.c_float), ("cap", C.c_float)]
+                + [(n, C.c_int32) for n in ("dtype", "rows", "trees", "n_heads", "n_seqs",
+                                            "table_width", "max_keys", "max_nodes", "window")])
+
+
+class AcceptArgs(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("tokens", "chosen", "tree", "starts", "lengths", "path",
+                                           "accepted", "new_tokens", "new_lengths")]
+                + [(n, C.c_int64) for n in ("path_stride", "new_tokens_stride")]
+                + [(n, C.c_int32) for n in ("rows", "trees", "max_nodes")])
+
+
+class CompactArgs(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("lengths", "path", "accepted", "seqs", "page_table")]
+                + [(n, C.c_int64) for n in ("path_stride", "table_stride")]
+                + [(n, C.c_int32) for n in ("trees", "max_nodes", "n_seqs", "table_width")])
+
+
+class ForkArgs(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("page_table", "parents", "lengths", "fresh", "new_table")]
+                + [(n, C.c_int64) for n in ("table_stride", "new_table_stride")]
+                + [(n, C.c_int32) for n in ("forks", "n_seqs", "table_width")])
+
+
 _vp = C.c_void_p
 _i32 = C.c_int32
 _i32p = C.POINTER(C.c_int32)
 _i64p = C.POINTER(C.c_int64)
 _dimsp = C.POINTER(Dims)
 
-# name -> (restype, argtypes); mirrors include/exactmoe.h, exactmoe_decoder.h, exactmoe_serving.h
+# name -> (restype, argtypes); mirrors include/exactmoe.h, exactmoe_decoder.h, exactmoe_serving.h,
+# exactmoe_drafts.h
 SIGNATURES = {
     "emoe_status_string": (C.c_char_p, [_i32]),
     "emoe_last_error": (C.c_char_p, []),
@@ -156,6 +191,15 @@ SIGNATURES = {
     "emoe_decoder_forward_paged": (_i32, [_vp, C.POINTER(PagedKVView), C.POINTER(DecoderBatch), _vp,
                                           C.POINTER(LogitsArgs), _vp, _vp, C.c_size_t, _vp,
                                           C.POINTER(Stats)]),
+    "emoe_paged_append_axes": (_i32, [C.POINTER(PagedKVView), C.POINTER(PagedAppendArgs),
+                                      C.POINTER(PagedAxes), _vp]),
+    "emoe_paged_tree_attention_workspace_bytes": (C.c_size_t, [C.POINTER(PagedKVView), _i32, _i32,
+                                                               _i32, _i32]),
+    "emoe_paged_tree_attention": (_i32, [C.POINTER(PagedKVView), C.POINTER(PagedTreeArgs), _vp,
+                                         C.c_size_t, _vp]),
+    "emoe_accept_drafts": (_i32, [C.POINTER(AcceptArgs), _vp]),
+    "emoe_paged_compact": (_i32, [C.POINTER(PagedKVView), _i32, C.POINTER(CompactArgs), _vp]),
+    "emoe_paged_fork": (_i32, [C.POINTER(PagedKVView), _i32, C.POINTER(ForkArgs), _vp]),
     "emoe_profile_begin": (_i32, [_i32]),
     "emoe_profile_end": (_i32, [_vp, _vp, _i32, _i32p]),
 }
@@ -199,7 +243,9 @@ def binding():
         h = lib()
         b.init(ExactMoEError, *[C.cast(getattr(h, n), C.c_void_p).value for n in
                                 ("emoe_last_error", "emoe_paged_append", "emoe_paged_attention",
-                                 "emoe_process_logits", "emoe_decoder_forward_paged")])
+                                 "emoe_process_logits", "emoe_decoder_forward_paged",
+                                 "emoe_paged_append_axes", "emoe_paged_tree_attention",
+                                 "emoe_accept_drafts", "emoe_paged_compact", "emoe_paged_fork")])
         _binding = b
     return _binding
 

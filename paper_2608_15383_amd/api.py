@@ -400,6 +400,74 @@ def decoder_paged_workspace_bytes(dd: DecoderDims, n_tokens: int, n_out: int, ma
     return int(lib().emoe_decoder_paged_workspace_bytes(C.byref(dd), n_tokens, n_out, max_keys))
 
 
+# ---------------------------------------------------------------- drafted tokens
+# The calls of exactmoe_drafts.h.
+def paged_append_axes(kv: PagedKV, q, k, v, positions, angles, axes, page_table, inv_freq, seqs=None,
+                      q_out=None, interleaved: bool = False, stream=None) -> None:
+    """emoe_paged_append_axes: paged_append with angles[t][axes[i]] * inv_freq[i] in place of
+    positions[t] * inv_freq[i].  angles i32 [n][axes]; axes i32 [rotary_dim / 2], the axis of each
+    pair, or None: the first one.  A drafted node of depth d behind n keys: angles [[n + d]]."""
+    binding().paged_append_axes(kv.address, kv.index, q, k, v, positions, page_table, inv_freq, seqs,
+                                q_out, interleaved, angles, axes, _stream_on(kv.index, stream))
+
+
+def paged_tree_attention_workspace_bytes(kv: PagedKV, trees: int, n_heads: int, max_keys: int,
+                                         max_nodes: int) -> int:
+    return int(lib().emoe_paged_tree_attention_workspace_bytes(C.byref(kv.view), trees, n_heads,
+                                                               max_keys, max_nodes))
+
+
+def paged_tree_attention(kv: PagedKV, q, page_table, lengths, out, workspace, max_keys: int,
+                         max_nodes: int, tree=None, starts=None, seqs=None,
+                         scale: float | None = None, cap: float = 0.0, slopes=None, window: int = 0,
+                         lse=None, stream=None) -> None:
+    """emoe_paged_tree_attention: out[r] = attention of node r of the trees behind the first
+    lengths[g] keys of their sequences, over those keys and the nodes of its mask.  q, out [rows]
+    [heads][dim]; lengths, seqs i32 [trees]; starts i32 [trees + 1], the trees' first rows (None:
+    max_nodes rows each); tree i64 [rows], bit j: sees node j (None: chains); page_table i32
+    [sequences][pages]; slopes f32 [heads]; lse f32 [rows][heads]; scale 1 / sqrt(dim) when None.
+    max_keys bounds lengths and nodes together.  workspace: paged_tree_attention_workspace_bytes,
+    of any content."""
+    if scale is None:
+        scale = kv.view.head_dim ** -0.5
+    binding().paged_tree_attention(kv.address, kv.index, q, page_table, lengths, out, workspace,
+                                   max_keys, max_nodes, tree, starts, seqs, scale, cap, slopes,
+                                   window, lse, _stream_on(kv.index, stream))
+
+
+def accept_drafts(tokens, chosen, lengths, path, accepted, new_tokens=None, new_lengths=None,
+                  tree=None, starts=None, stream=None) -> None:
+    """emoe_accept_drafts: from each tree's first node down, as long as a child's token is the one
+    chosen after its parent.  tokens, chosen i32 [rows]; tree, starts as in paged_tree_attention;
+    path, new_tokens i32 [trees][most nodes], accepted i32 [trees]; new_lengths = lengths +
+    accepted, i32 [trees]."""
+    if not tokens.is_cuda:
+        _refuse(f"tokens is on {tokens.device}")
+    binding().accept_drafts(tokens, chosen, lengths, path, accepted, new_tokens, new_lengths, tree,
+                            starts, _stream_on(tokens.device.index, stream))
+
+
+def paged_compact(kvs, page_table, lengths, path, accepted, seqs=None, stream=None) -> None:
+    """emoe_paged_compact: in every cache of the list kvs, position lengths[g] + i of a sequence
+    takes what lengths[g] + path[g][i] held, for i < accepted[g].  path i32 [trees][most nodes];
+    lengths (those before the acceptance), accepted, seqs i32 [trees]."""
+    if not kvs:
+        _refuse("kvs is empty")
+    binding().paged_compact(kvs, kvs[0].index, page_table, lengths, path, accepted, seqs,
+                            _stream_on(kvs[0].index, stream))
+
+
+def paged_fork(kvs, page_table, parents, lengths, fresh, new_table, stream=None) -> None:
+    """emoe_paged_fork: new_table[f] = the pages of the first lengths[f] positions of sequence
+    parents[f]; a page in use only in part is copied to page fresh[f] of every cache of the list kvs
+    (fresh None or outside the pool: shared).  parents, lengths, fresh i32 [forks]; new_table i32
+    [forks][the width of page_table]."""
+    if not kvs:
+        _refuse("kvs is empty")
+    binding().paged_fork(kvs, kvs[0].index, page_table, parents, lengths, fresh, new_table,
+                         _stream_on(kvs[0].index, stream))
+
+
 def profile_begin(max_kernels: int) -> None:
     """emoe_profile_begin: time each kernel the layer calls launch from this thread."""
     check(lib().emoe_profile_begin(max_kernels))
@@ -422,4 +490,5 @@ __all__ = ["Dims", "Stats", "WsLayout", "ExactMoEError", "EMOE_PATH_AUTO", "EMOE
            "decoder_workspace_bytes", "Decoder", "moe_forward_sequential", "test_fail_copy_after", "profile_begin", "profile_end",
            "PagedKV", "rope_frequencies", "paged_append", "paged_attention",
            "paged_attention_workspace_bytes", "decoder_paged_workspace_bytes", "process_logits", "process_logits_workspace_bytes",
-           "lib"]
+           "paged_append_axes", "paged_tree_attention", "paged_tree_attention_workspace_bytes",
+           "accept_drafts", "paged_compact", "paged_fork", "lib"]

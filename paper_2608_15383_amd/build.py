@@ -22,7 +22,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libexactmoe.so")
 BINDING = os.path.join(PKG, "_binding.so")
 SOURCES = ["capi.hip", "quantize.hip", "route.hip", "gemv.hip", "gemm.hip", "decode.hip",
-           "decoder.hip", "paged.hip", "logits.hip"]
+           "decoder.hip", "paged.hip", "logits.hip", "tree.hip", "tree_bf16.hip", "tree_fp16.hip",
+           "drafts.hip"]
 
 CXX = os.environ.get("CXX", "g++")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

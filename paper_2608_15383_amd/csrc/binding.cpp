@@ -1,5 +1,5 @@
-// Compiled half of the Python binding of exactmoe_serving.h: takes tensors,
-// checks what the library cannot see in a pointer (types, shapes, strides,
+// Compiled half of the Python binding of exactmoe_serving.h and exactmoe_drafts.h:
+// takes tensors, checks what the library cannot see in a pointer (types, shapes, strides,
 // devices) and calls the C entry points, whose addresses and whose exception
 // class Python hands over once (init).  Marshalling only.  A decode step's calls
 // take 3 to 15 us on the GPU, and the same checks in Python took 5 to 8 us of a
@@ -12,8 +12,9 @@
 #include <initializer_list>
 #include <stdexcept>
 #include <string>
+#include <vector>
 
-#include "exactmoe_serving.h"
+#include "exactmoe_drafts.h"
 
 namespace {
 
@@ -22,6 +23,11 @@ decltype(&emoe_paged_append) g_append = nullptr;
 decltype(&emoe_paged_attention) g_attention = nullptr;
 decltype(&emoe_process_logits) g_logits = nullptr;
 decltype(&emoe_decoder_forward_paged) g_decoder = nullptr;
+decltype(&emoe_paged_append_axes) g_append_axes = nullptr;
+decltype(&emoe_paged_tree_attention) g_tree = nullptr;
+decltype(&emoe_accept_drafts) g_accept = nullptr;
+decltype(&emoe_paged_compact) g_compact = nullptr;
+decltype(&emoe_paged_fork) g_fork = nullptr;
 decltype(&emoe_last_error) g_last_error = nullptr;
 
 struct Refused : std::runtime_error {
@@ -30,7 +36,7 @@ struct Refused : std::runtime_error {
 
 [[noreturn]] void refuse(const std::string& message) { throw Refused(message); }
 
-enum Kind { kI32 = -1, kF64 = -2 };  // besides emoe_dtype
+enum Kind { kI32 = -1, kF64 = -2, kI64 = -3 };  // besides emoe_dtype
 
 // The emoe_dtype of a tensor; 16-bit patterns without a type of their own are bf16.
 int type_of(const at::Tensor& t, const char* name) {
@@ -44,6 +50,8 @@ int type_of(const at::Tensor& t, const char* name) {
     case at::kInt:
     case at::kUInt32: return kI32;
     case at::kDouble: return kF64;
+    case at::kLong:
+    case at::kUInt64: return kI64;
     default: refuse(std::string(name) + ": type " + c10::toString(t.scalar_type()) + " is not supported");
   }
 }
@@ -184,51 +192,74 @@ int32_t on_device(int device, Fn fn, Args... args) {
   return status;
 }
 
-// (kv, device, q, k, v, positions, page_table, inv_freq, seqs, q_out, interleaved, stream)
+// What the appends have in common: (kv, device, q, k, v, positions, page_table, inv_freq, seqs, q_out,
+// interleaved).
+emoe_paged_append_args append_args(const Kv& kv, PyObject* const* a) {
+  const int64_t hk = kv.view->n_kv_heads, d = kv.view->head_dim;
+  const at::Tensor& k0 = tensor(a[3], "k");
+  const int type = type_of(k0, "k");
+  const int64_t n = k0.dim() ? k0.size(0) : 0;
+  const at::Tensor& k = head_rows(a[3], "k", type, n, hk, d, kv.device);
+  const at::Tensor& v = head_rows(a[4], "v", type, n, hk, d, kv.device);
+  emoe_paged_append_args A{};
+  A.k = k.data_ptr();
+  A.k_stride = k.stride(0);
+  A.v = v.data_ptr();
+  A.v_stride = v.stride(0);
+  if (a[2] != Py_None) {
+    const at::Tensor& q0 = tensor(a[2], "q");
+    const int64_t heads = q0.dim() == 3 ? q0.size(1) : 0;
+    const at::Tensor& q = head_rows(a[2], "q", type, n, heads, d, kv.device);
+    const at::Tensor& q_out = a[9] == Py_None ? q : head_rows(a[9], "q_out", type, n, heads, d, kv.device);
+    A.q = q.data_ptr();
+    A.q_stride = q.stride(0);
+    A.q_out = q_out.data_ptr();
+    A.q_out_stride = q_out.stride(0);
+    A.n_heads = i32(heads, "heads");
+  }
+  A.positions = pointer<const int32_t>(&need(array(a[5], "positions", kI32, {n}, kv.device), "positions"));
+  const at::Tensor& table = need(array(a[6], "page_table", kI32, {kAny, kAny}, kv.device), "page_table");
+  const at::Tensor* freq = array(a[7], "inv_freq", kF64, {kAny}, kv.device);
+  A.inv_freq = pointer<const double>(freq);
+  A.seqs = pointer<const int32_t>(array(a[8], "seqs", kI32, {n}, kv.device));
+  A.page_table = pointer<const int32_t>(&table);
+  A.table_stride = table.stride(0);
+  A.dtype = type;
+  A.tokens = i32(n, "tokens");
+  A.n_seqs = i32(table.size(0), "sequences");
+  A.table_width = i32(table.size(1), "page_table");
+  A.rotary_dim = freq ? i32(2 * freq->size(0), "inv_freq") : 0;
+  A.interleaved = PyObject_IsTrue(a[10]);
+  if (A.interleaved < 0) {
+    PyErr_Clear();
+    refuse("interleaved: need True or False");
+  }
+  return A;
+}
+
+// (kv .. interleaved, stream)
 PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return guarded([&]() -> int32_t {
     if (n_args != 12) refuse("paged_append: 12 arguments");
     const Kv kv(a[0], a[1]);
-    const int64_t hk = kv.view->n_kv_heads, d = kv.view->head_dim;
-    const at::Tensor& k0 = tensor(a[3], "k");
-    const int type = type_of(k0, "k");
-    const int64_t n = k0.dim() ? k0.size(0) : 0;
-    const at::Tensor& k = head_rows(a[3], "k", type, n, hk, d, kv.device);
-    const at::Tensor& v = head_rows(a[4], "v", type, n, hk, d, kv.device);
-    emoe_paged_append_args A{};
-    A.k = k.data_ptr();
-    A.k_stride = k.stride(0);
-    A.v = v.data_ptr();
-    A.v_stride = v.stride(0);
-    if (a[2] != Py_None) {
-      const at::Tensor& q0 = tensor(a[2], "q");
-      const int64_t heads = q0.dim() == 3 ? q0.size(1) : 0;
-      const at::Tensor& q = head_rows(a[2], "q", type, n, heads, d, kv.device);
-      const at::Tensor& q_out = a[9] == Py_None ? q : head_rows(a[9], "q_out", type, n, heads, d, kv.device);
-      A.q = q.data_ptr();
-      A.q_stride = q.stride(0);
-      A.q_out = q_out.data_ptr();
-      A.q_out_stride = q_out.stride(0);
-      A.n_heads = i32(heads, "heads");
-    }
-    A.positions = pointer<const int32_t>(&need(array(a[5], "positions", kI32, {n}, kv.device), "positions"));
-    const at::Tensor& table = need(array(a[6], "page_table", kI32, {kAny, kAny}, kv.device), "page_table");
-    const at::Tensor* freq = array(a[7], "inv_freq", kF64, {kAny}, kv.device);
-    A.inv_freq = pointer<const double>(freq);
-    A.seqs = pointer<const int32_t>(array(a[8], "seqs", kI32, {n}, kv.device));
-    A.page_table = pointer<const int32_t>(&table);
-    A.table_stride = table.stride(0);
-    A.dtype = type;
-    A.tokens = i32(n, "tokens");
-    A.n_seqs = i32(table.size(0), "sequences");
-    A.table_width = i32(table.size(1), "page_table");
-    A.rotary_dim = freq ? i32(2 * freq->size(0), "inv_freq") : 0;
-    A.interleaved = PyObject_IsTrue(a[10]);
-    if (A.interleaved < 0) {
-      PyErr_Clear();
-      refuse("interleaved: need True or False");
-    }
+    const emoe_paged_append_args A = append_args(kv, a);
     return on_device(kv.device, g_append, kv.view, &A, stream_of(a[11]));
+  });
+}
+
+// (kv .. interleaved, angles, axes, stream)
+PyObject* paged_append_axes(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return guarded([&]() -> int32_t {
+    if (n_args != 14) refuse("paged_append_axes: 14 arguments");
+    const Kv kv(a[0], a[1]);
+    const emoe_paged_append_args A = append_args(kv, a);
+    const at::Tensor& angles = need(array(a[11], "angles", kI32, {A.tokens, kAny}, kv.device), "angles");
+    emoe_paged_axes X{};
+    X.angles = pointer<const int32_t>(&angles);
+    X.axes = pointer<const int32_t>(array(a[12], "axes", kI32, {A.rotary_dim / 2}, kv.device));
+    X.angle_stride = angles.stride(0);
+    X.n_axes = i32(angles.size(1), "angles");
+    return on_device(kv.device, g_append_axes, kv.view, &A, &X, stream_of(a[13]));
   });
 }
 
@@ -376,15 +407,179 @@ PyObject* decoder_forward_paged(PyObject*, PyObject* const* a, Py_ssize_t n_args
   });
 }
 
+float real(PyObject* o, const char* name) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) {
+    PyErr_Clear();
+    refuse(std::string(name) + ": need a number");
+  }
+  return (float)v;
+}
+
+// (kv, device, q, page_table, lengths, out, workspace, max_keys, max_nodes, tree, starts, seqs, scale, cap,
+//  slopes, window, lse, stream)
+PyObject* paged_tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return guarded([&]() -> int32_t {
+    if (n_args != 18) refuse("paged_tree_attention: 18 arguments");
+    const Kv kv(a[0], a[1]);
+    const at::Tensor& q0 = tensor(a[2], "q");
+    const int type = type_of(q0, "q");
+    if (q0.dim() != 3) refuse("q: need 3 axes, got shape " + shape_text(q0));
+    const int64_t rows = q0.size(0), heads = q0.size(1), d = kv.view->head_dim;
+    const at::Tensor& q = head_rows(a[2], "q", type, rows, heads, d, kv.device);
+    const at::Tensor& table = need(array(a[3], "page_table", kI32, {kAny, kAny}, kv.device), "page_table");
+    const at::Tensor& lengths = need(array(a[4], "lengths", kI32, {kAny}, kv.device), "lengths");
+    const int64_t trees = lengths.size(0);
+    const at::Tensor& out = head_rows(a[5], "out", type, rows, heads, d, kv.device);
+    const at::Tensor* lse = array(a[16], "lse", EMOE_F32, {rows, heads}, kv.device);
+    if (lse && !lse->is_contiguous()) refuse("lse must be contiguous");
+    const Workspace ws(a[6], kv.device);
+    emoe_paged_tree_args A{};
+    A.q = q.data_ptr();
+    A.out = out.data_ptr();
+    A.lse = pointer<float>(lse);
+    A.lengths = pointer<const int32_t>(&lengths);
+    A.tree = pointer<const uint64_t>(array(a[9], "tree", kI64, {rows}, kv.device));
+    A.starts = pointer<const int32_t>(array(a[10], "starts", kI32, {trees + 1}, kv.device));
+    A.seqs = pointer<const int32_t>(array(a[11], "seqs", kI32, {trees}, kv.device));
+    A.slopes = pointer<const float>(array(a[14], "slopes", EMOE_F32, {heads}, kv.device));
+    A.page_table = pointer<const int32_t>(&table);
+    A.q_stride = q.stride(0);
+    A.out_stride = out.stride(0);
+    A.table_stride = table.stride(0);
+    A.scale = real(a[12], "scale");
+    A.cap = real(a[13], "cap");
+    A.dtype = type;
+    A.rows = i32(rows, "rows");
+    A.trees = i32(trees, "trees");
+    A.n_heads = i32(heads, "heads");
+    A.n_seqs = i32(table.size(0), "sequences");
+    A.table_width = i32(table.size(1), "page_table");
+    A.max_keys = i32(number(a[7], "max_keys"), "max_keys");
+    A.max_nodes = i32(number(a[8], "max_nodes"), "max_nodes");
+    A.window = i32(number(a[15], "window"), "window");
+    return on_device(kv.device, g_tree, kv.view, &A, ws.p, ws.bytes, stream_of(a[17]));
+  });
+}
+
+// (tokens, chosen, lengths, path, accepted, new_tokens, new_lengths, tree, starts, stream)
+PyObject* accept_drafts(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return guarded([&]() -> int32_t {
+    if (n_args != 10) refuse("accept_drafts: 10 arguments");
+    const at::Tensor& t0 = tensor(a[0], "tokens");
+    if (!t0.is_cuda()) refuse("tokens is on " + t0.device().str());
+    const int device = t0.device().index();
+    const at::Tensor& tokens = need(array(a[0], "tokens", kI32, {kAny}, device), "tokens");
+    const int64_t rows = tokens.size(0);
+    const at::Tensor& path = need(array(a[3], "path", kI32, {kAny, kAny}, device), "path");
+    const int64_t trees = path.size(0), nodes = path.size(1);
+    const at::Tensor* made = array(a[5], "new_tokens", kI32, {trees, nodes}, device);
+    emoe_accept_args A{};
+    A.tokens = pointer<const int32_t>(&tokens);
+    A.chosen = pointer<const int32_t>(&need(array(a[1], "chosen", kI32, {rows}, device), "chosen"));
+    A.lengths = pointer<const int32_t>(array(a[2], "lengths", kI32, {trees}, device));
+    A.path = pointer<int32_t>(&path);
+    A.accepted = pointer<int32_t>(&need(array(a[4], "accepted", kI32, {trees}, device), "accepted"));
+    A.new_tokens = pointer<int32_t>(made);
+    A.new_lengths = pointer<int32_t>(array(a[6], "new_lengths", kI32, {trees}, device));
+    A.tree = pointer<const uint64_t>(array(a[7], "tree", kI64, {rows}, device));
+    A.starts = pointer<const int32_t>(array(a[8], "starts", kI32, {trees + 1}, device));
+    A.path_stride = path.stride(0);
+    A.new_tokens_stride = made ? made->stride(0) : 0;
+    A.rows = i32(rows, "rows");
+    A.trees = i32(trees, "trees");
+    A.max_nodes = i32(nodes, "path");
+    return on_device(device, g_accept, &A, stream_of(a[9]));
+  });
+}
+
+// The caches of a sequence of PagedKV, all on `device`.
+std::vector<emoe_paged_kv> layers(PyObject* o, int device) {
+  if (!PyList_Check(o) && !PyTuple_Check(o)) refuse("kvs: need a list of PagedKV");
+  const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+  std::vector<emoe_paged_kv> out;
+  out.reserve((size_t)n);
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    PyObject* item = PySequence_Fast_GET_ITEM(o, i);
+    PyObject* address = PyObject_GetAttrString(item, "address");
+    PyObject* index = address ? PyObject_GetAttrString(item, "index") : nullptr;
+    int64_t at = 0, dev = -1;
+    const bool good = index && PyLong_Check(address) && PyLong_Check(index);
+    if (good) {
+      at = PyLong_AsLongLong(address);
+      dev = PyLong_AsLongLong(index);
+    }
+    Py_XDECREF(address);
+    Py_XDECREF(index);
+    PyErr_Clear();
+    if (!good) refuse("kvs: need a list of PagedKV");
+    if (dev != device) refuse("kvs: caches on more than one device");
+    out.push_back(*reinterpret_cast<const emoe_paged_kv*>(at));
+  }
+  return out;
+}
+
+// (kvs, device, page_table, lengths, path, accepted, seqs, stream)
+PyObject* paged_compact(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return guarded([&]() -> int32_t {
+    if (n_args != 8) refuse("paged_compact: 8 arguments");
+    const int device = (int)number(a[1], "device");
+    const std::vector<emoe_paged_kv> kvs = layers(a[0], device);
+    const at::Tensor& table = need(array(a[2], "page_table", kI32, {kAny, kAny}, device), "page_table");
+    const at::Tensor& path = need(array(a[4], "path", kI32, {kAny, kAny}, device), "path");
+    const int64_t trees = path.size(0);
+    emoe_compact_args A{};
+    A.lengths = pointer<const int32_t>(&need(array(a[3], "lengths", kI32, {trees}, device), "lengths"));
+    A.path = pointer<const int32_t>(&path);
+    A.accepted = pointer<const int32_t>(&need(array(a[5], "accepted", kI32, {trees}, device), "accepted"));
+    A.seqs = pointer<const int32_t>(array(a[6], "seqs", kI32, {trees}, device));
+    A.page_table = pointer<const int32_t>(&table);
+    A.path_stride = path.stride(0);
+    A.table_stride = table.stride(0);
+    A.trees = i32(trees, "trees");
+    A.max_nodes = i32(path.size(1), "path");
+    A.n_seqs = i32(table.size(0), "sequences");
+    A.table_width = i32(table.size(1), "page_table");
+    return on_device(device, g_compact, kvs.data(), (int32_t)kvs.size(), &A, stream_of(a[7]));
+  });
+}
+
+// (kvs, device, page_table, parents, lengths, fresh, new_table, stream)
+PyObject* paged_fork(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return guarded([&]() -> int32_t {
+    if (n_args != 8) refuse("paged_fork: 8 arguments");
+    const int device = (int)number(a[1], "device");
+    const std::vector<emoe_paged_kv> kvs = layers(a[0], device);
+    const at::Tensor& table = need(array(a[2], "page_table", kI32, {kAny, kAny}, device), "page_table");
+    const at::Tensor& parents = need(array(a[3], "parents", kI32, {kAny}, device), "parents");
+    const int64_t forks = parents.size(0);
+    const at::Tensor& to = need(array(a[6], "new_table", kI32, {forks, table.size(1)}, device), "new_table");
+    emoe_fork_args A{};
+    A.page_table = pointer<const int32_t>(&table);
+    A.parents = pointer<const int32_t>(&parents);
+    A.lengths = pointer<const int32_t>(&need(array(a[4], "lengths", kI32, {forks}, device), "lengths"));
+    A.fresh = pointer<const int32_t>(array(a[5], "fresh", kI32, {forks}, device));
+    A.new_table = pointer<int32_t>(&to);
+    A.table_stride = table.stride(0);
+    A.new_table_stride = to.stride(0);
+    A.forks = i32(forks, "forks");
+    A.n_seqs = i32(table.size(0), "sequences");
+    A.table_width = i32(table.size(1), "page_table");
+    return on_device(device, g_fork, kvs.data(), (int32_t)kvs.size(), &A, stream_of(a[7]));
+  });
+}
+
 // (error class, addresses of emoe_last_error, _paged_append, _paged_attention, _process_logits,
-//  _decoder_forward_paged)
+//  _decoder_forward_paged, _paged_append_axes, _paged_tree_attention, _accept_drafts, _paged_compact,
+//  _paged_fork)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
-  if (n_args != 6) {
-    PyErr_SetString(PyExc_TypeError, "init: 6 arguments");
+  constexpr int kCalls = 10;
+  if (n_args != 1 + kCalls) {
+    PyErr_SetString(PyExc_TypeError, "init: 11 arguments");
     return nullptr;
   }
-  uintptr_t at[5];
-  for (int i = 0; i < 5; ++i) {
+  uintptr_t at[kCalls];
+  for (int i = 0; i < kCalls; ++i) {
     at[i] = (uintptr_t)PyLong_AsUnsignedLongLong(a[1 + i]);
     if (PyErr_Occurred()) return nullptr;
   }
@@ -396,12 +591,19 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   g_attention = reinterpret_cast<decltype(g_attention)>(at[2]);
   g_logits = reinterpret_cast<decltype(g_logits)>(at[3]);
   g_decoder = reinterpret_cast<decltype(g_decoder)>(at[4]);
+  g_append_axes = reinterpret_cast<decltype(g_append_axes)>(at[5]);
+  g_tree = reinterpret_cast<decltype(g_tree)>(at[6]);
+  g_accept = reinterpret_cast<decltype(g_accept)>(at[7]);
+  g_compact = reinterpret_cast<decltype(g_compact)>(at[8]);
+  g_fork = reinterpret_cast<decltype(g_fork)>(at[9]);
   Py_RETURN_NONE;
 }
 
 #define FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(init),           FAST(paged_append),          FAST(paged_attention),
-                         FAST(process_logits), FAST(decoder_forward_paged), {nullptr, nullptr, 0, nullptr}};
+                         FAST(process_logits), FAST(decoder_forward_paged),
+                         FAST(paged_append_axes), FAST(paged_tree_attention), FAST(accept_drafts),
+                         FAST(paged_compact),  FAST(paged_fork), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,766 @@
+// The attention of trees of drafted tokens over a paged cache
+// (exactmoe_drafts.h): its kernels, which tree_bf16.hip and tree_fp16.hip build for
+// their types.
+#pragma once
+
+#include "exactmoe_drafts.h"
+#include "paged.h"
+
+namespace emoe {
+
+struct TreeArg {
+  KvView kv;
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;
+  const int32_t *lengths, *starts, *seqs, *table;
+  const uint64_t* tree;
+  const float* slopes;
+  int32_t* heads_of;  // of each output that workgroups share: first worker, parts, place in its first
+  float* parts;
+  int64_t q_stride, out_stride, table_stride;
+  float scale, cap;
+  int32_t tree0, trees, rows, n_heads, group, blocks, n_seqs, table_width, max_keys, max_nodes, window;
+  int32_t workers, least_run;  // workers 0: a workgroup to every output
+  int32_t part_floats;
+};
+
+// How a call is launched (tree.hip chooses): tiles of 16 columns that a wavefront
+// holds, and the rest as in TreeArg.
+struct TreePlan {
+  int64_t trees_per_launch;
+  int tiles, blocks, lines, workers, least_run, part_floats, stripes;
+  int64_t most_parts, most_shared;
+};
+
+void launch_tree_bf16(const TreeArg& a, const TreePlan& p, int head_dim, bool e4m3, hipStream_t stream);
+void launch_tree_fp16(const TreeArg& a, const TreePlan& p, int head_dim, bool e4m3, hipStream_t stream);
+
+constexpr int kTreeWaves = 4;
+
+// A tree: its rows, and the keys [first, end) that some node of it may see, of
+// which those from n on are its nodes.
+struct TreeSpan {
+  int start, count, seq, n, first, end;
+};
+__device__ __forceinline__ TreeSpan tree_span(const TreeArg& a, int g) {
+  TreeSpan s;
+  int64_t count = a.max_nodes;
+  if (a.starts) {
+    s.start = a.starts[g];
+    count = (int64_t)a.starts[g + 1] - s.start;
+    if (s.start < 0 || s.start > a.rows) s.start = a.rows;
+  } else {
+    s.start = g * a.max_nodes;
+  }
+  s.count = (int)max((int64_t)0, min(count, (int64_t)min(a.max_nodes, a.rows - s.start)));
+  s.seq = a.seqs ? a.seqs[g] : g;
+  s.n = min(a.lengths[g], 1 << 30);
+  s.first = s.end = 0;
+  if ((uint32_t)s.seq < (uint32_t)a.n_seqs && s.n >= 0) {
+    const int64_t most = min((int64_t)a.max_keys, (int64_t)a.table_width << a.kv.page_log2);
+    s.end = (int)min((int64_t)s.n + s.count, most);
+    s.first = a.window > 0 ? min(s.end, max(0, s.n + 1 - a.window)) : 0;
+  }
+  return s;
+}
+// Units of its column block cb, of a tile for each wavefront; one that sees no key
+// has one, which writes its zeros.
+__device__ __forceinline__ int tree_units(const TreeArg& a, const TreeSpan& s, int columns, int cb) {
+  if (s.count * a.group <= cb * columns) return 0;
+  const int tiles = (s.end + kTileKeys - 1) / kTileKeys - s.first / kTileKeys;
+  return max(1, (tiles + kTreeWaves - 1) / kTreeWaves);
+}
+
+// tanh to a few units of fp32's rounding everywhere: its series where
+// 1 - 2 / (1 + e^2y) would cancel.
+__device__ __forceinline__ float tanh_of(float y) {
+  const float a = fabsf(y), t = exp2_hw(a * -2.8853900817779268f);
+  const float far = (1.f - t) * __builtin_amdgcn_rcpf(1.f + t);
+  const float z = y * y;
+  float s = fmaf(z, 21844.f / 6081075.f, -1382.f / 155925.f);
+  s = fmaf(z, s, 62.f / 2835.f);
+  s = fmaf(z, s, -17.f / 315.f);
+  s = fmaf(z, s, 2.f / 15.f);
+  s = fmaf(z, s, -1.f / 3.f);
+  const float near = fmaf(a * z, s, a);
+  return copysignf(a < 0.3f ? near : far, y);
+}
+
+// Tile (paged.h) for kTiles tiles of 16 columns, so that what is made of keys and
+// values (trades between lanes, conversions, transposes) is made once for all.
+template <class T, bool kE4M3, int kDh, int kTiles>
+struct WideTile : Tile<T, kE4M3, kDh> {
+  typedef Tile<T, kE4M3, kDh> B;
+  typedef typename B::H16 H16;
+  typedef typename B::HW HW;
+
+  __device__ __forceinline__ void wide_scores(const uint4 (&q)[kTiles][B::kSteps], bool second,
+                                              f32x4 (&s)[kTiles][2]) const {
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) s[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < B::kPairs; ++p)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t c0[B::kChunkWords], c1[B::kChunkWords];
+#pragma unroll
+        for (int w = 0; w < B::kChunkWords; ++w) {
+          const uint32_t a = this->k[2 * h][p][w], b = this->k[2 * h + 1][p][w];
+          const uint32_t a2 = __builtin_amdgcn_update_dpp(0, (int)a, 0x4E, 0xF, 0xF, true);
+          const uint32_t b2 = __builtin_amdgcn_update_dpp(0, (int)b, 0x4E, 0xF, 0xF, true);
+          c0[w] = second ? b2 : a;
+          c1[w] = second ? b : a2;
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int sub = 0; sub < B::kSub; ++sub) {
+            const uint32_t(&c)[B::kChunkWords] = half ? c1 : c0;
+            uint4 x;
+            if constexpr (kE4M3) {
+              const uint32_t lo = c[2 * sub], hi = c[2 * sub + 1];
+              x = make_uint4(H16::template from_e4m3<false>(lo), H16::template from_e4m3<true>(lo),
+                             H16::template from_e4m3<false>(hi), H16::template from_e4m3<true>(hi));
+            } else {
+              x = make_uint4(c[0], c[1], c[2], c[3]);
+            }
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n)
+              s[n][h] = H16::mfma(x, q[n][(2 * p + half) * B::kSub + sub], s[n][h]);
+          }
+      }
+  }
+
+  template <int kW>
+  __device__ __forceinline__ void wide_add(const uint4 (&hi)[kTiles], const uint4 (&lo)[kTiles],
+                                           f32x4 (&acc)[kTiles][B::kDims]) const {
+    uint32_t e[4], o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t a = this->template pair<kW>(2 * i), b = this->template pair<kW>(2 * i + 1);
+      e[i] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+      o[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    }
+    const uint4 ve = make_uint4(e[0], e[1], e[2], e[3]), vo = make_uint4(o[0], o[1], o[2], o[3]);
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+      acc[n][2 * kW] = HW::mfma(ve, hi[n], acc[n][2 * kW]);
+      acc[n][2 * kW + 1] = HW::mfma(vo, hi[n], acc[n][2 * kW + 1]);
+    }
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+      acc[n][2 * kW] = HW::mfma(ve, lo[n], acc[n][2 * kW]);
+      acc[n][2 * kW + 1] = HW::mfma(vo, lo[n], acc[n][2 * kW + 1]);
+    }
+    if constexpr (kW + 1 < B::kDims / 2) wide_add<kW + 1>(hi, lo, acc);
+  }
+
+  // Which of a lane's 8 keys have an infinity or a NaN among its values.
+  __device__ __forceinline__ uint32_t not_finite() const {
+    constexpr uint32_t kExp = kE4M3 ? 0x7f7f7f7fu : (T::kType == EMOE_F16 ? 0x7c007c00u : 0x7f807f80u);
+    uint32_t bad = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int w = 0; w < B::kVWords; ++w) {
+        const uint32_t x = this->v[j][w] & kExp;
+        if constexpr (kE4M3) {
+#pragma unroll
+          for (int b = 0; b < 32; b += 8) bad |= ((x >> b) & 0x7fu) == 0x7fu ? 1u << j : 0u;
+        } else {
+          bad |= (x & 0xffffu) == (kExp & 0xffffu) || (x >> 16) == (kExp >> 16) ? 1u << j : 0u;
+        }
+      }
+    return bad;
+  }
+};
+
+// One value of the cache, as the formula takes it (before v_scale).
+template <class T, bool kE4M3>
+__device__ __forceinline__ float cache_value(const uint8_t* at) {
+  if constexpr (kE4M3) {
+    const uint32_t pair = Half16<Bf16>::from_e4m3<false>((uint32_t)*at);
+    return bf16_to_f32(pair & 0xffffu);
+  } else {
+    return T::up(*reinterpret_cast<const uint16_t*>(at));
+  }
+}
+
+// A column is a query head of a key head's group, of one node: column c is node
+// c / group, head c % group.  A workgroup takes a block of 16 * kTiles columns of a
+// tree and a run of its keys, each wavefront every fourth tile of 32 keys, for all
+// columns of the block; statistics and outputs of a column stay in the lanes of its
+// own (Tile says how).  The softmax runs once over the keys with a running maximum.
+//
+// Runs: the units of all trees stand behind each other and every worker takes the
+// same number of them, wherever trees begin and end.  Outputs that a worker covers
+// whole it writes; of the others (its first and its last at most) it leaves maximum,
+// sum and unscaled output in the workspace, which tree_join_kernel joins.
+//
+// A tile that all columns see whole has nothing masked.  In the others (the tree's
+// own keys, the window's edge, missing pages) a weight of 0 would not undo an
+// infinity or a NaN among the values, which the columns share: keys with such
+// values are cleared from the product and added by themselves, to the columns that
+// see them.
+template <class T, bool kE4M3, int kDh, int kTiles, bool kShaped>
+__global__ __launch_bounds__(64 * kTreeWaves, kTiles * kDh >= 512 || kDh == 256 ? 1 : 2)
+void paged_tree_kernel(TreeArg a) {
+  constexpr int kWaves = kTreeWaves, kThreads = 64 * kWaves, kColumns = 16 * kTiles;
+  typedef WideTile<T, kE4M3, kDh, kTiles> Tl;
+  constexpr float kLead = Tl::kF16Weights ? 7.f : 0.f;
+  constexpr int kRow = kDh + 4;  // padded: lanes 16 apart in dimensions, 1 in columns
+  __shared__ float ms[kWaves][kColumns], ls[kWaves][kColumns];
+  __shared__ __attribute__((aligned(16))) float os[kWaves][16][kRow];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, g4 = lane >> 4;
+  const uint32_t k_off = Tl::k_offset(lane, a.kv.slot_bytes);
+  const uint32_t v_off = Tl::v_offset(lane, a.kv.slot_bytes);
+
+  // Blocks of one key head and run are 8 workgroups apart, on one die, so that its L2
+  // serves what the others read again.
+  const int chunk = blockIdx.x / (8 * a.blocks), at = blockIdx.x % (8 * a.blocks);
+  const int runs = a.workers ? a.workers : a.trees;
+  const int pairs = min(8, runs * a.kv.n_kv_heads - 8 * chunk);
+  const int pair = 8 * chunk + at % pairs, cb = at / pairs;
+  const int w = pair / a.kv.n_kv_heads, hk = pair % a.kv.n_kv_heads;
+  const int lines = a.kv.n_kv_heads * a.blocks, y = hk * a.blocks + cb;
+
+  // The trees of a chunk of 64, one per lane.
+  int c0 = 0;
+  TreeSpan mine;
+  int mine_units = 0;
+  auto load_chunk = [&]() {
+    mine_units = 0;
+    mine = TreeSpan{0, 0, 0, 0, 0, 0};
+    if (c0 + lane < a.trees) {
+      mine = tree_span(a, a.tree0 + c0 + lane);
+      mine_units = tree_units(a, mine, kColumns, cb);
+    }
+  };
+  int run = 1, u = 0, u_end = 1, base = 0, tr = 0;  // units, and the first of tree tr's
+  if (a.workers) {
+    int total = 0;
+    for (c0 = 0; c0 < a.trees; c0 += 64) {
+      load_chunk();
+      total += __builtin_amdgcn_readlane(wave_scan(mine_units), 63);
+    }
+    run = max(a.least_run, (total + a.workers - 1) / a.workers);
+    if ((int64_t)w * run >= total) return;  // the same for the whole workgroup
+    u = w * run;
+    u_end = min(u + run, total);
+    for (c0 = 0;; c0 += 64) {
+      if (a.trees > 64) load_chunk();
+      else c0 = 0;
+      const int incl = wave_scan(mine_units), all = __builtin_amdgcn_readlane(incl, 63);
+      if (u < base + all) {
+        const int i = (int)__builtin_ctzll(__ballot(u < base + incl));
+        base += __builtin_amdgcn_readlane(incl - mine_units, i);
+        tr = c0 + i;
+        break;
+      }
+      base += all;
+    }
+  } else {
+    tr = w;
+    c0 = tr & ~63;
+    load_chunk();
+    if (__builtin_amdgcn_readlane(mine_units, tr & 63) == 0) return;
+  }
+
+  float scale = a.scale;
+  if (!kShaped) scale *= 1.4426950408889634f;
+  if (kE4M3 && a.kv.k_scale) scale *= a.kv.k_scale[hk];
+  const float vs = kE4M3 && a.kv.v_scale ? a.kv.v_scale[hk] : 1.f;
+  const float inv_cap = kShaped && a.cap > 0.f ? 1.f / a.cap : 0.f;
+  const uint8_t* kbase = a.kv.k + (int64_t)hk * a.kv.head_bytes;
+  const uint8_t* vbase = a.kv.v + (int64_t)hk * a.kv.head_bytes;
+  const int slot_mask = (1 << a.kv.page_log2) - 1;
+  bool first_segment = true;
+
+  for (; u < u_end; ++tr) {
+    if (tr - c0 >= 64) {
+      c0 = tr & ~63;
+      load_chunk();
+    }
+    const int i64 = __builtin_amdgcn_readfirstlane(tr - c0);
+    const int all_units = __builtin_amdgcn_readlane(mine_units, i64);
+    if (all_units == 0) continue;
+    const int start = __builtin_amdgcn_readlane(mine.start, i64);
+    const int count = __builtin_amdgcn_readlane(mine.count, i64);
+    const int sq = __builtin_amdgcn_readlane(mine.seq, i64);
+    const int n = __builtin_amdgcn_readlane(mine.n, i64);
+    const int first = __builtin_amdgcn_readlane(mine.first, i64);
+    const int end = __builtin_amdgcn_readlane(mine.end, i64);
+    const int units = a.workers ? all_units : 1;
+    const int s0 = u - base, s1 = min(units, s0 + (u_end - u));
+    const int columns = min(kColumns, count * a.group - cb * kColumns);
+
+    // What each node sees, and its depth: node i's in lane i.
+    uint64_t sees = 0;
+    if (lane < count)
+      sees = a.tree ? a.tree[start + lane] : (2ull << lane) - 1;
+    const int depth = __popcll(sees & ((1ull << lane) - 1));
+    const int deepest = a.window > 0 ? (int)wave_reduce_u32<true>((uint32_t)(lane < count ? depth : 0)) : 0;
+
+    // This lane's columns: node, and what belongs to it.
+    int node[kTiles];
+    float slope[kTiles];
+    uint4 q[kTiles][Tl::kSteps];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+      const int c = 16 * i + l16, col = cb * kColumns + c;
+      node[i] = c < columns ? (int)((uint32_t)col / (uint32_t)a.group) : 0;
+      const int head = hk * a.group + (c < columns ? col - node[i] * a.group : 0);
+      slope[i] = 0.f;
+      if (kShaped && a.slopes) slope[i] = a.slopes[head] * 1.4426950408889634f;
+#pragma unroll
+      for (int s = 0; s < Tl::kSteps; ++s) {
+        q[i][s] = make_uint4(0, 0, 0, 0);
+        if (c < columns)
+          q[i][s] = *reinterpret_cast<const uint4*>(a.q + (int64_t)(start + node[i]) * a.q_stride +
+                                                    (int64_t)head * kDh + Tl::q_dim(s, g4));
+      }
+    }
+    f32x4 acc[kTiles][Tl::kDims];
+    float m[kTiles], l[kTiles];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < Tl::kDims; ++c) acc[i][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    const int t0 = first / kTileKeys, t_all = (end + kTileKeys - 1) / kTileKeys;
+    const int t_end = a.workers ? min(t0 + s1 * kWaves, t_all) : t_all;
+    int t = t0 + s0 * kWaves + wave;
+    const ConstI32 table = (ConstI32)(a.table + (int64_t)sq * a.table_stride);
+    // Keys of a tile that every column sees lie between these.
+    const int low = a.window > 0 ? max(0, n + deepest + 1 - a.window) : 0, high = min(n, end);
+
+    auto place = [&](const Octets& o, int key0, int64_t (&off)[4]) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int page = (uint32_t)o.page[i] < (uint32_t)a.kv.n_pages ? o.page[i] : 0;
+        off[i] = page * a.kv.page_bytes + (int64_t)((key0 + 8 * i) & slot_mask) * a.kv.slot_bytes;
+      }
+    };
+    Tl tile;
+    auto load_k = [&](const int64_t (&off)[4]) {
+      const uint8_t* const p[4] = {kbase + off[0], kbase + off[1], kbase + off[2], kbase + off[3]};
+      tile.load_k(p, k_off);
+    };
+    auto load_v = [&](const int64_t (&off)[4]) {
+      const uint8_t* const p[4] = {vbase + off[0], vbase + off[1], vbase + off[2], vbase + off[3]};
+      tile.load_v(p, a.kv.slot_bytes, v_off);
+    };
+
+    Octets now, next;
+    int64_t off[4];
+    if (t < t_end) {
+      now = octets_of(a.kv, table, t * kTileKeys, end);
+      place(now, t * kTileKeys, off);
+      load_k(off);
+      load_v(off);
+      if (t + kWaves < t_end) next = octets_of(a.kv, table, (t + kWaves) * kTileKeys, end);
+    }
+    while (t < t_end) {
+      const int key0 = t * kTileKeys, tn = t + kWaves;
+      const bool more = tn < t_end;
+      f32x4 s[kTiles][2];
+      tile.wide_scores(q, (lane & 2) != 0, s);
+      if (more) {
+        place(next, tn * kTileKeys, off);
+        load_k(off);
+      }
+      bool whole = key0 >= low && key0 + kTileKeys <= high;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) whole = whole && (uint32_t)now.page[i] < (uint32_t)a.kv.n_pages;
+      auto key_of = [&](int j, int group) { return key0 + 8 * (j >> 1) + 2 * group + (j & 1); };
+      // Whether a node with this mask and depth sees a key of the tile that has a page.
+      auto sees_key = [&](uint64_t mask, int deep, int key, int key_depth) -> bool {
+        bool yes = key < n || ((mask >> ((key - n) & 63)) & 1);
+        if (a.window > 0) yes = yes && (key < n ? key - n : key_depth) > deep - a.window;
+        return yes;
+      };
+      float z[kTiles][8];
+      if constexpr (kShaped) {
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) z[i][j] = s[i][j >> 2][j & 3] * scale;
+        if (a.cap > 0.f) {
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[i][j] = a.cap * tanh_of(z[i][j] * inv_cap);
+        }
+        int key_at[8];  // the keys' positions, from n on
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int key = key_of(j, g4), deep = __shfl(depth, (key - n) & 63);
+          key_at[j] = key < n ? key - n : deep;
+        }
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+          const int deep = __shfl(depth, node[i]);
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            z[i][j] = fmaf(-slope[i], (float)abs(deep - key_at[j]), z[i][j] * 1.4426950408889634f);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) z[i][j] = s[i][j >> 2][j & 3] * scale;
+      }
+      uint32_t there = 0xff, bad = 0;
+      if (!whole) {
+        there = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int key = key_of(j, g4);
+          if (key >= first && key < end && (uint32_t)now.page[j >> 1] < (uint32_t)a.kv.n_pages)
+            there |= 1u << j;
+        }
+        bad = tile.not_finite() & there;
+        bad |= __shfl_xor(bad, 1);
+        bad |= __shfl_xor(bad, 2);
+        bad |= __shfl_xor(bad, 4);
+        bad |= __shfl_xor(bad, 8);
+        tile.clear_v(there & ~bad);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int key = key_of(j, g4), key_depth = __shfl(depth, (key - n) & 63);
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i) {
+            const uint64_t mask = __shfl(sees, node[i]);
+            const int deep = __shfl(depth, node[i]);
+            if (!((there >> j) & 1) || !sees_key(mask, deep, key, key_depth)) z[i][j] = -INFINITY;
+          }
+        }
+      }
+      // The exponent that a column's weights refer to follows the maximum only when a
+      // score exceeds it by 8: until then they stay below 2^(8 + kLead).
+      float p[kTiles][8];
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) {
+        float top = z[i][0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) top = fmaxf(top, z[i][j]);
+        if (__any(top > m[i] + (8.f + kLead))) {
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float m2 = fmaxf(m[i], top - kLead);
+          const float shrink = m2 == -INFINITY ? 0.f : exp2_hw(m[i] - m2);
+          m[i] = m2;
+          l[i] *= shrink;
+#pragma unroll
+          for (int c = 0; c < Tl::kDims; ++c) acc[i][c] *= shrink;
+        }
+        const float ref = m[i] == -INFINITY ? 0.f : m[i];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          p[i][j] = exp2_hw(z[i][j] - ref);
+          l[i] += p[i][j];
+        }
+      }
+      if (__any(bad != 0)) {
+        // Key by key, its values from memory: lanes hold dimensions of their own.
+        for (int x = 0; x < 32; ++x) {
+          const int j = x & 7, kg = x >> 3, key = key_of(j, kg);
+          if (!((__builtin_amdgcn_readlane((int)bad, 16 * kg) >> j) & 1)) continue;
+          const int page = j >> 1 == 0 ? now.page[0] : j >> 1 == 1 ? now.page[1] : j >> 1 == 2 ? now.page[2] : now.page[3];
+          const uint8_t* row = vbase + page * a.kv.page_bytes + (int64_t)(key & slot_mask) * a.kv.slot_bytes;
+          const int key_depth = __shfl(depth, (key - n) & 63);
+          float weight[kTiles];
+          bool seen[kTiles];
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i) {
+            float mine_p = p[i][0];
+#pragma unroll
+            for (int k = 1; k < 8; ++k) mine_p = j == k ? p[i][k] : mine_p;
+            weight[i] = __shfl(mine_p, 16 * kg + l16);
+            const uint64_t mask = __shfl(sees, node[i]);
+            seen[i] = sees_key(mask, __shfl(depth, node[i]), key, key_depth);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < Tl::kDims; ++c) {
+              const float v = cache_value<T, kE4M3>(row + Tl::out_dim(4 * g4 + r, c) * Tl::kItem);
+#pragma unroll
+              for (int i = 0; i < kTiles; ++i)
+                acc[i][c][r] = seen[i] ? fmaf(weight[i], v, acc[i][c][r]) : acc[i][c][r];
+            }
+        }
+      }
+      // Weights as two 16-bit halves; small fp16 weights in turns of their own, 2^24
+      // and 2^48 times as large, as in paged_attention_kernel.
+      float lift = 1.f;
+      while (true) {
+        bool rest = false;
+        float part[kTiles][8];
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) part[i][j] = p[i][j];
+        if constexpr (Tl::kF16Weights) {
+          uint32_t least = ~0u;  // the bits, less 1, of the smallest weight above 0
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) least = min(least, __float_as_uint(p[i][j]) - 1u);
+          rest = __any(least < __float_as_uint(0x1p-9f) - 1u);
+          if (rest) {
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                const bool small = p[i][j] < 0x1p-9f;
+                part[i][j] = small ? 0.f : p[i][j];
+                p[i][j] = small ? p[i][j] * 0x1p24f : 0.f;
+              }
+          }
+        }
+        uint4 hi[kTiles], lo[kTiles];
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+          typedef typename Tl::W W;
+          uint32_t h[4], r[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t h0 = W::down(part[i][2 * j]), h1 = W::down(part[i][2 * j + 1]);
+            h[j] = h0 | (h1 << 16);
+            r[j] = W::down(part[i][2 * j] - W::up(h0)) | (W::down(part[i][2 * j + 1] - W::up(h1)) << 16);
+          }
+          hi[i] = make_uint4(h[0], h[1], h[2], h[3]);
+          lo[i] = make_uint4(r[0], r[1], r[2], r[3]);
+        }
+        tile.template wide_add<0>(hi, lo, acc);
+        if (!rest || lift == 0x1p48f) break;
+        tile.transpose_again();
+        lift *= 0x1p24f;
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+          for (int c = 0; c < Tl::kDims; ++c) acc[i][c] *= 0x1p24f;
+      }
+      if (lift != 1.f) {
+        const float back = lift == 0x1p24f ? 0x1p-24f : 0x1p-48f;
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+          for (int c = 0; c < Tl::kDims; ++c) acc[i][c] *= back;
+      }
+      if (more) {
+        load_v(off);
+        now = next;
+        if (tn + kWaves < t_end) next = octets_of(a.kv, table, (tn + kWaves) * kTileKeys, end);
+      }
+      t = tn;
+    }
+
+    // Join the wavefronts, a tile of columns at a time.
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+      l[i] += __shfl_xor(l[i], 16);
+      l[i] += __shfl_xor(l[i], 32);
+    }
+    __syncthreads();  // the last segment's readers are done
+    if (g4 == 0) {
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) {
+        ms[wave][16 * i + l16] = m[i];
+        ls[wave][16 * i + l16] = l[i];
+      }
+    }
+    __syncthreads();
+    const bool full = s0 == 0 && s1 == units;
+    float* part = a.parts + (int64_t)(2 * (w * lines + y) + (first_segment ? 0 : 1)) * a.part_floats;
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+      if (16 * i >= columns) break;
+      if (i > 0) __syncthreads();
+      float M = ms[0][16 * i + l16];
+#pragma unroll
+      for (int v = 1; v < kWaves; ++v) M = fmaxf(M, ms[v][16 * i + l16]);
+      const float f = part_weight(m[i], M);
+#pragma unroll
+      for (int c = 0; c < Tl::kDims; c += 4)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          *reinterpret_cast<float4*>(&os[wave][l16][Tl::out_dim(4 * g4 + r, c)]) =
+              make_float4(acc[i][c][r] * f, acc[i][c + 1][r] * f, acc[i][c + 2][r] * f, acc[i][c + 3][r] * f);
+      __syncthreads();
+      for (int x = tid; x < min(16, columns - 16 * i) * (kDh / 4); x += kThreads) {
+        const int h = x / (kDh / 4), d = 4 * (x % (kDh / 4)), c = 16 * i + h;
+        float4 o = *reinterpret_cast<const float4*>(&os[0][h][d]);
+#pragma unroll
+        for (int v = 1; v < kWaves; ++v) {
+          const float4 e = *reinterpret_cast<const float4*>(&os[v][h][d]);
+          o.x += e.x, o.y += e.y, o.z += e.z, o.w += e.w;
+        }
+        float top = ms[0][c], sum = 0.f;
+#pragma unroll
+        for (int v = 1; v < kWaves; ++v) top = fmaxf(top, ms[v][c]);
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) sum += ls[v][c] * part_weight(ms[v][c], top);
+        if (full) {
+          const int col = cb * kColumns + c, nd = (int)((uint32_t)col / (uint32_t)a.group);
+          const int64_t row = start + nd;
+          const int head = hk * a.group + col - nd * a.group;
+          const float inv = sum == 0.f ? 0.f : vs / sum;
+          uint2 r;
+          r.x = T::down(o.x * inv) | (T::down(o.y * inv) << 16);
+          r.y = T::down(o.z * inv) | (T::down(o.w * inv) << 16);
+          *reinterpret_cast<uint2*>(a.out + row * a.out_stride + (int64_t)head * kDh + d) = r;
+          if (d == 0 && a.lse)
+            a.lse[row * a.n_heads + head] =
+                sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+        } else {
+          *reinterpret_cast<float4*>(part + 2 * kColumns + c * kDh + d) = o;
+          if (d == 0) {
+            part[c] = top;
+            part[kColumns + c] = sum;
+          }
+        }
+      }
+    }
+    if (a.workers && s0 == 0 && tid == 0) {
+      int32_t* h = a.heads_of + 3 * ((int64_t)tr * lines + y);
+      h[0] = w;
+      h[1] = full ? 0 : (base + units - 1) / run - w + 1;
+      h[2] = first_segment ? 0 : 1;
+    }
+    u += s1 - s0;
+    base += units;
+    first_segment = false;
+  }
+}
+
+// Joins the parts of an output that workers shared, kStripes threads to four
+// dimensions of a column, each over every kStripes-th part.  Reads 4 bytes a column,
+// dimension and part, and writes the output.
+template <class T, bool kE4M3, int kDh, int kStripes>
+__global__ __launch_bounds__(256) void tree_join_kernel(TreeArg a, int tiles) {
+  __shared__ float4 so[256];
+  __shared__ float sm[256], sl[256];
+  constexpr int kItems = 256 / kStripes, kFours = kDh / 4;
+  const int columns = 16 * tiles, pieces = columns * kFours / kItems, lines = a.kv.n_kv_heads * a.blocks;
+  const int64_t output = blockIdx.x / pieces;
+  const int piece = blockIdx.x % pieces, tr = (int)(output / lines), y = (int)(output % lines);
+  const int hk = y / a.blocks, cb = y % a.blocks;
+  const TreeSpan s = tree_span(a, a.tree0 + tr);
+  if (s.count * a.group <= cb * columns) return;
+  const int32_t* h = a.heads_of + 3 * output;
+  const int w = h[0], parts = h[1], lead = h[2];
+  if (parts == 0) return;
+  const int item = piece * kItems + threadIdx.x % kItems, stripe = threadIdx.x / kItems;
+  const int c = item / kFours, d = 4 * (item % kFours), col = cb * columns + c;
+  float M = -INFINITY, L = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  constexpr int kAhead = 8;
+  if (col < s.count * a.group) {
+    for (int i0 = stripe; i0 < parts; i0 += kAhead * kStripes) {
+      float m_of[kAhead], l_of[kAhead];
+      float4 e[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int i = min(i0 + k * kStripes, parts - 1);
+        const float* p = a.parts + (2 * ((int64_t)(w + i) * lines + y) + (i == 0 ? lead : 0)) * a.part_floats;
+        m_of[k] = p[c];
+        l_of[k] = p[columns + c];
+        e[k] = *reinterpret_cast<const float4*>(p + 2 * columns + c * kDh + d);
+      }
+      float top = M;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (i0 + k * kStripes >= parts) {  // past the end: nothing (an infinity times 0 is not)
+          m_of[k] = -INFINITY;
+          l_of[k] = 0.f;
+          e[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        top = fmaxf(top, m_of[k]);
+      }
+      const float shrink = part_weight(M, top);
+      M = top;
+      L *= shrink;
+      o.x *= shrink, o.y *= shrink, o.z *= shrink, o.w *= shrink;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const float f = part_weight(m_of[k], M);
+        L = fmaf(f, l_of[k], L);
+        o.x = fmaf(f, e[k].x, o.x), o.y = fmaf(f, e[k].y, o.y);
+        o.z = fmaf(f, e[k].z, o.z), o.w = fmaf(f, e[k].w, o.w);
+      }
+    }
+  }
+  if constexpr (kStripes > 1) {
+    so[threadIdx.x] = o;
+    sm[threadIdx.x] = M;
+    sl[threadIdx.x] = L;
+    __syncthreads();
+    if (stripe != 0) return;
+    M = sm[threadIdx.x];
+    for (int i = 1; i < kStripes; ++i) M = fmaxf(M, sm[threadIdx.x + i * kItems]);
+    L = 0.f;
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < kStripes; ++i) {
+      const int x = threadIdx.x + i * kItems;
+      const float f = part_weight(sm[x], M);
+      L = fmaf(f, sl[x], L);
+      o.x = fmaf(f, so[x].x, o.x), o.y = fmaf(f, so[x].y, o.y);
+      o.z = fmaf(f, so[x].z, o.z), o.w = fmaf(f, so[x].w, o.w);
+    }
+  }
+  if (col >= s.count * a.group) return;
+  const int nd = (int)((uint32_t)col / (uint32_t)a.group), head = hk * a.group + col - nd * a.group;
+  const int64_t row = s.start + nd;
+  const float vs = kE4M3 && a.kv.v_scale ? a.kv.v_scale[hk] : 1.f, inv = L == 0.f ? 0.f : vs / L;
+  uint2 r;
+  r.x = T::down(o.x * inv) | (T::down(o.y * inv) << 16);
+  r.y = T::down(o.z * inv) | (T::down(o.w * inv) << 16);
+  *reinterpret_cast<uint2*>(a.out + row * a.out_stride + (int64_t)head * kDh + d) = r;
+  if (d == 0 && a.lse)
+    a.lse[row * a.n_heads + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+}
+
+template <class T, bool kE4M3, int kDh, int kTiles>
+void launch_tree_tiles(const TreeArg& a, const TreePlan& p, hipStream_t stream) {
+  const int64_t runs = a.workers ? a.workers : a.trees;
+  const dim3 grid((unsigned)(runs * p.lines)), block(64 * kTreeWaves);
+  if (a.cap > 0.f || a.slopes)
+    hipLaunchKernelGGL((paged_tree_kernel<T, kE4M3, kDh, kTiles, true>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((paged_tree_kernel<T, kE4M3, kDh, kTiles, false>), grid, block, 0, stream, a);
+  if (!a.workers) return;
+  const int64_t outputs = (int64_t)a.trees * p.lines, items = 16 * kTiles * (kDh / 4);
+  if (p.stripes == 4)
+    hipLaunchKernelGGL((tree_join_kernel<T, kE4M3, kDh, 4>), dim3((unsigned)(outputs * items / 64)),
+                       dim3(256), 0, stream, a, kTiles);
+  else
+    hipLaunchKernelGGL((tree_join_kernel<T, kE4M3, kDh, 1>), dim3((unsigned)(outputs * items / 256)),
+                       dim3(256), 0, stream, a, kTiles);
+}
+
+template <class T, bool kE4M3>
+void launch_tree(const TreeArg& a, const TreePlan& p, int head_dim, hipStream_t stream) {
+  if (head_dim == 256) {
+    if (p.tiles == 1) launch_tree_tiles<T, kE4M3, 256, 1>(a, p, stream);
+    else launch_tree_tiles<T, kE4M3, 256, 2>(a, p, stream);
+  } else if (head_dim == 128) {
+    if (p.tiles == 1) launch_tree_tiles<T, kE4M3, 128, 1>(a, p, stream);
+    else if (p.tiles == 2) launch_tree_tiles<T, kE4M3, 128, 2>(a, p, stream);
+    else launch_tree_tiles<T, kE4M3, 128, 4>(a, p, stream);
+  } else {
+    if (p.tiles == 1) launch_tree_tiles<T, kE4M3, 64, 1>(a, p, stream);
+    else if (p.tiles == 2) launch_tree_tiles<T, kE4M3, 64, 2>(a, p, stream);
+    else launch_tree_tiles<T, kE4M3, 64, 4>(a, p, stream);
+  }
+}
+
+}  // namespace emoe

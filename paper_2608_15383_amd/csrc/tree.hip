@@ -1,0 +1,132 @@
+// Attention of trees of drafted tokens over a paged cache (exactmoe_drafts.h): the
+// call's checks and how it is launched.  The kernels are in tree.h.
+#include "tree.h"
+
+using namespace emoe;
+
+namespace {
+
+constexpr int kPlaces = 512, kWholeKeys = 256, kManyOutputs = 1024;
+
+TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int32_t max_keys,
+                   int32_t max_nodes, int32_t window) {
+  TreePlan p;
+  const int64_t columns = (int64_t)(n_heads / kv.n_kv_heads) * max_nodes;
+  const int most_tiles = kv.head_dim == 256 ? 2 : 4;
+  p.tiles = columns <= 16 ? 1 : columns <= 32 || most_tiles == 2 ? 2 : 4;
+  p.blocks = (int)((columns + 16 * p.tiles - 1) / (16 * p.tiles));
+  p.lines = kv.n_kv_heads * p.blocks;
+  const int64_t span = (int64_t)window + max_nodes;
+  const int64_t keys = window > 0 && span < max_keys ? span : max_keys;
+  const int64_t most_units = keys / (kTreeWaves * kTileKeys) + 2;
+  const int64_t outputs = (int64_t)trees * p.lines;
+  const bool two = p.tiles * kv.head_dim < 512 && kv.head_dim < 256;  // workgroups on a CU
+  const int places = two ? kPlaces : kPlaces / 2;
+  const bool whole = keys <= kWholeKeys || outputs >= kManyOutputs || p.lines > places;
+  p.workers = whole ? 0 : places / p.lines;
+  p.least_run = 1;
+  p.part_floats = 16 * p.tiles * (2 + kv.head_dim);
+  p.stripes = outputs * 16 * p.tiles * (kv.head_dim / 4) / 256 < 1024 ? 4 : 1;
+  // A launch's units stay below 2^31, its threads below 2^32.
+  p.trees_per_launch = (((int64_t)1 << 31) - 1 - kPlaces) / most_units;
+  const int64_t most_outputs = whole ? (int64_t)1 << 23 : kManyOutputs;
+  if (p.trees_per_launch > most_outputs / p.lines) p.trees_per_launch = most_outputs / p.lines;
+  p.most_parts = whole ? 0 : 2 * (int64_t)p.workers * p.lines;
+  p.most_shared = whole ? 0 : outputs;
+  return p;
+}
+
+size_t shared_bytes(const TreePlan& p) { return ((size_t)p.most_shared * 12 + 15) / 16 * 16; }
+
+}  // namespace
+
+extern "C" {
+
+size_t emoe_paged_tree_attention_workspace_bytes(const emoe_paged_kv* kv, int32_t trees,
+                                                 int32_t n_heads, int32_t max_keys,
+                                                 int32_t max_nodes) {
+  if (check_kv(kv) || trees < 0 || n_heads < 1 || n_heads % kv->n_kv_heads || max_keys < 0 ||
+      max_keys > kMostKeys || n_heads > kMostHeads || max_nodes < 1 || max_nodes > EMOE_MAX_NODES)
+    return 0;
+  const TreePlan p = tree_plan(*kv, trees, n_heads, max_keys, max_nodes, 0);
+  return 16 + shared_bytes(p) + (size_t)p.most_parts * p.part_floats * 4;
+}
+
+int32_t emoe_paged_tree_attention(const emoe_paged_kv* kv, const emoe_paged_tree_args* args,
+                                  void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  int32_t st = check_kv(kv);
+  if (st) return st;
+  if (!args) return report_error(EMOE_EINVAL, "args is NULL");
+  const emoe_paged_tree_args& A = *args;
+  if ((st = check_io(*kv, A.dtype, A.page_table, A.n_seqs, A.table_width, A.table_stride))) return st;
+  if (A.rows < 0 || A.trees < 0 || A.max_keys < 0 || A.window < 0)
+    return report_error(EMOE_EINVAL, "negative rows, trees, max_keys or window (%d, %d, %d, %d)", A.rows,
+                        A.trees, A.max_keys, A.window);
+  if (A.max_nodes < 1 || A.max_nodes > EMOE_MAX_NODES)
+    return report_error(EMOE_ESHAPE, "max_nodes %d: need 1 to %d", A.max_nodes, EMOE_MAX_NODES);
+  if (A.n_heads < 1 || A.n_heads % kv->n_kv_heads)
+    return report_error(EMOE_ESHAPE, "n_heads %d is no multiple of n_kv_heads %d", A.n_heads,
+                        kv->n_kv_heads);
+  if (A.max_keys > kMostKeys || A.n_heads > kMostHeads)
+    return report_error(EMOE_ESHAPE, "max_keys %d or n_heads %d: need at most 2^30 and 2^20", A.max_keys,
+                        A.n_heads);
+  if (!A.starts && A.rows != (int64_t)A.trees * A.max_nodes)
+    return report_error(EMOE_ESHAPE, "%d rows without starts: need %d trees of %d nodes", A.rows, A.trees,
+                        A.max_nodes);
+  if (!std::isfinite(A.scale * 1.4426950408889634f))  // as the kernel takes it
+    return report_error(EMOE_EINVAL, "scale %g is not finite, or near the largest number", A.scale);
+  if (!(A.cap == 0.f || (A.cap >= 0x1p-60f && A.cap <= 0x1p60f)))
+    return report_error(EMOE_EINVAL, "cap %g: need 0 (none) or 2^-60 to 2^60", A.cap);
+  if (A.rows == 0 || A.trees == 0) return EMOE_OK;
+  const int64_t qw = (int64_t)A.n_heads * kv->head_dim;
+  if ((st = check_rows("q", A.q, A.q_stride, A.rows, qw))) return st;
+  if ((st = check_rows("out", A.out, A.out_stride, A.rows, qw))) return st;
+  if (!A.lengths) return report_error(EMOE_EINVAL, "lengths is NULL");
+  const size_t bytes =
+      emoe_paged_tree_attention_workspace_bytes(kv, A.trees, A.n_heads, A.max_keys, A.max_nodes);
+  if (!workspace || workspace_bytes < bytes)
+    return report_error(EMOE_EINVAL, "workspace of %zu bytes < %zu needed", workspace ? workspace_bytes : 0,
+                        bytes);
+  if (!aligned16(workspace)) return report_error(EMOE_EINVAL, "workspace: need 16-byte alignment");
+  const TreePlan plan = tree_plan(*kv, A.trees, A.n_heads, A.max_keys, A.max_nodes, A.window);
+  TreeArg a;
+  a.kv = view_of(*kv);
+  a.q = static_cast<const uint16_t*>(A.q);
+  a.out = static_cast<uint16_t*>(A.out);
+  a.lse = A.lse;
+  a.lengths = A.lengths;
+  a.starts = A.starts;
+  a.seqs = A.seqs;
+  a.tree = A.tree;
+  a.slopes = A.slopes;
+  a.table = A.page_table;
+  a.heads_of = static_cast<int32_t*>(workspace);
+  a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + shared_bytes(plan));
+  a.q_stride = A.q_stride;
+  a.out_stride = A.out_stride;
+  a.table_stride = A.table_stride;
+  a.scale = A.scale;
+  a.cap = A.cap;
+  a.rows = A.rows;
+  a.n_heads = A.n_heads;
+  a.group = A.n_heads / kv->n_kv_heads;
+  a.blocks = plan.blocks;
+  a.n_seqs = A.n_seqs;
+  a.table_width = A.table_width;
+  a.max_keys = A.max_keys;
+  a.max_nodes = A.max_nodes;
+  a.window = A.window;
+  a.workers = plan.workers;
+  a.least_run = plan.least_run;
+  a.part_floats = plan.part_floats;
+  for (int64_t t0 = 0; t0 < A.trees; t0 += plan.trees_per_launch) {
+    a.tree0 = (int32_t)t0;
+    a.trees = (int32_t)(A.trees - t0 < plan.trees_per_launch ? A.trees - t0 : plan.trees_per_launch);
+    if (A.dtype == EMOE_BF16) launch_tree_bf16(a, plan, kv->head_dim, kv->dtype == EMOE_E4M3, stream);
+    else launch_tree_fp16(a, plan, kv->head_dim, kv->dtype == EMOE_E4M3, stream);
+    if ((st = launched("paged_tree_kernel"))) return st;
+  }
+  return EMOE_OK;
+}
+
+}  // extern "C"
