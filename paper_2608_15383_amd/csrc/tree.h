@@ -22,14 +22,16 @@ struct TreeArg {
   float scale, cap;
   int32_t tree0, trees, rows, n_heads, group, blocks, n_seqs, table_width, max_keys, max_nodes, window;
   int32_t workers, least_run;  // workers 0: a workgroup to every output
+  int32_t unit_keys, unit_log2;
   int32_t part_floats;
 };
 
-// How a call is launched (tree.hip chooses): tiles of 16 columns that a wavefront
-// holds, and the rest as in TreeArg.
+// How a call is launched (tree.hip chooses): the tiles of 16 columns of a block, and the
+// rest as in TreeArg.
 struct TreePlan {
   int64_t trees_per_launch;
-  int tiles, blocks, lines, workers, least_run, part_floats, stripes;
+  bool wide;  // paged_tree_wide_kernel
+  int tiles, blocks, lines, workers, least_run, part_floats, stripes, unit_keys;
   int64_t most_parts, most_shared;
 };
 
@@ -64,27 +66,42 @@ __device__ __forceinline__ TreeSpan tree_span(const TreeArg& a, int g) {
   }
   return s;
 }
-// Units of its column block cb, of a tile for each wavefront; one that sees no key
-// has one, which writes its zeros.
-__device__ __forceinline__ int tree_units(const TreeArg& a, const TreeSpan& s, int columns, int cb) {
-  if (s.count * a.group <= cb * columns) return 0;
-  const int tiles = (s.end + kTileKeys - 1) / kTileKeys - s.first / kTileKeys;
-  return max(1, (tiles + kTreeWaves - 1) / kTreeWaves);
+// Units (of unit_keys keys) of each of its column blocks; a tree that sees no key has
+// one, which writes its zeros.
+__device__ __forceinline__ int tree_units(const TreeArg& a, const TreeSpan& s) {
+  return max(1, ((s.end + a.unit_keys - 1) >> a.unit_log2) - (s.first >> a.unit_log2));
 }
 
-// tanh to a few units of fp32's rounding everywhere: its series where
-// 1 - 2 / (1 + e^2y) would cancel.
-__device__ __forceinline__ float tanh_of(float y) {
-  const float a = fabsf(y), t = exp2_hw(a * -2.8853900817779268f);
-  const float far = (1.f - t) * __builtin_amdgcn_rcpf(1.f + t);
-  const float z = y * y;
-  float s = fmaf(z, 21844.f / 6081075.f, -1382.f / 155925.f);
-  s = fmaf(z, s, 62.f / 2835.f);
-  s = fmaf(z, s, -17.f / 315.f);
-  s = fmaf(z, s, 2.f / 15.f);
-  s = fmaf(z, s, -1.f / 3.f);
-  const float near = fmaf(a * z, s, a);
-  return copysignf(a < 0.3f ? near : far, y);
+// x = cap * tanh(x / cap), to a few units of fp32's rounding: below 0.3 by tanh's
+// series (1 - 2 / (1 + e^2y) would cancel), which alone serves a wavefront whose
+// scores are all that small beside the cap.
+__device__ __forceinline__ void cap_scores(float (&x)[8], float cap, float inv_cap) {
+  float most = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    x[j] *= inv_cap;
+    most = fmaxf(most, fabsf(x[j]));
+  }
+  float far[8];
+  const bool any_far = __any(!(most < 0.3f));
+  if (any_far) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float t = exp2_hw(fabsf(x[j]) * -2.8853900817779268f);
+      far[j] = copysignf((1.f - t) * __builtin_amdgcn_rcpf(1.f + t), x[j]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float y = x[j], z = y * y;
+    float s = fmaf(z, 21844.f / 6081075.f, -1382.f / 155925.f);
+    s = fmaf(z, s, 62.f / 2835.f);
+    s = fmaf(z, s, -17.f / 315.f);
+    s = fmaf(z, s, 2.f / 15.f);
+    s = fmaf(z, s, -1.f / 3.f);
+    const float near = fmaf(y * z, s, y);
+    x[j] = cap * (any_far && !(fabsf(y) < 0.3f) ? far[j] : near);
+  }
 }
 
 // Tile (paged.h) for kTiles tiles of 16 columns, so that what is made of keys and
@@ -189,14 +206,216 @@ __device__ __forceinline__ float cache_value(const uint8_t* at) {
   }
 }
 
+// The scores of a tile in powers of two: capped, and less the bias by distance.
+// key_at[j] is the key's place from the tree's first node on: below 0 its position,
+// else (only if `nodes`) the node, whose depth is in that lane.
+template <int kTiles>
+__device__ __forceinline__ void shape_scores(float (&z)[kTiles][8], float cap, float inv_cap, bool biased,
+                                             const float (&slope)[kTiles], const int (&deep_at)[kTiles],
+                                             int (&key_at)[8], bool nodes, int depth) {
+  if (cap > 0.f) {
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) cap_scores(z[i], cap, inv_cap);
+  }
+  if (biased && nodes) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int deep = __shfl(depth, key_at[j] & 63);
+      key_at[j] = key_at[j] < 0 ? key_at[j] : deep;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      z[i][j] *= 1.4426950408889634f;
+      if (biased) z[i][j] = fmaf(-slope[i], (float)abs(deep_at[i] - key_at[j]), z[i][j]);
+    }
+}
+
+// Whether a node with this mask and depth sees the key at key_at (as above, its own
+// depth key_depth) that has a page.
+__device__ __forceinline__ bool node_sees(uint64_t mask, int deep, int key_at, int key_depth, int window) {
+  bool yes = key_at < 0 || ((mask >> (key_at & 63)) & 1);
+  if (window > 0) yes = yes && (key_at < 0 ? key_at : key_depth) > deep - window;
+  return yes;
+}
+
+// One tile's step of the softmax: z to weights p.  The exponent that a column's
+// weights refer to follows the maximum only when a score exceeds it by 8: until then
+// they stay below 2^(8 + lead).  fp16 weights begin at 2^7: there is room above, but
+// little below.
+template <class Tl, int kTiles>
+__device__ __forceinline__ void soft_step(const float (&z)[kTiles][8], float (&m)[kTiles], float (&l)[kTiles],
+                                          f32x4 (&acc)[kTiles][Tl::kDims], float (&p)[kTiles][8]) {
+  constexpr float kLead = Tl::kF16Weights ? 7.f : 0.f;
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    float top = z[i][0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) top = fmaxf(top, z[i][j]);
+    if (__any(top > m[i] + (8.f + kLead))) {
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float m2 = fmaxf(m[i], top - kLead);
+      const float shrink = m2 == -INFINITY ? 0.f : exp2_hw(m[i] - m2);
+      m[i] = m2;
+      l[i] *= shrink;
+#pragma unroll
+      for (int c = 0; c < Tl::kDims; ++c) acc[i][c] *= shrink;
+    }
+    const float ref = m[i] == -INFINITY ? 0.f : m[i];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      p[i][j] = exp2_hw(z[i][j] - ref);
+      l[i] += p[i][j];
+    }
+  }
+}
+
+// Adds the weighted values.  Weights as two 16-bit halves; small fp16 weights in turns
+// of their own, 2^24 and 2^48 times as large, as in paged_attention_kernel.
+template <class Tl, int kTiles>
+__device__ __forceinline__ void add_weighted(Tl& tile, float (&p)[kTiles][8], f32x4 (&acc)[kTiles][Tl::kDims]) {
+  typedef typename Tl::W W;
+  float lift = 1.f;
+  while (true) {
+    bool rest = false;
+    float part[kTiles][8];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) part[i][j] = p[i][j];
+    if constexpr (Tl::kF16Weights) {
+      uint32_t least = ~0u;  // the bits, less 1, of the smallest weight above 0
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) least = min(least, __float_as_uint(p[i][j]) - 1u);
+      rest = __any(least < __float_as_uint(0x1p-9f) - 1u);
+      if (rest) {
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const bool small = p[i][j] < 0x1p-9f;
+            part[i][j] = small ? 0.f : p[i][j];
+            p[i][j] = small ? p[i][j] * 0x1p24f : 0.f;
+          }
+      }
+    }
+    uint4 hi[kTiles], lo[kTiles];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+      uint32_t h[4], r[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t h0 = W::down(part[i][2 * j]), h1 = W::down(part[i][2 * j + 1]);
+        h[j] = h0 | (h1 << 16);
+        r[j] = W::down(part[i][2 * j] - W::up(h0)) | (W::down(part[i][2 * j + 1] - W::up(h1)) << 16);
+      }
+      hi[i] = make_uint4(h[0], h[1], h[2], h[3]);
+      lo[i] = make_uint4(r[0], r[1], r[2], r[3]);
+    }
+    tile.template wide_add<0>(hi, lo, acc);
+    if (!rest || lift == 0x1p48f) break;
+    tile.transpose_again();
+    lift *= 0x1p24f;
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int c = 0; c < Tl::kDims; ++c) acc[i][c] *= 0x1p24f;
+  }
+  if (lift != 1.f) {
+    const float back = lift == 0x1p24f ? 0x1p-24f : 0x1p-48f;
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int c = 0; c < Tl::kDims; ++c) acc[i][c] *= back;
+  }
+}
+
+// Adds one key's values, which are at `row`, weighted by p of lane group kg's key j, to
+// the columns that see it: lanes hold dimensions of their own.
+template <class T, bool kE4M3, class Tl, int kTiles>
+__device__ __forceinline__ void add_one_key(const uint8_t* row, int j, int kg, const float (&p)[kTiles][8],
+                                            const bool (&seen)[kTiles], f32x4 (&acc)[kTiles][Tl::kDims]) {
+  const int lane = lane_id(), l16 = lane & 15, g4 = lane >> 4;
+  float weight[kTiles];
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    float own = p[i][0];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) own = j == k ? p[i][k] : own;
+    weight[i] = __shfl(own, 16 * kg + l16);
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int c = 0; c < Tl::kDims; ++c) {
+      const float v = cache_value<T, kE4M3>(row + Tl::out_dim(4 * g4 + r, c) * Tl::kItem);
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) acc[i][c][r] = seen[i] ? fmaf(weight[i], v, acc[i][c][r]) : acc[i][c][r];
+      asm volatile("" ::: "memory");  // one load after the other: this is rare, registers are not to spare
+    }
+}
+
+// Locates a worker's run: the units of all blocks of all trees stand behind each
+// other.  The trees of a chunk of 64 are kept one per lane.
+struct TreeChunk {
+  TreeSpan span;
+  int first, units, blocks;
+
+  __device__ __forceinline__ void load(const TreeArg& a, int c0, int columns) {
+    first = c0;
+    units = blocks = 0;
+    span = TreeSpan{0, 0, 0, 0, 0, 0};
+    if (c0 + lane_id() < a.trees) {
+      span = tree_span(a, a.tree0 + c0 + lane_id());
+      units = tree_units(a, span);
+      blocks = (span.count * a.group + columns - 1) / columns;
+    }
+  }
+};
+struct TreeRun {
+  int run, u, u_end, base, tr, cb;  // units; the first one of block cb of tree tr
+};
+__device__ __forceinline__ bool find_run(const TreeArg& a, int w, int columns, TreeChunk& ch, TreeRun& r) {
+  int total = 0;
+  for (int c0 = 0; c0 < a.trees; c0 += 64) {
+    ch.load(a, c0, columns);
+    total += __builtin_amdgcn_readlane(wave_scan(ch.units * ch.blocks), 63);
+  }
+  r.run = max(a.least_run, (total + a.workers - 1) / a.workers);
+  if ((int64_t)w * r.run >= total) return false;
+  r.u = w * r.run;
+  r.u_end = min(r.u + r.run, total);
+  r.base = 0;
+  for (int c0 = 0;; c0 += 64) {
+    if (a.trees > 64) ch.load(a, c0, columns);
+    const int own = ch.units * ch.blocks, incl = wave_scan(own);
+    const int all = __builtin_amdgcn_readlane(incl, 63);
+    if (r.u < r.base + all) {
+      const int i = (int)__builtin_ctzll(__ballot(r.u < r.base + incl));
+      r.base += __builtin_amdgcn_readlane(incl - own, i);
+      const int units = __builtin_amdgcn_readlane(ch.units, i);
+      r.cb = (r.u - r.base) / units;
+      r.base += r.cb * units;
+      r.tr = c0 + i;
+      return true;
+    }
+    r.base += all;
+  }
+}
+
 // A column is a query head of a key head's group, of one node: column c is node
 // c / group, head c % group.  A workgroup takes a block of 16 * kTiles columns of a
 // tree and a run of its keys, each wavefront every fourth tile of 32 keys, for all
 // columns of the block; statistics and outputs of a column stay in the lanes of its
 // own (Tile says how).  The softmax runs once over the keys with a running maximum.
 //
-// Runs: the units of all trees stand behind each other and every worker takes the
-// same number of them, wherever trees begin and end.  Outputs that a worker covers
+// Runs: the units of all blocks of all trees stand behind each other and every worker
+// of a key head takes the same number of them, wherever blocks begin and end.  Outputs that a worker covers
 // whole it writes; of the others (its first and its last at most) it leaves maximum,
 // sum and unscaled output in the workspace, which tree_join_kernel joins.
 //
@@ -206,11 +425,10 @@ __device__ __forceinline__ float cache_value(const uint8_t* at) {
 // values are cleared from the product and added by themselves, to the columns that
 // see them.
 template <class T, bool kE4M3, int kDh, int kTiles, bool kShaped>
-__global__ __launch_bounds__(64 * kTreeWaves, kTiles * kDh >= 512 || kDh == 256 ? 1 : 2)
+__global__ __launch_bounds__(64 * kTreeWaves, kDh == 256 ? 1 : 2)
 void paged_tree_kernel(TreeArg a) {
   constexpr int kWaves = kTreeWaves, kThreads = 64 * kWaves, kColumns = 16 * kTiles;
   typedef WideTile<T, kE4M3, kDh, kTiles> Tl;
-  constexpr float kLead = Tl::kF16Weights ? 7.f : 0.f;
   constexpr int kRow = kDh + 4;  // padded: lanes 16 apart in dimensions, 1 in columns
   __shared__ float ms[kWaves][kColumns], ls[kWaves][kColumns];
   __shared__ __attribute__((aligned(16))) float os[kWaves][16][kRow];
@@ -219,55 +437,28 @@ void paged_tree_kernel(TreeArg a) {
   const uint32_t k_off = Tl::k_offset(lane, a.kv.slot_bytes);
   const uint32_t v_off = Tl::v_offset(lane, a.kv.slot_bytes);
 
-  // Blocks of one key head and run are 8 workgroups apart, on one die, so that its L2
-  // serves what the others read again.
-  const int chunk = blockIdx.x / (8 * a.blocks), at = blockIdx.x % (8 * a.blocks);
-  const int runs = a.workers ? a.workers : a.trees;
-  const int pairs = min(8, runs * a.kv.n_kv_heads - 8 * chunk);
-  const int pair = 8 * chunk + at % pairs, cb = at / pairs;
-  const int w = pair / a.kv.n_kv_heads, hk = pair % a.kv.n_kv_heads;
-  const int lines = a.kv.n_kv_heads * a.blocks, y = hk * a.blocks + cb;
-
-  // The trees of a chunk of 64, one per lane.
-  int c0 = 0;
-  TreeSpan mine;
-  int mine_units = 0;
-  auto load_chunk = [&]() {
-    mine_units = 0;
-    mine = TreeSpan{0, 0, 0, 0, 0, 0};
-    if (c0 + lane < a.trees) {
-      mine = tree_span(a, a.tree0 + c0 + lane);
-      mine_units = tree_units(a, mine, kColumns, cb);
-    }
-  };
-  int run = 1, u = 0, u_end = 1, base = 0, tr = 0;  // units, and the first of tree tr's
+  // Workers of several key heads stand next to each other, as their keys do in memory.
+  // Where every output has a workgroup, a tree's blocks of one key head are 8 apart, on
+  // one die, so that its L2 serves what the others read again.
+  int w, hk, cb = 0;
   if (a.workers) {
-    int total = 0;
-    for (c0 = 0; c0 < a.trees; c0 += 64) {
-      load_chunk();
-      total += __builtin_amdgcn_readlane(wave_scan(mine_units), 63);
-    }
-    run = max(a.least_run, (total + a.workers - 1) / a.workers);
-    if ((int64_t)w * run >= total) return;  // the same for the whole workgroup
-    u = w * run;
-    u_end = min(u + run, total);
-    for (c0 = 0;; c0 += 64) {
-      if (a.trees > 64) load_chunk();
-      else c0 = 0;
-      const int incl = wave_scan(mine_units), all = __builtin_amdgcn_readlane(incl, 63);
-      if (u < base + all) {
-        const int i = (int)__builtin_ctzll(__ballot(u < base + incl));
-        base += __builtin_amdgcn_readlane(incl - mine_units, i);
-        tr = c0 + i;
-        break;
-      }
-      base += all;
-    }
+    w = blockIdx.x / a.kv.n_kv_heads;
+    hk = blockIdx.x % a.kv.n_kv_heads;
   } else {
-    tr = w;
-    c0 = tr & ~63;
-    load_chunk();
-    if (__builtin_amdgcn_readlane(mine_units, tr & 63) == 0) return;
+    const int chunk = blockIdx.x / (8 * a.blocks), at = blockIdx.x % (8 * a.blocks);
+    const int pairs = min(8, a.trees * a.kv.n_kv_heads - 8 * chunk), pair = 8 * chunk + at % pairs;
+    cb = at / pairs;
+    w = pair / a.kv.n_kv_heads;
+    hk = pair % a.kv.n_kv_heads;
+  }
+
+  TreeChunk ch;
+  TreeRun r{1, 0, 1, 0, w, cb};
+  if (a.workers) {
+    if (!find_run(a, w, kColumns, ch, r)) return;  // the same for the whole workgroup
+  } else {
+    ch.load(a, w & ~63, kColumns);
+    if (cb >= __builtin_amdgcn_readlane(ch.blocks, w & 63)) return;
   }
 
   float scale = a.scale;
@@ -280,23 +471,23 @@ void paged_tree_kernel(TreeArg a) {
   const int slot_mask = (1 << a.kv.page_log2) - 1;
   bool first_segment = true;
 
-  for (; u < u_end; ++tr) {
-    if (tr - c0 >= 64) {
-      c0 = tr & ~63;
-      load_chunk();
+  while (r.u < r.u_end) {
+    if (r.tr - ch.first >= 64) ch.load(a, r.tr & ~63, kColumns);
+    const int i64 = __builtin_amdgcn_readfirstlane(r.tr - ch.first);
+    if (r.cb >= __builtin_amdgcn_readlane(ch.blocks, i64)) {
+      r.cb = 0;
+      ++r.tr;
+      continue;
     }
-    const int i64 = __builtin_amdgcn_readfirstlane(tr - c0);
-    const int all_units = __builtin_amdgcn_readlane(mine_units, i64);
-    if (all_units == 0) continue;
-    const int start = __builtin_amdgcn_readlane(mine.start, i64);
-    const int count = __builtin_amdgcn_readlane(mine.count, i64);
-    const int sq = __builtin_amdgcn_readlane(mine.seq, i64);
-    const int n = __builtin_amdgcn_readlane(mine.n, i64);
-    const int first = __builtin_amdgcn_readlane(mine.first, i64);
-    const int end = __builtin_amdgcn_readlane(mine.end, i64);
-    const int units = a.workers ? all_units : 1;
-    const int s0 = u - base, s1 = min(units, s0 + (u_end - u));
-    const int columns = min(kColumns, count * a.group - cb * kColumns);
+    const int start = __builtin_amdgcn_readlane(ch.span.start, i64);
+    const int count = __builtin_amdgcn_readlane(ch.span.count, i64);
+    const int sq = __builtin_amdgcn_readlane(ch.span.seq, i64);
+    const int n = __builtin_amdgcn_readlane(ch.span.n, i64);
+    const int first = __builtin_amdgcn_readlane(ch.span.first, i64);
+    const int end = __builtin_amdgcn_readlane(ch.span.end, i64);
+    const int units = a.workers ? __builtin_amdgcn_readlane(ch.units, i64) : 1;
+    const int s0 = r.u - r.base, s1 = min(units, s0 + (r.u_end - r.u));
+    const int columns = min(kColumns, count * a.group - r.cb * kColumns);
 
     // What each node sees, and its depth: node i's in lane i.
     uint64_t sees = 0;
@@ -308,13 +499,15 @@ void paged_tree_kernel(TreeArg a) {
     // This lane's columns: node, and what belongs to it.
     int node[kTiles];
     float slope[kTiles];
+    int deep_at[kTiles];
     uint4 q[kTiles][Tl::kSteps];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
-      const int c = 16 * i + l16, col = cb * kColumns + c;
+      const int c = 16 * i + l16, col = r.cb * kColumns + c;
       node[i] = c < columns ? (int)((uint32_t)col / (uint32_t)a.group) : 0;
       const int head = hk * a.group + (c < columns ? col - node[i] * a.group : 0);
       slope[i] = 0.f;
+      deep_at[i] = kShaped ? __shfl(depth, node[i]) : 0;
       if (kShaped && a.slopes) slope[i] = a.slopes[head] * 1.4426950408889634f;
 #pragma unroll
       for (int s = 0; s < Tl::kSteps; ++s) {
@@ -380,42 +573,16 @@ void paged_tree_kernel(TreeArg a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) whole = whole && (uint32_t)now.page[i] < (uint32_t)a.kv.n_pages;
       auto key_of = [&](int j, int group) { return key0 + 8 * (j >> 1) + 2 * group + (j & 1); };
-      // Whether a node with this mask and depth sees a key of the tile that has a page.
-      auto sees_key = [&](uint64_t mask, int deep, int key, int key_depth) -> bool {
-        bool yes = key < n || ((mask >> ((key - n) & 63)) & 1);
-        if (a.window > 0) yes = yes && (key < n ? key - n : key_depth) > deep - a.window;
-        return yes;
-      };
       float z[kTiles][8];
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[i][j] = s[i][j >> 2][j & 3] * scale;
       if constexpr (kShaped) {
+        int key_at[8];
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) z[i][j] = s[i][j >> 2][j & 3] * scale;
-        if (a.cap > 0.f) {
-#pragma unroll
-          for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) z[i][j] = a.cap * tanh_of(z[i][j] * inv_cap);
-        }
-        int key_at[8];  // the keys' positions, from n on
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int key = key_of(j, g4), deep = __shfl(depth, (key - n) & 63);
-          key_at[j] = key < n ? key - n : deep;
-        }
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-          const int deep = __shfl(depth, node[i]);
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            z[i][j] = fmaf(-slope[i], (float)abs(deep - key_at[j]), z[i][j] * 1.4426950408889634f);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) z[i][j] = s[i][j >> 2][j & 3] * scale;
+        for (int j = 0; j < 8; ++j) key_at[j] = key_of(j, g4) - n;
+        shape_scores(z, a.cap, inv_cap, a.slopes != nullptr, slope, deep_at, key_at, key0 + kTileKeys > n, depth);
       }
       uint32_t there = 0xff, bad = 0;
       if (!whole) {
@@ -434,128 +601,32 @@ void paged_tree_kernel(TreeArg a) {
         tile.clear_v(there & ~bad);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int key = key_of(j, g4), key_depth = __shfl(depth, (key - n) & 63);
+          const int key_at = key_of(j, g4) - n, key_depth = __shfl(depth, key_at & 63);
 #pragma unroll
           for (int i = 0; i < kTiles; ++i) {
             const uint64_t mask = __shfl(sees, node[i]);
             const int deep = __shfl(depth, node[i]);
-            if (!((there >> j) & 1) || !sees_key(mask, deep, key, key_depth)) z[i][j] = -INFINITY;
+            if (!((there >> j) & 1) || !node_sees(mask, deep, key_at, key_depth, a.window)) z[i][j] = -INFINITY;
           }
         }
       }
-      // The exponent that a column's weights refer to follows the maximum only when a
-      // score exceeds it by 8: until then they stay below 2^(8 + kLead).
       float p[kTiles][8];
-#pragma unroll
-      for (int i = 0; i < kTiles; ++i) {
-        float top = z[i][0];
-#pragma unroll
-        for (int j = 1; j < 8; ++j) top = fmaxf(top, z[i][j]);
-        if (__any(top > m[i] + (8.f + kLead))) {
-          top = fmaxf(top, __shfl_xor(top, 16));
-          top = fmaxf(top, __shfl_xor(top, 32));
-          const float m2 = fmaxf(m[i], top - kLead);
-          const float shrink = m2 == -INFINITY ? 0.f : exp2_hw(m[i] - m2);
-          m[i] = m2;
-          l[i] *= shrink;
-#pragma unroll
-          for (int c = 0; c < Tl::kDims; ++c) acc[i][c] *= shrink;
-        }
-        const float ref = m[i] == -INFINITY ? 0.f : m[i];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          p[i][j] = exp2_hw(z[i][j] - ref);
-          l[i] += p[i][j];
-        }
-      }
+      soft_step<Tl>(z, m, l, acc, p);
       if (__any(bad != 0)) {
-        // Key by key, its values from memory: lanes hold dimensions of their own.
         for (int x = 0; x < 32; ++x) {
           const int j = x & 7, kg = x >> 3, key = key_of(j, kg);
           if (!((__builtin_amdgcn_readlane((int)bad, 16 * kg) >> j) & 1)) continue;
-          const int page = j >> 1 == 0 ? now.page[0] : j >> 1 == 1 ? now.page[1] : j >> 1 == 2 ? now.page[2] : now.page[3];
-          const uint8_t* row = vbase + page * a.kv.page_bytes + (int64_t)(key & slot_mask) * a.kv.slot_bytes;
+          const uint8_t* row = vbase + table[key >> a.kv.page_log2] * a.kv.page_bytes +
+                               (int64_t)(key & slot_mask) * a.kv.slot_bytes;
           const int key_depth = __shfl(depth, (key - n) & 63);
-          float weight[kTiles];
           bool seen[kTiles];
 #pragma unroll
-          for (int i = 0; i < kTiles; ++i) {
-            float mine_p = p[i][0];
-#pragma unroll
-            for (int k = 1; k < 8; ++k) mine_p = j == k ? p[i][k] : mine_p;
-            weight[i] = __shfl(mine_p, 16 * kg + l16);
-            const uint64_t mask = __shfl(sees, node[i]);
-            seen[i] = sees_key(mask, __shfl(depth, node[i]), key, key_depth);
-          }
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int c = 0; c < Tl::kDims; ++c) {
-              const float v = cache_value<T, kE4M3>(row + Tl::out_dim(4 * g4 + r, c) * Tl::kItem);
-#pragma unroll
-              for (int i = 0; i < kTiles; ++i)
-                acc[i][c][r] = seen[i] ? fmaf(weight[i], v, acc[i][c][r]) : acc[i][c][r];
-            }
-        }
-      }
-      // Weights as two 16-bit halves; small fp16 weights in turns of their own, 2^24
-      // and 2^48 times as large, as in paged_attention_kernel.
-      float lift = 1.f;
-      while (true) {
-        bool rest = false;
-        float part[kTiles][8];
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) part[i][j] = p[i][j];
-        if constexpr (Tl::kF16Weights) {
-          uint32_t least = ~0u;  // the bits, less 1, of the smallest weight above 0
-#pragma unroll
           for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) least = min(least, __float_as_uint(p[i][j]) - 1u);
-          rest = __any(least < __float_as_uint(0x1p-9f) - 1u);
-          if (rest) {
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const bool small = p[i][j] < 0x1p-9f;
-                part[i][j] = small ? 0.f : p[i][j];
-                p[i][j] = small ? p[i][j] * 0x1p24f : 0.f;
-              }
-          }
+            seen[i] = node_sees(__shfl(sees, node[i]), __shfl(depth, node[i]), key - n, key_depth, a.window);
+          add_one_key<T, kE4M3, Tl>(row, j, kg, p, seen, acc);
         }
-        uint4 hi[kTiles], lo[kTiles];
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-          typedef typename Tl::W W;
-          uint32_t h[4], r[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t h0 = W::down(part[i][2 * j]), h1 = W::down(part[i][2 * j + 1]);
-            h[j] = h0 | (h1 << 16);
-            r[j] = W::down(part[i][2 * j] - W::up(h0)) | (W::down(part[i][2 * j + 1] - W::up(h1)) << 16);
-          }
-          hi[i] = make_uint4(h[0], h[1], h[2], h[3]);
-          lo[i] = make_uint4(r[0], r[1], r[2], r[3]);
-        }
-        tile.template wide_add<0>(hi, lo, acc);
-        if (!rest || lift == 0x1p48f) break;
-        tile.transpose_again();
-        lift *= 0x1p24f;
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-          for (int c = 0; c < Tl::kDims; ++c) acc[i][c] *= 0x1p24f;
       }
-      if (lift != 1.f) {
-        const float back = lift == 0x1p24f ? 0x1p-24f : 0x1p-48f;
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-          for (int c = 0; c < Tl::kDims; ++c) acc[i][c] *= back;
-      }
+      add_weighted(tile, p, acc);
       if (more) {
         load_v(off);
         now = next;
@@ -580,7 +651,7 @@ void paged_tree_kernel(TreeArg a) {
     }
     __syncthreads();
     const bool full = s0 == 0 && s1 == units;
-    float* part = a.parts + (int64_t)(2 * (w * lines + y) + (first_segment ? 0 : 1)) * a.part_floats;
+    float* part = a.parts + (int64_t)(2 * (w * a.kv.n_kv_heads + hk) + (first_segment ? 0 : 1)) * a.part_floats;
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
       if (16 * i >= columns) break;
@@ -592,9 +663,9 @@ void paged_tree_kernel(TreeArg a) {
 #pragma unroll
       for (int c = 0; c < Tl::kDims; c += 4)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          *reinterpret_cast<float4*>(&os[wave][l16][Tl::out_dim(4 * g4 + r, c)]) =
-              make_float4(acc[i][c][r] * f, acc[i][c + 1][r] * f, acc[i][c + 2][r] * f, acc[i][c + 3][r] * f);
+        for (int q4 = 0; q4 < 4; ++q4)
+          *reinterpret_cast<float4*>(&os[wave][l16][Tl::out_dim(4 * g4 + q4, c)]) =
+              make_float4(acc[i][c][q4] * f, acc[i][c + 1][q4] * f, acc[i][c + 2][q4] * f, acc[i][c + 3][q4] * f);
       __syncthreads();
       for (int x = tid; x < min(16, columns - 16 * i) * (kDh / 4); x += kThreads) {
         const int h = x / (kDh / 4), d = 4 * (x % (kDh / 4)), c = 16 * i + h;
@@ -610,14 +681,14 @@ void paged_tree_kernel(TreeArg a) {
 #pragma unroll
         for (int v = 0; v < kWaves; ++v) sum += ls[v][c] * part_weight(ms[v][c], top);
         if (full) {
-          const int col = cb * kColumns + c, nd = (int)((uint32_t)col / (uint32_t)a.group);
+          const int col = r.cb * kColumns + c, nd = (int)((uint32_t)col / (uint32_t)a.group);
           const int64_t row = start + nd;
           const int head = hk * a.group + col - nd * a.group;
           const float inv = sum == 0.f ? 0.f : vs / sum;
-          uint2 r;
-          r.x = T::down(o.x * inv) | (T::down(o.y * inv) << 16);
-          r.y = T::down(o.z * inv) | (T::down(o.w * inv) << 16);
-          *reinterpret_cast<uint2*>(a.out + row * a.out_stride + (int64_t)head * kDh + d) = r;
+          uint2 four;
+          four.x = T::down(o.x * inv) | (T::down(o.y * inv) << 16);
+          four.y = T::down(o.z * inv) | (T::down(o.w * inv) << 16);
+          *reinterpret_cast<uint2*>(a.out + row * a.out_stride + (int64_t)head * kDh + d) = four;
           if (d == 0 && a.lse)
             a.lse[row * a.n_heads + head] =
                 sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
@@ -631,13 +702,14 @@ void paged_tree_kernel(TreeArg a) {
       }
     }
     if (a.workers && s0 == 0 && tid == 0) {
-      int32_t* h = a.heads_of + 3 * ((int64_t)tr * lines + y);
+      int32_t* h = a.heads_of + 3 * (((int64_t)r.tr * a.blocks + r.cb) * a.kv.n_kv_heads + hk);
       h[0] = w;
-      h[1] = full ? 0 : (base + units - 1) / run - w + 1;
+      h[1] = full ? 0 : (r.base + units - 1) / r.run - w + 1;
       h[2] = first_segment ? 0 : 1;
     }
-    u += s1 - s0;
-    base += units;
+    r.u += s1 - s0;
+    r.base += units;
+    ++r.cb;
     first_segment = false;
   }
 }
@@ -650,13 +722,13 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArg a, int tiles) {
   __shared__ float4 so[256];
   __shared__ float sm[256], sl[256];
   constexpr int kItems = 256 / kStripes, kFours = kDh / 4;
-  const int columns = 16 * tiles, pieces = columns * kFours / kItems, lines = a.kv.n_kv_heads * a.blocks;
-  const int64_t output = blockIdx.x / pieces;
-  const int piece = blockIdx.x % pieces, tr = (int)(output / lines), y = (int)(output % lines);
-  const int hk = y / a.blocks, cb = y % a.blocks;
+  const int columns = 16 * tiles, pieces = columns * kFours / kItems;
+  const int output = blockIdx.x / pieces, piece = blockIdx.x % pieces;
+  const int hk = output % a.kv.n_kv_heads, cb = output / a.kv.n_kv_heads % a.blocks;
+  const int tr = output / a.kv.n_kv_heads / a.blocks;
   const TreeSpan s = tree_span(a, a.tree0 + tr);
   if (s.count * a.group <= cb * columns) return;
-  const int32_t* h = a.heads_of + 3 * output;
+  const int32_t* h = a.heads_of + 3 * (int64_t)output;
   const int w = h[0], parts = h[1], lead = h[2];
   if (parts == 0) return;
   const int item = piece * kItems + threadIdx.x % kItems, stripe = threadIdx.x / kItems;
@@ -671,7 +743,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArg a, int tiles) {
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         const int i = min(i0 + k * kStripes, parts - 1);
-        const float* p = a.parts + (2 * ((int64_t)(w + i) * lines + y) + (i == 0 ? lead : 0)) * a.part_floats;
+        const float* p = a.parts + (2 * ((int64_t)(w + i) * a.kv.n_kv_heads + hk) + (i == 0 ? lead : 0)) * a.part_floats;
         m_of[k] = p[c];
         l_of[k] = p[columns + c];
         e[k] = *reinterpret_cast<const float4*>(p + 2 * columns + c * kDh + d);
@@ -727,40 +799,6 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArg a, int tiles) {
   *reinterpret_cast<uint2*>(a.out + row * a.out_stride + (int64_t)head * kDh + d) = r;
   if (d == 0 && a.lse)
     a.lse[row * a.n_heads + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
-}
-
-template <class T, bool kE4M3, int kDh, int kTiles>
-void launch_tree_tiles(const TreeArg& a, const TreePlan& p, hipStream_t stream) {
-  const int64_t runs = a.workers ? a.workers : a.trees;
-  const dim3 grid((unsigned)(runs * p.lines)), block(64 * kTreeWaves);
-  if (a.cap > 0.f || a.slopes)
-    hipLaunchKernelGGL((paged_tree_kernel<T, kE4M3, kDh, kTiles, true>), grid, block, 0, stream, a);
-  else
-    hipLaunchKernelGGL((paged_tree_kernel<T, kE4M3, kDh, kTiles, false>), grid, block, 0, stream, a);
-  if (!a.workers) return;
-  const int64_t outputs = (int64_t)a.trees * p.lines, items = 16 * kTiles * (kDh / 4);
-  if (p.stripes == 4)
-    hipLaunchKernelGGL((tree_join_kernel<T, kE4M3, kDh, 4>), dim3((unsigned)(outputs * items / 64)),
-                       dim3(256), 0, stream, a, kTiles);
-  else
-    hipLaunchKernelGGL((tree_join_kernel<T, kE4M3, kDh, 1>), dim3((unsigned)(outputs * items / 256)),
-                       dim3(256), 0, stream, a, kTiles);
-}
-
-template <class T, bool kE4M3>
-void launch_tree(const TreeArg& a, const TreePlan& p, int head_dim, hipStream_t stream) {
-  if (head_dim == 256) {
-    if (p.tiles == 1) launch_tree_tiles<T, kE4M3, 256, 1>(a, p, stream);
-    else launch_tree_tiles<T, kE4M3, 256, 2>(a, p, stream);
-  } else if (head_dim == 128) {
-    if (p.tiles == 1) launch_tree_tiles<T, kE4M3, 128, 1>(a, p, stream);
-    else if (p.tiles == 2) launch_tree_tiles<T, kE4M3, 128, 2>(a, p, stream);
-    else launch_tree_tiles<T, kE4M3, 128, 4>(a, p, stream);
-  } else {
-    if (p.tiles == 1) launch_tree_tiles<T, kE4M3, 64, 1>(a, p, stream);
-    else if (p.tiles == 2) launch_tree_tiles<T, kE4M3, 64, 2>(a, p, stream);
-    else launch_tree_tiles<T, kE4M3, 64, 4>(a, p, stream);
-  }
 }
 
 }  // namespace emoe

@@ -8,30 +8,34 @@ namespace {
 
 constexpr int kPlaces = 512, kWholeKeys = 256, kManyOutputs = 1024;
 
-TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int32_t max_keys,
+TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int64_t max_keys,
                    int32_t max_nodes, int32_t window) {
   TreePlan p;
   const int64_t columns = (int64_t)(n_heads / kv.n_kv_heads) * max_nodes;
-  const int most_tiles = kv.head_dim == 256 ? 2 : 4;
-  p.tiles = columns <= 16 ? 1 : columns <= 32 || most_tiles == 2 ? 2 : 4;
+  const bool deep = kv.head_dim == 256;
+  p.wide = columns > (deep ? 16 : 32);
+  p.tiles = columns <= 16 ? 1 : !p.wide ? 2 : columns <= 64 || deep ? 4 : 8;
   p.blocks = (int)((columns + 16 * p.tiles - 1) / (16 * p.tiles));
   p.lines = kv.n_kv_heads * p.blocks;
   const int64_t span = (int64_t)window + max_nodes;
   const int64_t keys = window > 0 && span < max_keys ? span : max_keys;
-  const int64_t most_units = keys / (kTreeWaves * kTileKeys) + 2;
+  const int row_bytes = kv.head_dim * (kv.dtype == EMOE_E4M3 ? 1 : 2);
+  p.unit_keys = !p.wide ? kTreeWaves * kTileKeys : row_bytes == 512 ? 32 : 64;
+  const int64_t most_units = (keys / p.unit_keys + 2) * p.blocks;
   const int64_t outputs = (int64_t)trees * p.lines;
-  const bool two = p.tiles * kv.head_dim < 512 && kv.head_dim < 256;  // workgroups on a CU
-  const int places = two ? kPlaces : kPlaces / 2;
-  const bool whole = keys <= kWholeKeys || outputs >= kManyOutputs || p.lines > places;
-  p.workers = whole ? 0 : places / p.lines;
+  const int places = !p.wide && deep ? kPlaces / 2 : kPlaces;
+  // A launch's units stay below 2^31, its threads below 2^32.
+  p.trees_per_launch = (((int64_t)1 << 31) - 1 - kPlaces) / most_units;
+  const bool whole = keys <= kWholeKeys || outputs >= kManyOutputs || kv.n_kv_heads > places ||
+                     p.trees_per_launch < 1;
+  if (whole) p.trees_per_launch = trees;
+  const int64_t most_outputs = whole ? (int64_t)1 << 23 : kManyOutputs;
+  if (p.trees_per_launch > most_outputs / p.lines) p.trees_per_launch = most_outputs / p.lines;
+  p.workers = whole ? 0 : places / kv.n_kv_heads;
   p.least_run = 1;
   p.part_floats = 16 * p.tiles * (2 + kv.head_dim);
   p.stripes = outputs * 16 * p.tiles * (kv.head_dim / 4) / 256 < 1024 ? 4 : 1;
-  // A launch's units stay below 2^31, its threads below 2^32.
-  p.trees_per_launch = (((int64_t)1 << 31) - 1 - kPlaces) / most_units;
-  const int64_t most_outputs = whole ? (int64_t)1 << 23 : kManyOutputs;
-  if (p.trees_per_launch > most_outputs / p.lines) p.trees_per_launch = most_outputs / p.lines;
-  p.most_parts = whole ? 0 : 2 * (int64_t)p.workers * p.lines;
+  p.most_parts = whole ? 0 : 2 * (int64_t)p.workers * kv.n_kv_heads;
   p.most_shared = whole ? 0 : outputs;
   return p;
 }
@@ -88,7 +92,9 @@ int32_t emoe_paged_tree_attention(const emoe_paged_kv* kv, const emoe_paged_tree
     return report_error(EMOE_EINVAL, "workspace of %zu bytes < %zu needed", workspace ? workspace_bytes : 0,
                         bytes);
   if (!aligned16(workspace)) return report_error(EMOE_EINVAL, "workspace: need 16-byte alignment");
-  const TreePlan plan = tree_plan(*kv, A.trees, A.n_heads, A.max_keys, A.max_nodes, A.window);
+  const int64_t held = (int64_t)A.table_width * kv->page_size;  // no more keys than the table holds
+  const TreePlan plan = tree_plan(*kv, A.trees, A.n_heads, held < A.max_keys ? held : A.max_keys,
+                                  A.max_nodes, A.window);
   TreeArg a;
   a.kv = view_of(*kv);
   a.q = static_cast<const uint16_t*>(A.q);
@@ -118,6 +124,8 @@ int32_t emoe_paged_tree_attention(const emoe_paged_kv* kv, const emoe_paged_tree
   a.window = A.window;
   a.workers = plan.workers;
   a.least_run = plan.least_run;
+  a.unit_keys = plan.unit_keys;
+  a.unit_log2 = __builtin_ctz((unsigned)a.unit_keys);
   a.part_floats = plan.part_floats;
   for (int64_t t0 = 0; t0 < A.trees; t0 += plan.trees_per_launch) {
     a.tree0 = (int32_t)t0;

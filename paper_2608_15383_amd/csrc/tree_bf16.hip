@@ -1,5 +1,5 @@
 // The tree attention's kernels for bf16 queries.
-#include "tree.h"
+#include "tree_wide.h"
 
 namespace emoe {
 

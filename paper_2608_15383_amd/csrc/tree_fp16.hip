@@ -1,5 +1,5 @@
 // The tree attention's kernels for fp16 queries.
-#include "tree.h"
+#include "tree_wide.h"
 
 namespace emoe {
 
