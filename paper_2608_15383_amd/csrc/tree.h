@@ -241,12 +241,14 @@ __device__ __forceinline__ bool node_sees(uint64_t mask, int deep, int key_at, i
   return yes;
 }
 
-// One tile's step of the softmax: z to weights p.  The exponent that a column's
-// weights refer to follows the maximum only when a score exceeds it by 8: until then
-// they stay below 2^(8 + lead).  fp16 weights begin at 2^7: there is room above, but
-// little below.
+// One tile's step of the softmax: weights p of the scores z, which a factor >= 0 makes
+// powers of two.  The exponent that a column's weights refer to follows the maximum
+// only when a score exceeds it by 8: until then they stay below 2^(8 + lead).  fp16
+// weights begin at 2^7: there is room above, but little below.  In a tile with masked
+// keys, of score -inf, those weigh 0 even if the factor is 0.
 template <class Tl, int kTiles>
-__device__ __forceinline__ void soft_step(const float (&z)[kTiles][8], float (&m)[kTiles], float (&l)[kTiles],
+__device__ __forceinline__ void soft_step(const float (&z)[kTiles][8], float factor, bool masked,
+                                          float (&m)[kTiles], float (&l)[kTiles],
                                           f32x4 (&acc)[kTiles][Tl::kDims], float (&p)[kTiles][8]) {
   constexpr float kLead = Tl::kF16Weights ? 7.f : 0.f;
 #pragma unroll
@@ -254,6 +256,7 @@ __device__ __forceinline__ void soft_step(const float (&z)[kTiles][8], float (&m
     float top = z[i][0];
 #pragma unroll
     for (int j = 1; j < 8; ++j) top = fmaxf(top, z[i][j]);
+    top *= factor;
     if (__any(top > m[i] + (8.f + kLead))) {
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
@@ -266,11 +269,38 @@ __device__ __forceinline__ void soft_step(const float (&z)[kTiles][8], float (&m
     }
     const float ref = m[i] == -INFINITY ? 0.f : m[i];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      p[i][j] = exp2_hw(z[i][j] - ref);
-      l[i] += p[i][j];
-    }
+    for (int j = 0; j < 8; ++j) p[i][j] = exp2_hw(fmaf(z[i][j], factor, -ref));
   }
+  if (masked) {
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[i][j] = z[i][j] == -INFINITY ? 0.f : p[i][j];
+  }
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) l[i] += p[i][j];
+}
+
+// Two values rounded to a pair of the type, and up again.
+__device__ __forceinline__ uint32_t pair_down(Bf16, float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 v = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ uint32_t pair_down(Fp16, float a, float b) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  const f16x2 v = {(_Float16)a, (_Float16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ float pair_up(Bf16, uint32_t w, bool high) {
+  return __uint_as_float(high ? w & 0xffff0000u : w << 16);
+}
+__device__ __forceinline__ float pair_up(Fp16, uint32_t w, bool high) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  const f16x2 v = __builtin_bit_cast(f16x2, w);
+  return (float)(high ? v.y : v.x);
 }
 
 // Adds the weighted values.  Weights as two 16-bit halves; small fp16 weights in turns
@@ -310,9 +340,10 @@ __device__ __forceinline__ void add_weighted(Tl& tile, float (&p)[kTiles][8], f3
       uint32_t h[4], r[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint32_t h0 = W::down(part[i][2 * j]), h1 = W::down(part[i][2 * j + 1]);
-        h[j] = h0 | (h1 << 16);
-        r[j] = W::down(part[i][2 * j] - W::up(h0)) | (W::down(part[i][2 * j + 1] - W::up(h1)) << 16);
+        h[j] = pair_down(W(), part[i][2 * j], part[i][2 * j + 1]);
+        asm("" : "+v"(h[j]));  // one conversion of the pair, not a further one of each
+        r[j] = pair_down(W(), part[i][2 * j] - pair_up(W(), h[j], false),
+                         part[i][2 * j + 1] - pair_up(W(), h[j], true));
       }
       hi[i] = make_uint4(h[0], h[1], h[2], h[3]);
       lo[i] = make_uint4(r[0], r[1], r[2], r[3]);
@@ -333,6 +364,13 @@ __device__ __forceinline__ void add_weighted(Tl& tile, float (&p)[kTiles][8], f3
 #pragma unroll
       for (int c = 0; c < Tl::kDims; ++c) acc[i][c] *= back;
   }
+}
+
+// A query's chunk, its sign turned where the scores' scale is negative (so that the
+// scale may be taken as positive).
+__device__ __forceinline__ uint4 signed_chunk(const uint16_t* at, uint32_t flip) {
+  const uint4 x = *reinterpret_cast<const uint4*>(at);
+  return make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
 }
 
 // Adds one key's values, which are at `row`, weighted by p of lane group kg's key j, to
@@ -464,6 +502,8 @@ void paged_tree_kernel(TreeArg a) {
   float scale = a.scale;
   if (!kShaped) scale *= 1.4426950408889634f;
   if (kE4M3 && a.kv.k_scale) scale *= a.kv.k_scale[hk];
+  const uint32_t flip = scale < 0.f ? 0x80008000u : 0u;
+  scale = fabsf(scale);
   const float vs = kE4M3 && a.kv.v_scale ? a.kv.v_scale[hk] : 1.f;
   const float inv_cap = kShaped && a.cap > 0.f ? 1.f / a.cap : 0.f;
   const uint8_t* kbase = a.kv.k + (int64_t)hk * a.kv.head_bytes;
@@ -513,8 +553,8 @@ void paged_tree_kernel(TreeArg a) {
       for (int s = 0; s < Tl::kSteps; ++s) {
         q[i][s] = make_uint4(0, 0, 0, 0);
         if (c < columns)
-          q[i][s] = *reinterpret_cast<const uint4*>(a.q + (int64_t)(start + node[i]) * a.q_stride +
-                                                    (int64_t)head * kDh + Tl::q_dim(s, g4));
+          q[i][s] = signed_chunk(a.q + (int64_t)(start + node[i]) * a.q_stride + (int64_t)head * kDh + Tl::q_dim(s, g4),
+                                 flip);
       }
     }
     f32x4 acc[kTiles][Tl::kDims];
@@ -577,7 +617,7 @@ void paged_tree_kernel(TreeArg a) {
 #pragma unroll
       for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) z[i][j] = s[i][j >> 2][j & 3] * scale;
+        for (int j = 0; j < 8; ++j) z[i][j] = kShaped ? s[i][j >> 2][j & 3] * scale : s[i][j >> 2][j & 3];
       if constexpr (kShaped) {
         int key_at[8];
 #pragma unroll
@@ -611,7 +651,7 @@ void paged_tree_kernel(TreeArg a) {
         }
       }
       float p[kTiles][8];
-      soft_step<Tl>(z, m, l, acc, p);
+      soft_step<Tl>(z, kShaped ? 1.f : scale, !whole, m, l, acc, p);
       if (__any(bad != 0)) {
         for (int x = 0; x < 32; ++x) {
           const int j = x & 7, kg = x >> 3, key = key_of(j, kg);

@@ -100,6 +100,11 @@ struct WideSegment {
     const int deepest = a.window > 0 ? (int)wave_reduce_u32<true>((uint32_t)(lane < count ? depth : 0)) : 0;
     const bool active = 16 * wave < columns;
 
+    float scale = a.scale;
+    if (!kShaped) scale *= 1.4426950408889634f;
+    if (kE4M3 && a.kv.k_scale) scale *= a.kv.k_scale[hk];
+    const uint32_t flip = scale < 0.f ? 0x80008000u : 0u;
+    scale = fabsf(scale);
     int node[kTiles], deep_at[kTiles];
     float slope[kTiles];
     uint4 q[kTiles][Tl::kSteps];
@@ -117,17 +122,13 @@ struct WideSegment {
       for (int s = 0; s < Tl::kSteps; ++s) {
         q[i][s] = make_uint4(0, 0, 0, 0);
         if (c < columns)
-          q[i][s] = *reinterpret_cast<const uint4*>(a.q + (int64_t)(start + node[i]) * a.q_stride +
-                                                    (int64_t)head * kDh + q_dim(s, g4));
+          q[i][s] = signed_chunk(a.q + (int64_t)(start + node[i]) * a.q_stride + (int64_t)head * kDh + q_dim(s, g4), flip);
       }
       m[i] = -INFINITY;
       l[i] = 0.f;
 #pragma unroll
       for (int c = 0; c < Tl::kDims; ++c) acc[i][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    float scale = a.scale;
-    if (!kShaped) scale *= 1.4426950408889634f;
-    if (kE4M3 && a.kv.k_scale) scale *= a.kv.k_scale[hk];
     const float inv_cap = kShaped && a.cap > 0.f ? 1.f / a.cap : 0.f;
     const uint8_t* kbase = a.kv.k + (int64_t)hk * a.kv.head_bytes;
     const uint8_t* vbase = a.kv.v + (int64_t)hk * a.kv.head_bytes;
@@ -201,7 +202,7 @@ struct WideSegment {
 #pragma unroll
         for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) z[i][j] = s[i][j >> 2][j & 3] * scale;
+          for (int j = 0; j < 8; ++j) z[i][j] = kShaped ? s[i][j >> 2][j & 3] * scale : s[i][j >> 2][j & 3];
         if constexpr (kShaped) {
           int key_at[8];
 #pragma unroll
@@ -210,7 +211,8 @@ struct WideSegment {
         }
         const uint32_t octets = (there_octets >> (4 * sub)) & 15;
         uint32_t bad = 0;
-        if (!(key0 >= low && key0 + 32 <= high && octets == 15)) {
+        const bool masked = !(key0 >= low && key0 + 32 <= high && octets == 15);
+        if (masked) {
           uint32_t there = 0;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
@@ -234,7 +236,7 @@ struct WideSegment {
             }
           }
         }
-        soft_step<Tl>(z, m, l, acc, p);
+        soft_step<Tl>(z, kShaped ? 1.f : scale, masked, m, l, acc, p);
         if (__any(bad != 0)) {
           for (int x = 0; x < 32; ++x) {
             const int j = x & 7, kg = x >> 3, key = key_of(j, kg);
