@@ -21,7 +21,7 @@ struct TreeArg {
   int64_t q_stride, out_stride, table_stride;
   float scale, cap;
   int32_t tree0, trees, rows, n_heads, group, blocks, n_seqs, table_width, max_keys, max_nodes, window;
-  int32_t workers, least_run;  // workers 0: a workgroup to every output
+  int32_t workers, slack;  // workers 0: a workgroup to every output
   int32_t unit_keys, unit_log2;
   int32_t part_floats;
 };
@@ -31,7 +31,7 @@ struct TreeArg {
 struct TreePlan {
   int64_t trees_per_launch;
   bool wide;  // paged_tree_wide_kernel
-  int tiles, blocks, lines, workers, least_run, part_floats, stripes, unit_keys;
+  int tiles, blocks, lines, workers, slack, part_floats, stripes, unit_keys;
   int64_t most_parts, most_shared;
 };
 
@@ -75,24 +75,25 @@ __device__ __forceinline__ int tree_units(const TreeArg& a, const TreeSpan& s) {
 // x = cap * tanh(x / cap), to a few units of fp32's rounding: below 0.3 by tanh's
 // series (1 - 2 / (1 + e^2y) would cancel), which alone serves a wavefront whose
 // scores are all that small beside the cap.
-__device__ __forceinline__ void cap_scores(float (&x)[8], float cap, float inv_cap) {
+template <int kKeys>
+__device__ __forceinline__ void cap_scores(float (&x)[kKeys], float cap, float inv_cap) {
   float most = 0.f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
+  for (int j = 0; j < kKeys; ++j) {
     x[j] *= inv_cap;
     most = fmaxf(most, fabsf(x[j]));
   }
-  float far[8];
+  float far[kKeys];
   const bool any_far = __any(!(most < 0.3f));
   if (any_far) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < kKeys; ++j) {
       const float t = exp2_hw(fabsf(x[j]) * -2.8853900817779268f);
       far[j] = copysignf((1.f - t) * __builtin_amdgcn_rcpf(1.f + t), x[j]);
     }
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
+  for (int j = 0; j < kKeys; ++j) {
     const float y = x[j], z = y * y;
     float s = fmaf(z, 21844.f / 6081075.f, -1382.f / 155925.f);
     s = fmaf(z, s, 62.f / 2835.f);
@@ -152,7 +153,7 @@ struct WideTile : Tile<T, kE4M3, kDh> {
   }
 
   template <int kW>
-  __device__ __forceinline__ void wide_add(const uint4 (&hi)[kTiles], const uint4 (&lo)[kTiles],
+  __device__ __forceinline__ void wide_add(const uint4 (&hi)[kTiles][1], const uint4 (&lo)[kTiles][1],
                                            f32x4 (&acc)[kTiles][B::kDims]) const {
     uint32_t e[4], o[4];
 #pragma unroll
@@ -164,16 +165,18 @@ struct WideTile : Tile<T, kE4M3, kDh> {
     const uint4 ve = make_uint4(e[0], e[1], e[2], e[3]), vo = make_uint4(o[0], o[1], o[2], o[3]);
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
-      acc[n][2 * kW] = HW::mfma(ve, hi[n], acc[n][2 * kW]);
-      acc[n][2 * kW + 1] = HW::mfma(vo, hi[n], acc[n][2 * kW + 1]);
+      acc[n][2 * kW] = HW::mfma(ve, hi[n][0], acc[n][2 * kW]);
+      acc[n][2 * kW + 1] = HW::mfma(vo, hi[n][0], acc[n][2 * kW + 1]);
     }
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
-      acc[n][2 * kW] = HW::mfma(ve, lo[n], acc[n][2 * kW]);
-      acc[n][2 * kW + 1] = HW::mfma(vo, lo[n], acc[n][2 * kW + 1]);
+      acc[n][2 * kW] = HW::mfma(ve, lo[n][0], acc[n][2 * kW]);
+      acc[n][2 * kW + 1] = HW::mfma(vo, lo[n][0], acc[n][2 * kW + 1]);
     }
     if constexpr (kW + 1 < B::kDims / 2) wide_add<kW + 1>(hi, lo, acc);
   }
+
+  __device__ static __forceinline__ int dim(int c, int g, int r) { return B::out_dim(4 * g + r, c); }
 
   // Which of a lane's 8 keys have an infinity or a NaN among its values.
   __device__ __forceinline__ uint32_t not_finite() const {
@@ -209,17 +212,17 @@ __device__ __forceinline__ float cache_value(const uint8_t* at) {
 // The scores of a tile in powers of two: capped, and less the bias by distance.
 // key_at[j] is the key's place from the tree's first node on: below 0 its position,
 // else (only if `nodes`) the node, whose depth is in that lane.
-template <int kTiles>
-__device__ __forceinline__ void shape_scores(float (&z)[kTiles][8], float cap, float inv_cap, bool biased,
+template <int kTiles, int kKeys>
+__device__ __forceinline__ void shape_scores(float (&z)[kTiles][kKeys], float cap, float inv_cap, bool biased,
                                              const float (&slope)[kTiles], const int (&deep_at)[kTiles],
-                                             int (&key_at)[8], bool nodes, int depth) {
+                                             int (&key_at)[kKeys], bool nodes, int depth) {
   if (cap > 0.f) {
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) cap_scores(z[i], cap, inv_cap);
   }
   if (biased && nodes) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < kKeys; ++j) {
       const int deep = __shfl(depth, key_at[j] & 63);
       key_at[j] = key_at[j] < 0 ? key_at[j] : deep;
     }
@@ -227,7 +230,7 @@ __device__ __forceinline__ void shape_scores(float (&z)[kTiles][8], float cap, f
 #pragma unroll
   for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < kKeys; ++j) {
       z[i][j] *= 1.4426950408889634f;
       if (biased) z[i][j] = fmaf(-slope[i], (float)abs(deep_at[i] - key_at[j]), z[i][j]);
     }
@@ -242,22 +245,43 @@ __device__ __forceinline__ bool node_sees(uint64_t mask, int deep, int key_at, i
 }
 
 // One tile's step of the softmax: weights p of the scores z, which a factor >= 0 makes
-// powers of two.  The exponent that a column's weights refer to follows the maximum
-// only when a score exceeds it by 8: until then they stay below 2^(8 + lead).  fp16
-// weights begin at 2^7: there is room above, but little below.  In a tile with masked
-// keys, of score -inf, those weigh 0 even if the factor is 0.
-template <class Tl, int kTiles>
-__device__ __forceinline__ void soft_step(const float (&z)[kTiles][8], float factor, bool masked,
+// powers of two.  The exponent m that a column's weights refer to is that of the
+// maximum of its first tile (plus 2^lead), and follows the maximum again only when the
+// weights of a lane come to more than 2^(8 + lead): until then nothing is rescaled, and
+// no maximum sought.  fp16 weights begin at 2^7: there is room above, but little below.
+// In a tile with masked keys, of score -inf, those weigh 0 even if the factor is 0.
+template <class Tl, int kTiles, int kAcc, int kKeys>
+__device__ __forceinline__ void soft_step(const float (&z)[kTiles][kKeys], float factor, bool masked,
                                           float (&m)[kTiles], float (&l)[kTiles],
-                                          f32x4 (&acc)[kTiles][Tl::kDims], float (&p)[kTiles][8]) {
+                                          f32x4 (&acc)[kTiles][kAcc], float (&p)[kTiles][kKeys]) {
   constexpr float kLead = Tl::kF16Weights ? 7.f : 0.f;
+  float sum[kTiles];
+  auto weights = [&](int i) __attribute__((always_inline)) {
+    const float ref = m[i] == -INFINITY ? 0.f : m[i];
+#pragma unroll
+    for (int j = 0; j < kKeys; ++j) p[i][j] = exp2_hw(fmaf(z[i][j], factor, -ref));
+    if (masked) {
+#pragma unroll
+      for (int j = 0; j < kKeys; ++j) p[i][j] = z[i][j] == -INFINITY ? 0.f : p[i][j];
+    }
+    float s[4] = {p[i][0], p[i][1], p[i][2], p[i][3]};
+#pragma unroll
+    for (int j = 4; j < kKeys; ++j) s[j & 3] += p[i][j];
+    sum[i] = (s[0] + s[1]) + (s[2] + s[3]);
+  };
+  bool follow = false;
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
-    float top = z[i][0];
+    weights(i);
+    follow = follow || m[i] == -INFINITY || sum[i] > (Tl::kF16Weights ? 0x1p15f : 0x1p8f);
+  }
+  if (__any(follow)) {
 #pragma unroll
-    for (int j = 1; j < 8; ++j) top = fmaxf(top, z[i][j]);
-    top *= factor;
-    if (__any(top > m[i] + (8.f + kLead))) {
+    for (int i = 0; i < kTiles; ++i) {
+      float top = z[i][0];
+#pragma unroll
+      for (int j = 1; j < kKeys; ++j) top = fmaxf(top, z[i][j]);
+      top *= factor;
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
       const float m2 = fmaxf(m[i], top - kLead);
@@ -265,22 +289,12 @@ __device__ __forceinline__ void soft_step(const float (&z)[kTiles][8], float fac
       m[i] = m2;
       l[i] *= shrink;
 #pragma unroll
-      for (int c = 0; c < Tl::kDims; ++c) acc[i][c] *= shrink;
+      for (int c = 0; c < kAcc; ++c) acc[i][c] *= shrink;
+      weights(i);
     }
-    const float ref = m[i] == -INFINITY ? 0.f : m[i];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) p[i][j] = exp2_hw(fmaf(z[i][j], factor, -ref));
-  }
-  if (masked) {
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) p[i][j] = z[i][j] == -INFINITY ? 0.f : p[i][j];
   }
 #pragma unroll
-  for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) l[i] += p[i][j];
+  for (int i = 0; i < kTiles; ++i) l[i] += sum[i];
 }
 
 // Two values rounded to a pair of the type, and up again.
@@ -303,66 +317,68 @@ __device__ __forceinline__ float pair_up(Fp16, uint32_t w, bool high) {
   return (float)(high ? v.y : v.x);
 }
 
-// Adds the weighted values.  Weights as two 16-bit halves; small fp16 weights in turns
+// Adds the weighted values by add(high halves, low halves).  Weights as two 16-bit halves; small fp16 weights in turns
 // of their own, 2^24 and 2^48 times as large, as in paged_attention_kernel.
-template <class Tl, int kTiles>
-__device__ __forceinline__ void add_weighted(Tl& tile, float (&p)[kTiles][8], f32x4 (&acc)[kTiles][Tl::kDims]) {
+template <class Tl, int kTiles, int kAcc, int kKeys, class Add>
+__device__ __forceinline__ void add_in_halves(float (&p)[kTiles][kKeys], f32x4 (&acc)[kTiles][kAcc], Add add) {
   typedef typename Tl::W W;
   float lift = 1.f;
   while (true) {
     bool rest = false;
-    float part[kTiles][8];
+    float part[kTiles][kKeys];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) part[i][j] = p[i][j];
+      for (int j = 0; j < kKeys; ++j) part[i][j] = p[i][j];
     if constexpr (Tl::kF16Weights) {
       uint32_t least = ~0u;  // the bits, less 1, of the smallest weight above 0
 #pragma unroll
       for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) least = min(least, __float_as_uint(p[i][j]) - 1u);
+        for (int j = 0; j < kKeys; ++j) least = min(least, __float_as_uint(p[i][j]) - 1u);
       rest = __any(least < __float_as_uint(0x1p-9f) - 1u);
       if (rest) {
 #pragma unroll
         for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
+          for (int j = 0; j < kKeys; ++j) {
             const bool small = p[i][j] < 0x1p-9f;
             part[i][j] = small ? 0.f : p[i][j];
             p[i][j] = small ? p[i][j] * 0x1p24f : 0.f;
           }
       }
     }
-    uint4 hi[kTiles], lo[kTiles];
+    uint4 hi[kTiles][kKeys / 8], lo[kTiles][kKeys / 8];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
-      uint32_t h[4], r[4];
+      uint32_t h[kKeys / 2], r[kKeys / 2];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < kKeys / 2; ++j) {
         h[j] = pair_down(W(), part[i][2 * j], part[i][2 * j + 1]);
         asm("" : "+v"(h[j]));  // one conversion of the pair, not a further one of each
         r[j] = pair_down(W(), part[i][2 * j] - pair_up(W(), h[j], false),
                          part[i][2 * j + 1] - pair_up(W(), h[j], true));
       }
-      hi[i] = make_uint4(h[0], h[1], h[2], h[3]);
-      lo[i] = make_uint4(r[0], r[1], r[2], r[3]);
+#pragma unroll
+      for (int k = 0; k < kKeys / 8; ++k) {
+        hi[i][k] = make_uint4(h[4 * k], h[4 * k + 1], h[4 * k + 2], h[4 * k + 3]);
+        lo[i][k] = make_uint4(r[4 * k], r[4 * k + 1], r[4 * k + 2], r[4 * k + 3]);
+      }
     }
-    tile.template wide_add<0>(hi, lo, acc);
+    add(hi, lo);
     if (!rest || lift == 0x1p48f) break;
-    tile.transpose_again();
     lift *= 0x1p24f;
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-      for (int c = 0; c < Tl::kDims; ++c) acc[i][c] *= 0x1p24f;
+      for (int c = 0; c < kAcc; ++c) acc[i][c] *= 0x1p24f;
   }
   if (lift != 1.f) {
     const float back = lift == 0x1p24f ? 0x1p-24f : 0x1p-48f;
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-      for (int c = 0; c < Tl::kDims; ++c) acc[i][c] *= back;
+      for (int c = 0; c < kAcc; ++c) acc[i][c] *= back;
   }
 }
 
@@ -375,31 +391,30 @@ __device__ __forceinline__ uint4 signed_chunk(const uint16_t* at, uint32_t flip)
 
 // Adds one key's values, which are at `row`, weighted by p of lane group kg's key j, to
 // the columns that see it: lanes hold dimensions of their own.
-template <class T, bool kE4M3, class Tl, int kTiles>
-__device__ __forceinline__ void add_one_key(const uint8_t* row, int j, int kg, const float (&p)[kTiles][8],
-                                            const bool (&seen)[kTiles], f32x4 (&acc)[kTiles][Tl::kDims]) {
+template <class T, bool kE4M3, class Tl, class Out, int kTiles, int kAcc, int kKeys>
+__device__ __forceinline__ void add_one_key(const uint8_t* row, int j, int kg, const float (&p)[kTiles][kKeys],
+                                            const bool (&seen)[kTiles], f32x4 (&acc)[kTiles][kAcc]) {
   const int lane = lane_id(), l16 = lane & 15, g4 = lane >> 4;
   float weight[kTiles];
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
     float own = p[i][0];
 #pragma unroll
-    for (int k = 1; k < 8; ++k) own = j == k ? p[i][k] : own;
+    for (int k = 1; k < kKeys; ++k) own = j == k ? p[i][k] : own;
     weight[i] = __shfl(own, 16 * kg + l16);
   }
 #pragma unroll
   for (int r = 0; r < 4; ++r)
 #pragma unroll
-    for (int c = 0; c < Tl::kDims; ++c) {
-      const float v = cache_value<T, kE4M3>(row + Tl::out_dim(4 * g4 + r, c) * Tl::kItem);
+    for (int c = 0; c < kAcc; ++c) {
+      const float v = cache_value<T, kE4M3>(row + Out::dim(c, g4, r) * Tl::kItem);
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) acc[i][c][r] = seen[i] ? fmaf(weight[i], v, acc[i][c][r]) : acc[i][c][r];
       asm volatile("" ::: "memory");  // one load after the other: this is rare, registers are not to spare
     }
 }
 
-// Locates a worker's run: the units of all blocks of all trees stand behind each
-// other.  The trees of a chunk of 64 are kept one per lane.
+// The trees of a chunk of 64, one per lane.
 struct TreeChunk {
   TreeSpan span;
   int first, units, blocks;
@@ -415,8 +430,16 @@ struct TreeChunk {
     }
   }
 };
+
+// How the blocks of a launch are cut for the workers of a key head.  Either a block has
+// ceil(units / target) parts and every worker one, so that a worker never begins a
+// second block, which costs it as much as several units; or, where there are too few
+// workers for that, the units of all blocks stand behind each other and every worker
+// takes the same number of them.
 struct TreeRun {
-  int run, u, u_end, base, tr, cb;  // units; the first one of block cb of tree tr
+  int u, u_end, base;    // units: of the run, the first one of block cb of tree tr
+  int tr, cb;
+  int run, each;         // units of a run; of a part (0: equal runs)
 };
 __device__ __forceinline__ bool find_run(const TreeArg& a, int w, int columns, TreeChunk& ch, TreeRun& r) {
   int total = 0;
@@ -424,11 +447,30 @@ __device__ __forceinline__ bool find_run(const TreeArg& a, int w, int columns, T
     ch.load(a, c0, columns);
     total += __builtin_amdgcn_readlane(wave_scan(ch.units * ch.blocks), 63);
   }
-  r.run = max(a.least_run, (total + a.workers - 1) / a.workers);
+  r.run = (total + a.workers - 1) / a.workers;
+  r.each = 0;
+  r.base = 0;
+  if (a.trees <= 64) {
+    for (int t = r.run; t <= r.run + a.slack; t += max(1, t / 8)) {
+      const int parts = ch.blocks ? (int)((uint32_t)(ch.units + t - 1) / (uint32_t)t) : 0;
+      const int own = parts * ch.blocks, incl = wave_scan(own);
+      const int all = __builtin_amdgcn_readlane(incl, 63);
+      if (all > a.workers) continue;
+      if (w >= all) return false;
+      const int i = (int)__builtin_ctzll(__ballot(w < incl));
+      const int units = __builtin_amdgcn_readlane(ch.units, i), cuts = __builtin_amdgcn_readlane(parts, i);
+      const int at = w - __builtin_amdgcn_readlane(incl - own, i);
+      r.tr = i;
+      r.cb = at / cuts;
+      r.each = (int)((uint32_t)(units + cuts - 1) / (uint32_t)cuts);
+      r.u = (at % cuts) * r.each;
+      r.u_end = min(units, r.u + r.each);
+      return r.u < r.u_end;
+    }
+  }
   if ((int64_t)w * r.run >= total) return false;
   r.u = w * r.run;
   r.u_end = min(r.u + r.run, total);
-  r.base = 0;
   for (int c0 = 0;; c0 += 64) {
     if (a.trees > 64) ch.load(a, c0, columns);
     const int own = ch.units * ch.blocks, incl = wave_scan(own);
@@ -445,6 +487,15 @@ __device__ __forceinline__ bool find_run(const TreeArg& a, int w, int columns, T
     r.base += all;
   }
 }
+// Leaves where the parts of an output are: first worker, parts (0: it is whole), and
+// which of its first worker's parts is the first.
+__device__ __forceinline__ void note_parts(const TreeArg& a, const TreeRun& r, int w, int hk, int units, int s1,
+                                           bool first_segment) {
+  int32_t* h = a.heads_of + 3 * (((int64_t)r.tr * a.blocks + r.cb) * a.kv.n_kv_heads + hk);
+  h[0] = w;
+  h[1] = s1 == units ? 0 : r.each ? (units + r.each - 1) / r.each : (r.base + units - 1) / r.run - w + 1;
+  h[2] = first_segment ? 0 : 1;
+}
 
 // A column is a query head of a key head's group, of one node: column c is node
 // c / group, head c % group.  A workgroup takes a block of 16 * kTiles columns of a
@@ -452,10 +503,9 @@ __device__ __forceinline__ bool find_run(const TreeArg& a, int w, int columns, T
 // columns of the block; statistics and outputs of a column stay in the lanes of its
 // own (Tile says how).  The softmax runs once over the keys with a running maximum.
 //
-// Runs: the units of all blocks of all trees stand behind each other and every worker
-// of a key head takes the same number of them, wherever blocks begin and end.  Outputs that a worker covers
-// whole it writes; of the others (its first and its last at most) it leaves maximum,
-// sum and unscaled output in the workspace, which tree_join_kernel joins.
+// Outputs that a worker covers whole it writes; of the others (its first and its last at
+// most) it leaves maximum, sum and unscaled output in the workspace, which
+// tree_join_kernel joins.
 //
 // A tile that all columns see whole has nothing masked.  In the others (the tree's
 // own keys, the window's edge, missing pages) a weight of 0 would not undo an
@@ -491,7 +541,7 @@ void paged_tree_kernel(TreeArg a) {
   }
 
   TreeChunk ch;
-  TreeRun r{1, 0, 1, 0, w, cb};
+  TreeRun r{0, 1, 0, w, cb, 1, 0};
   if (a.workers) {
     if (!find_run(a, w, kColumns, ch, r)) return;  // the same for the whole workgroup
   } else {
@@ -663,10 +713,15 @@ void paged_tree_kernel(TreeArg a) {
 #pragma unroll
           for (int i = 0; i < kTiles; ++i)
             seen[i] = node_sees(__shfl(sees, node[i]), __shfl(depth, node[i]), key - n, key_depth, a.window);
-          add_one_key<T, kE4M3, Tl>(row, j, kg, p, seen, acc);
+          add_one_key<T, kE4M3, Tl, Tl>(row, j, kg, p, seen, acc);
         }
       }
-      add_weighted(tile, p, acc);
+      bool again = false;
+      add_in_halves<Tl>(p, acc, [&](const uint4(&hi)[kTiles][1], const uint4(&lo)[kTiles][1]) __attribute__((always_inline)) {
+        if (again) tile.transpose_again();
+        again = true;
+        tile.template wide_add<0>(hi, lo, acc);
+      });
       if (more) {
         load_v(off);
         now = next;
@@ -741,12 +796,7 @@ void paged_tree_kernel(TreeArg a) {
         }
       }
     }
-    if (a.workers && s0 == 0 && tid == 0) {
-      int32_t* h = a.heads_of + 3 * (((int64_t)r.tr * a.blocks + r.cb) * a.kv.n_kv_heads + hk);
-      h[0] = w;
-      h[1] = full ? 0 : (r.base + units - 1) / r.run - w + 1;
-      h[2] = first_segment ? 0 : 1;
-    }
+    if (a.workers && s0 == 0 && tid == 0) note_parts(a, r, w, hk, units, s1, first_segment);
     r.u += s1 - s0;
     r.base += units;
     ++r.cb;

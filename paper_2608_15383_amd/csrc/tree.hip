@@ -19,8 +19,8 @@ TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int6
   p.lines = kv.n_kv_heads * p.blocks;
   const int64_t span = (int64_t)window + max_nodes;
   const int64_t keys = window > 0 && span < max_keys ? span : max_keys;
-  const int row_bytes = kv.head_dim * (kv.dtype == EMOE_E4M3 ? 1 : 2);
-  p.unit_keys = !p.wide ? kTreeWaves * kTileKeys : row_bytes == 512 ? 32 : 64;
+  // A step of the wide kernel; a tile for each wavefront of the other.
+  p.unit_keys = !p.wide ? kTreeWaves * kTileKeys : deep && kv.dtype != EMOE_E4M3 ? kTileKeys : 2 * kTileKeys;
   const int64_t most_units = (keys / p.unit_keys + 2) * p.blocks;
   const int64_t outputs = (int64_t)trees * p.lines;
   const int places = !p.wide && deep ? kPlaces / 2 : kPlaces;
@@ -32,7 +32,7 @@ TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int6
   const int64_t most_outputs = whole ? (int64_t)1 << 23 : kManyOutputs;
   if (p.trees_per_launch > most_outputs / p.lines) p.trees_per_launch = most_outputs / p.lines;
   p.workers = whole ? 0 : places / kv.n_kv_heads;
-  p.least_run = 1;
+  p.slack = p.wide ? 12 : 6;
   p.part_floats = 16 * p.tiles * (2 + kv.head_dim);
   p.stripes = outputs * 16 * p.tiles * (kv.head_dim / 4) / 256 < 1024 ? 4 : 1;
   p.most_parts = whole ? 0 : 2 * (int64_t)p.workers * kv.n_kv_heads;
@@ -123,7 +123,7 @@ int32_t emoe_paged_tree_attention(const emoe_paged_kv* kv, const emoe_paged_tree
   a.max_nodes = A.max_nodes;
   a.window = A.window;
   a.workers = plan.workers;
-  a.least_run = plan.least_run;
+  a.slack = plan.slack;
   a.unit_keys = plan.unit_keys;
   a.unit_log2 = __builtin_ctz((unsigned)a.unit_keys);
   a.part_floats = plan.part_floats;

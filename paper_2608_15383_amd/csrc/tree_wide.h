@@ -6,9 +6,13 @@
 
 namespace emoe {
 
-// Wait until this wavefront's loads have arrived, in registers and in LDS.
-__device__ __forceinline__ void wait_all_loads() {
-  __builtin_amdgcn_s_waitcnt((0x7 << 4) | (0xF << 8));  // vmcnt(0) only
+// Wait until at most kLeft of this wavefront's loads are under way.
+template <int kLeft>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(kLeft < 64, "vmcnt");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((kLeft & 15) | ((kLeft >> 4) << 14) | (0x7 << 4) | (0xF << 8));
+  asm volatile("" ::: "memory");
 }
 // Workgroup barrier that orders LDS accesses but does not wait for loads.
 __device__ __forceinline__ void lds_barrier() {
@@ -17,87 +21,109 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
-
-// Keys and values of one step of a workgroup.  Row r of a key holds its 16-byte
-// chunks in the order c ^ swizzle(r), so that lanes that read the same chunk of
-// neighbouring keys use all banks.
-template <int kDh, bool kE4M3>
-struct WideStage {
-  static constexpr int kRow = kDh * (kE4M3 ? 1 : 2);
-  static constexpr int kKeys = kRow == 512 ? 32 : 64;
-  uint8_t k[kKeys * kRow], v[kKeys * kRow];
-
-  __device__ static __forceinline__ int swizzle(int row) { return kRow == 64 ? (row >> 1) & 3 : row & 7; }
-};
-// Stage S of two, one LDS variable each: the compiler waits for copies into a
-// variable before reads of that variable only.
-template <class Stage, int S>
-__device__ __forceinline__ Stage& wide_stage() {
-  __shared__ __attribute__((aligned(1024))) Stage stage;
-  return stage;
+// Copies 16 bytes per lane to LDS, at `to` + 16 * lane, past the caches (131,072 keys: 122 -> 104 us).  As assembly, since the compiler
+// would have every read of LDS wait for all copies under way; it has no registers as
+// outputs, and the kernel itself waits for it.
+__device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(to), "v"(from) : "memory");
 }
 
+// A ring of tiles of 32 keys and their values in LDS.  Row r of a tile holds its 16-byte
+// chunks in the order c ^ swizzle(r) (values: swizzle_v), so that lanes that read the same
+// chunk of several rows use all banks.  The kernel takes steps of two tiles (one of 512-byte
+// rows); two to four steps in up to 64 KB: two workgroups to a CU.
 template <int kDh, bool kE4M3>
-constexpr int wide_keys() { return WideStage<kDh, kE4M3>::kKeys; }
+struct WideRing {
+  static constexpr int kRow = kDh * (kE4M3 ? 1 : 2), kSide = 32 * kRow, kTile = 2 * kSide;
+  static constexpr int kStepTiles = kRow == 512 ? 1 : 2, kStep = kStepTiles * kTile;
+  static constexpr int kSteps = 65536 / kStep < 4 ? 65536 / kStep : 4;
+  static constexpr int kCopies = kStep / 4096;  // of a wavefront and step
+
+  __device__ static __forceinline__ int swizzle(int row) { return kRow == 64 ? (row >> 1) & 3 : row & 7; }
+  // Of values, which are read transposed: 4 rows of 32 bytes at once, or 8 of 16 (8 bits).
+  __device__ static __forceinline__ int swizzle_v(int row) {
+    return !kE4M3 ? 2 * (row & 3) : kRow == 64 ? (row >> 1 & 1) | (row >> 3 & 2) : (row & 3) | (row >> 2 & 4);
+  }
+  __device__ static __forceinline__ uint8_t* memory() {
+    __shared__ __attribute__((aligned(1024))) uint8_t ring[kSteps * kStep];
+    return ring;
+  }
+};
 
 // One block of columns of a tree over a run of its keys, of which this wavefront has
 // the tiles wave, wave + 4 .. of 16 columns.
 template <class T, bool kE4M3, int kDh, int kTiles, bool kShaped>
 struct WideSegment {
   typedef WideTile<T, kE4M3, kDh, kTiles> Tl;
-  typedef WideStage<kDh, kE4M3> Stage;
-  static constexpr int kRow = Stage::kRow, kKeys = Stage::kKeys, kItem = Tl::kItem;
+  typedef WideRing<kDh, kE4M3> Ring;
+  static constexpr int kRow = Ring::kRow, kItem = Tl::kItem;
   static constexpr int kSub = kE4M3 ? 2 : 1;         // steps of a 16-byte chunk of keys
   static constexpr int kChunks = kRow / 64;          // chunks of a lane
-  static constexpr int kLaneBytes = Tl::kVWords * 4 > 16 ? 16 : Tl::kVWords * 4;  // of values, at once
+  // Tiles of 32 keys that are taken together (two where registers allow: more to do while
+  // a product or a read is under way), and a lane's keys of them.
+  static constexpr int kU = kTiles == 1 ? Ring::kStepTiles : 1, kKeys = 8 * kU;
+  static constexpr int kBlocks = kDh / 16;            // of output dimensions
+  struct Out {                                       // dimension of row r of block c, in lane group g
+    __device__ static __forceinline__ int dim(int c, int g, int r) { return 16 * c + 4 * g + r; }
+  };
+
+  // Which of a lane's 8 keys have an infinity or a NaN among these values.
+  __device__ static __forceinline__ uint32_t not_finite(const uint4& v) {
+    constexpr uint32_t kExp = Tl::kF16Weights ? 0x7c00u : 0x7f80u;
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t bad = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) bad |= ((w[j >> 1] >> (16 * (j & 1))) & kExp) == kExp ? 1u << j : 0u;
+    return bad;
+  }
+  // The values of the keys that are not in `keep` become 0.
+  __device__ static __forceinline__ uint4 cleared_values(const uint4& v, uint32_t keep) {
+    uint32_t m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      m[i] = ((keep >> (2 * i)) & 1 ? 0xffffu : 0u) | ((keep >> (2 * i)) & 2 ? 0xffff0000u : 0u);
+    return make_uint4(v.x & m[0], v.y & m[1], v.z & m[2], v.w & m[3]);
+  }
 
   // Dimension of the first element that lane group g has of step s.
   __device__ static __forceinline__ int q_dim(int s, int g) {
     return (16 / kItem) * (4 * (s / kSub) + g) + 8 * (s % kSub);
   }
 
-  // Copies the wavefront's quarter of a stage's rows; `page` is the page of the
-  // stage's octet that the lane stands for.
-  template <class St>
-  __device__ static __forceinline__ void fetch(const TreeArg& a, St& stage, const uint8_t* kbase,
+  // Copies the wavefront's octet of a tile, which is in `page`.
+  __device__ static __forceinline__ void fetch(const TreeArg& a, uint32_t tile_at, const uint8_t* kbase,
                                                const uint8_t* vbase, int key0, int page, int wave, int lane) {
-    constexpr int kRows = kKeys / 4, kRowsAtOnce = 1024 / kRow, kLoads = kRows / kRowsAtOnce;
-    const int slot_mask = (1 << a.kv.page_log2) - 1;
-    const int in = lane / (kRow / 16), chunk = lane % (kRow / 16);
-    auto octet_at = [&](int row) -> int64_t {
-      const int p = __builtin_amdgcn_readlane(page, row >> 3);
-      return ((uint32_t)p < (uint32_t)a.kv.n_pages ? p : 0) * a.kv.page_bytes +
-             (int64_t)((key0 + row) & slot_mask) * a.kv.slot_bytes;
-    };
+    constexpr int kRowsAtOnce = 1024 / kRow;
+    const int64_t at = ((uint32_t)page < (uint32_t)a.kv.n_pages ? page : 0) * a.kv.page_bytes +
+                       (int64_t)((key0 + 8 * wave) & ((1 << a.kv.page_log2) - 1)) * a.kv.slot_bytes;
+    if constexpr (kRowsAtOnce == 16) {  // keys from the lower half of the lanes, values from the upper one
+      const int row = (lane >> 2) & 7;
+      const int swizzle = lane < 32 ? Ring::swizzle(row) : Ring::swizzle_v(8 * wave + row);
+      const uint8_t* from = (lane < 32 ? kbase : vbase) + at + (uint32_t)(row * a.kv.slot_bytes) +
+                            16 * ((lane & 3) ^ swizzle);
+      copy_to_lds(from, tile_at + 1024 * wave);
+    } else {
+      const int in = lane / (kRow / 16), chunk = lane % (kRow / 16);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int row = __builtin_amdgcn_readfirstlane(kRows * wave + i * kRowsAtOnce);
-      int64_t at = octet_at(row);
-      if constexpr (kRowsAtOnce == 16) {
-        const int64_t second = octet_at(row + 8);
-        at = lane >= 32 ? second : at;
+      for (int i = 0; i < 8 / kRowsAtOnce; ++i) {
+        const int row = i * kRowsAtOnce + in;
+        const uint32_t slot = row * a.kv.slot_bytes;
+        const uint32_t to = tile_at + (8 * wave + i * kRowsAtOnce) * kRow;
+        copy_to_lds(kbase + at + (slot + 16 * (chunk ^ Ring::swizzle(row))), to);
+        copy_to_lds(vbase + at + (slot + 16 * (chunk ^ Ring::swizzle_v(8 * wave + row))), to + Ring::kSide);
       }
-      const uint32_t off = (in & 7) * a.kv.slot_bytes +
-                           16 * (chunk ^ Stage::swizzle((i * kRowsAtOnce & 7) + in));
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)(kbase + at + off),
-          (__attribute__((address_space(3))) void*)&stage.k[row * kRow], 16, 0, 0);
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)(vbase + at + off),
-          (__attribute__((address_space(3))) void*)&stage.v[row * kRow], 16, 0, 0);
     }
   }
+  // Where a row's keys and values are in a tile.
+  static constexpr bool kMixed = kRow == 64;  // octets of keys and of values in turn
+  __device__ static __forceinline__ int key_row(int row) { return kMixed ? 1024 * (row >> 3) + 64 * (row & 7) : row * kRow; }
+  static constexpr int kValues = kMixed ? 512 : Ring::kSide;
 
   __device__ static __forceinline__ void run(const TreeArg& a, const TreeRun& r, int w, int hk, int start,
                                              int count, int sq, int n, int first, int end, int units, int s0,
                                              int s1, int columns, int block_columns, bool first_segment) {
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l16 = lane & 15, g4 = lane >> 4;
-    // What each node sees, and its depth: node i's in lane i.
-    uint64_t sees = 0;
-    if (lane < count) sees = a.tree ? a.tree[start + lane] : (2ull << lane) - 1;
-    const int depth = __popcll(sees & ((1ull << lane) - 1));
-    const int deepest = a.window > 0 ? (int)wave_reduce_u32<true>((uint32_t)(lane < count ? depth : 0)) : 0;
     const bool active = 16 * wave < columns;
 
     float scale = a.scale;
@@ -105,10 +131,61 @@ struct WideSegment {
     if (kE4M3 && a.kv.k_scale) scale *= a.kv.k_scale[hk];
     const uint32_t flip = scale < 0.f ? 0x80008000u : 0u;
     scale = fabsf(scale);
+    const float inv_cap = kShaped && a.cap > 0.f ? 1.f / a.cap : 0.f;
+    const uint8_t* kbase = a.kv.k + (int64_t)hk * a.kv.head_bytes;
+    const uint8_t* vbase = a.kv.v + (int64_t)hk * a.kv.head_bytes;
+    const ConstI32 table = (ConstI32)(a.table + (int64_t)sq * a.table_stride);
+
+    constexpr int kS = Ring::kStepTiles, kStepKeys = 32 * kS, kAhead = Ring::kSteps - 1;
+    const int t_all = (end + kStepKeys - 1) / kStepKeys, t0 = first / kStepKeys;
+    int t = t0 + s0;
+    const int t_end = a.workers ? min(t0 + s1, t_all) : t_all;
+    uint8_t* ring = Ring::memory();
+    const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)ring;
+    struct Pages {
+      Octets tile[kS];
+    };
+    auto pages_of = [&](int step) -> Pages {
+      Pages o;
+#pragma unroll
+      for (int u = 0; u < kS; ++u) o.tile[u] = octets_of(a.kv, table, step * kStepKeys + 32 * u, end);
+      return o;
+    };
+    auto there = [&](const Pages& o) -> uint32_t {
+      uint32_t bits = 0;
+#pragma unroll
+      for (int i = 0; i < 4 * kS; ++i)
+        bits |= (uint32_t)o.tile[i >> 2].page[i & 3] < (uint32_t)a.kv.n_pages ? 1u << i : 0u;
+      return bits;
+    };
+    auto fetch_step = [&](int step, const Pages& o) {
+#pragma unroll
+      for (int u = 0; u < kS; ++u) {
+        const Octets& x = o.tile[u];
+        const int page = wave == 0 ? x.page[0] : wave == 1 ? x.page[1] : wave == 2 ? x.page[2] : x.page[3];
+        fetch(a, ring_at + (step % Ring::kSteps) * Ring::kStep + u * Ring::kTile, kbase, vbase,
+              step * kStepKeys + 32 * u, page, wave, lane);
+      }
+    };
+    uint32_t queue = 0;  // which octets the steps from t on have, 4 kU bits each
+    lds_barrier();  // the last segment's readers are done
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (t + i < t_end) {
+        const Pages o = pages_of(t + i);
+        queue |= there(o) << (4 * kS * i);
+        fetch_step(t + i, o);
+      }
+    }
+    // What each node sees, and its depth: node i's in lane i.
+    uint64_t sees = 0;
+    if (lane < count) sees = a.tree ? a.tree[start + lane] : (2ull << lane) - 1;
+    const int depth = __popcll(sees & ((1ull << lane) - 1));
+    const int deepest = a.window > 0 ? (int)wave_reduce_u32<true>((uint32_t)(lane < count ? depth : 0)) : 0;
     int node[kTiles], deep_at[kTiles];
     float slope[kTiles];
     uint4 q[kTiles][Tl::kSteps];
-    f32x4 acc[kTiles][Tl::kDims];
+    f32x4 acc[kTiles][kBlocks];
     float m[kTiles], l[kTiles];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
@@ -127,164 +204,170 @@ struct WideSegment {
       m[i] = -INFINITY;
       l[i] = 0.f;
 #pragma unroll
-      for (int c = 0; c < Tl::kDims; ++c) acc[i][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int c = 0; c < kBlocks; ++c) acc[i][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const float inv_cap = kShaped && a.cap > 0.f ? 1.f / a.cap : 0.f;
-    const uint8_t* kbase = a.kv.k + (int64_t)hk * a.kv.head_bytes;
-    const uint8_t* vbase = a.kv.v + (int64_t)hk * a.kv.head_bytes;
-    const int32_t* table = a.table + (int64_t)sq * a.table_stride;
     const int low = a.window > 0 ? max(0, n + deepest + 1 - a.window) : 0, high = min(n, end);
-
-    // A lane's places in a stage: its keys' chunks (even and odd), its values' part of
-    // the rows 4 g4 + 0 .. 3.
-    int k_at[2], v_at[4];
+    // A lane's places in a tile: its keys' chunks (even and odd), its part of the values.
+    int k_at[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      k_at[i] = l16 * kRow + 16 * ((g4 | (kRow == 64 ? 0 : 4 * i)) ^ Stage::swizzle(l16));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = 4 * g4 + i, byte = kLaneBytes * l16;
-      v_at[i] = row * kRow + 16 * ((byte >> 4) ^ Stage::swizzle(row)) + (byte & 15);
-    }
+      k_at[i] = key_row(l16) + 16 * ((g4 | (kRow == 64 ? 0 : 4 * i)) ^ Ring::swizzle(l16));
+    // 16 bits: row 4 g4 + l16 / 4, 8 bytes l16 % 4 of 32; 8 bits: row r = l16 / 2 of the
+    // group's eight, 8 bytes l16 % 2 of 16.
+    const int v_row = kE4M3 ? 4 * g4 + (l16 >> 1 & 3) + 16 * (l16 >> 3) : 4 * g4 + (l16 >> 2);
+    const int v_at = kValues + key_row(v_row) + 8 * (l16 & 1);
+    const int v_swizzle = Ring::swizzle_v(v_row);
+    constexpr int kHalf = kMixed ? 2048 : 16 * kRow;  // from row r to row r + 16
 
-    auto compute = [&](const Stage& stage, int t, uint32_t there_octets) __attribute__((always_inline)) {
+    auto compute = [&](const uint8_t* held, int key0, uint32_t octets) __attribute__((always_inline)) {
+      f32x4 s[kTiles][2 * kU];
 #pragma unroll
-      for (int sub = 0; sub < kKeys / 32; ++sub) {
-        const int key0 = t * kKeys + 32 * sub;
-        if (key0 >= end || key0 + 32 <= first) continue;
-        f32x4 s[kTiles][2];
+      for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i)
+        for (int h = 0; h < 2 * kU; ++h) s[i][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int h = 0; h < 2; ++h) s[i][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int p = 0; p < kChunks; ++p)
 #pragma unroll
-        for (int p = 0; p < kChunks; ++p)
+        for (int h = 0; h < 2 * kU; ++h) {
+          const uint4 c = *reinterpret_cast<const uint4*>(held + k_at[p & 1] + (h >> 1) * Ring::kTile +
+                                                          (h & 1) * kHalf + 128 * (p >> 1));
+          if constexpr (kE4M3) {
+            typedef typename Tl::H16 H;
+            const uint4 x0 = make_uint4(H::template from_e4m3<false>(c.x), H::template from_e4m3<true>(c.x),
+                                        H::template from_e4m3<false>(c.y), H::template from_e4m3<true>(c.y));
+            const uint4 x1 = make_uint4(H::template from_e4m3<false>(c.z), H::template from_e4m3<true>(c.z),
+                                        H::template from_e4m3<false>(c.w), H::template from_e4m3<true>(c.w));
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint4 c = *reinterpret_cast<const uint4*>(stage.k + k_at[p & 1] + (32 * sub + 16 * h) * kRow +
-                                                            128 * (p >> 1));
-            if constexpr (kE4M3) {
-              typedef typename Tl::H16 H;
-              const uint4 x0 = make_uint4(H::template from_e4m3<false>(c.x), H::template from_e4m3<true>(c.x),
-                                          H::template from_e4m3<false>(c.y), H::template from_e4m3<true>(c.y));
-              const uint4 x1 = make_uint4(H::template from_e4m3<false>(c.z), H::template from_e4m3<true>(c.z),
-                                          H::template from_e4m3<false>(c.w), H::template from_e4m3<true>(c.w));
+            for (int i = 0; i < kTiles; ++i) s[i][h] = H::mfma(x0, q[i][2 * p], s[i][h]);
 #pragma unroll
-              for (int i = 0; i < kTiles; ++i) {
-                s[i][h] = H::mfma(x0, q[i][2 * p], s[i][h]);
-                s[i][h] = H::mfma(x1, q[i][2 * p + 1], s[i][h]);
-              }
-            } else {
-#pragma unroll
-              for (int i = 0; i < kTiles; ++i) s[i][h] = Tl::H16::mfma(c, q[i][p], s[i][h]);
-            }
-          }
-        Tl tile;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint8_t* at = stage.v + v_at[j & 3] + (32 * sub + 16 * (j >> 2)) * kRow;
-          if constexpr (Tl::kVWords == 1) {
-            tile.v[j][0] = *reinterpret_cast<const uint32_t*>(at);
-          } else if constexpr (Tl::kVWords == 2) {
-            const uint2 x = *reinterpret_cast<const uint2*>(at);
-            tile.v[j][0] = x.x, tile.v[j][1] = x.y;
+            for (int i = 0; i < kTiles; ++i) s[i][h] = H::mfma(x1, q[i][2 * p + 1], s[i][h]);
           } else {
 #pragma unroll
-            for (int u = 0; u < Tl::kVWords / 4; ++u) {
-              const uint4 x = *reinterpret_cast<const uint4*>(at + 256 * u);
-              tile.v[j][4 * u] = x.x, tile.v[j][4 * u + 1] = x.y, tile.v[j][4 * u + 2] = x.z,
-                         tile.v[j][4 * u + 3] = x.w;
-            }
+            for (int i = 0; i < kTiles; ++i) s[i][h] = Tl::H16::mfma(c, q[i][p], s[i][h]);
           }
         }
-        auto key_of = [&](int j, int group) { return key0 + 16 * (j >> 2) + 4 * group + (j & 3); };
-        float z[kTiles][8], p[kTiles][8];
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) z[i][j] = kShaped ? s[i][j >> 2][j & 3] * scale : s[i][j >> 2][j & 3];
-        if constexpr (kShaped) {
-          int key_at[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) key_at[j] = key_of(j, g4) - n;
-          shape_scores(z, a.cap, inv_cap, a.slopes != nullptr, slope, deep_at, key_at, key0 + 32 > n, depth);
+      // The values of dimensions 16 c + l16 of the lane group's 8 keys of a tile, in the
+      // order of the scores: LDS transposes them on the way.
+      auto values = [&](int c, int u) __attribute__((always_inline)) -> uint4 {
+        const uint8_t* tile = held + u * Ring::kTile;
+        if constexpr (kE4M3) {
+          typedef int i32x2 __attribute__((ext_vector_type(2)));
+          typedef __attribute__((address_space(3))) i32x2* At;
+          const i32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((At)(tile + v_at + 16 * (c ^ v_swizzle)));
+          return make_uint4(Tl::HW::template from_e4m3<false>((uint32_t)x[0]),
+                            Tl::HW::template from_e4m3<true>((uint32_t)x[0]),
+                            Tl::HW::template from_e4m3<false>((uint32_t)x[1]),
+                            Tl::HW::template from_e4m3<true>((uint32_t)x[1]));
+        } else {
+          typedef short i16x4 __attribute__((ext_vector_type(4)));
+          typedef __attribute__((address_space(3))) i16x4* At;
+          const uint8_t* at = tile + v_at + 16 * ((2 * c + (l16 >> 1 & 1)) ^ v_swizzle);
+          const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)at));
+          const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(at + kHalf)));
+          return make_uint4(x.x, x.y, y.x, y.y);
         }
-        const uint32_t octets = (there_octets >> (4 * sub)) & 15;
-        uint32_t bad = 0;
-        const bool masked = !(key0 >= low && key0 + 32 <= high && octets == 15);
-        if (masked) {
-          uint32_t there = 0;
+      };
+      // The place in the step of a lane group's key j, and its octet.
+      auto key_of = [&](int j, int group) { return 32 * (j >> 3) + 16 * (j >> 2 & 1) + 4 * group + (j & 3); };
+      float z[kTiles][kKeys], p[kTiles][kKeys];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int key = key_of(j, g4);
-            if (key >= first && key < end && (octets >> (2 * (j >> 2) + (g4 >> 1))) & 1) there |= 1u << j;
-          }
-          bad = tile.not_finite() & there;
-          bad |= __shfl_xor(bad, 1);
-          bad |= __shfl_xor(bad, 2);
-          bad |= __shfl_xor(bad, 4);
-          bad |= __shfl_xor(bad, 8);
-          tile.clear_v(there & ~bad);
+      for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int key_at = key_of(j, g4) - n, key_depth = __shfl(depth, key_at & 63);
+        for (int j = 0; j < kKeys; ++j) z[i][j] = kShaped ? s[i][j >> 2][j & 3] * scale : s[i][j >> 2][j & 3];
+      if constexpr (kShaped) {
+        int key_at[kKeys];
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i) {
-              const uint64_t mask = __shfl(sees, node[i]);
-              const int deep = __shfl(depth, node[i]);
-              if (!((there >> j) & 1) || !node_sees(mask, deep, key_at, key_depth, a.window)) z[i][j] = -INFINITY;
-            }
-          }
-        }
-        soft_step<Tl>(z, kShaped ? 1.f : scale, masked, m, l, acc, p);
-        if (__any(bad != 0)) {
-          for (int x = 0; x < 32; ++x) {
-            const int j = x & 7, kg = x >> 3, key = key_of(j, kg);
-            if (!((__builtin_amdgcn_readlane((int)bad, 16 * kg) >> j) & 1)) continue;
-            const uint8_t* row = vbase + table[key >> a.kv.page_log2] * a.kv.page_bytes +
-                                 (int64_t)(key & ((1 << a.kv.page_log2) - 1)) * a.kv.slot_bytes;
-            const int key_depth = __shfl(depth, (key - n) & 63);
-            bool seen[kTiles];
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i)
-              seen[i] = node_sees(__shfl(sees, node[i]), __shfl(depth, node[i]), key - n, key_depth, a.window);
-            add_one_key<T, kE4M3, Tl>(row, j, kg, p, seen, acc);
-          }
-        }
-        add_weighted(tile, p, acc);
+        for (int j = 0; j < kKeys; ++j) key_at[j] = key0 + key_of(j, g4) - n;
+        shape_scores(z, a.cap, inv_cap, a.slopes != nullptr, slope, deep_at, key_at, key0 + 32 * kU > n, depth);
       }
+      uint32_t bad = 0, keep = ~0u;
+      const bool masked = !(key0 >= low && key0 + 32 * kU <= high && octets == (1u << (4 * kU)) - 1);
+      if (masked) {
+        uint32_t there = 0;
+#pragma unroll
+        for (int j = 0; j < kKeys; ++j) {
+          const int at = key_of(j, g4), key = key0 + at;
+          if (key >= first && key < end && (octets >> (at >> 3)) & 1) there |= 1u << j;
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u)
+#pragma unroll 1
+          for (int c = 0; c < kBlocks; ++c) bad |= not_finite(values(c, u)) << (8 * u);
+        bad &= there;
+        bad |= __shfl_xor(bad, 1);
+        bad |= __shfl_xor(bad, 2);
+        bad |= __shfl_xor(bad, 4);
+        bad |= __shfl_xor(bad, 8);
+        keep = there & ~bad;
+#pragma unroll
+        for (int j = 0; j < kKeys; ++j) {
+          const int key_at = key0 + key_of(j, g4) - n, key_depth = __shfl(depth, key_at & 63);
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i) {
+            const uint64_t mask = __shfl(sees, node[i]);
+            const int deep = __shfl(depth, node[i]);
+            if (!((there >> j) & 1) || !node_sees(mask, deep, key_at, key_depth, a.window)) z[i][j] = -INFINITY;
+          }
+        }
+      }
+      soft_step<Tl>(z, kShaped ? 1.f : scale, masked, m, l, acc, p);
+      if (__any(bad != 0)) {
+#pragma unroll 1
+        for (int x = 0; x < 4 * kKeys; ++x) {
+          const int j = x % kKeys, kg = x / kKeys, key = key0 + key_of(j, kg);
+          if (!((__builtin_amdgcn_readlane((int)bad, 16 * kg) >> j) & 1)) continue;
+          const uint8_t* row = vbase + table[key >> a.kv.page_log2] * a.kv.page_bytes +
+                               (int64_t)(key & ((1 << a.kv.page_log2) - 1)) * a.kv.slot_bytes;
+          const int key_depth = __shfl(depth, (key - n) & 63);
+          bool seen[kTiles];
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i)
+            seen[i] = node_sees(__shfl(sees, node[i]), __shfl(depth, node[i]), key - n, key_depth, a.window);
+          add_one_key<T, kE4M3, Tl, Out>(row, j, kg, p, seen, acc);
+        }
+      }
+      add_in_halves<Tl>(p, acc, [&](const uint4(&hi)[kTiles][kU], const uint4(&lo)[kTiles][kU])
+                                    __attribute__((always_inline)) {
+        auto add = [&](auto cleared) __attribute__((always_inline)) {
+#pragma unroll
+          for (int c = 0; c < kBlocks; ++c)
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+              uint4 v = values(c, u);
+              if constexpr (decltype(cleared)::value) v = cleared_values(v, keep >> (8 * u));
+#pragma unroll
+              for (int i = 0; i < kTiles; ++i) acc[i][c] = Tl::HW::mfma(v, hi[i][u], acc[i][c]);
+#pragma unroll
+              for (int i = 0; i < kTiles; ++i) acc[i][c] = Tl::HW::mfma(v, lo[i][u], acc[i][c]);
+            }
+        };
+        if (masked) add(std::true_type());
+        else add(std::false_type());
+      });
     };
 
-    const int t_all = (end + kKeys - 1) / kKeys, t0 = first / kKeys;
-    int t = t0 + s0;
-    const int t_end = a.workers ? min(t0 + s1, t_all) : t_all;
-    auto page_of = [&](int tile) -> int {
-      const int key = tile * kKeys + 8 * lane;
-      return lane < kKeys / 8 && tile < t_end && key < end ? table[key >> a.kv.page_log2] : -1;
-    };
-    auto octets_of = [&](int page) -> uint32_t {
-      return (uint32_t)__ballot((uint32_t)page < (uint32_t)a.kv.n_pages) & ((1u << (kKeys / 8)) - 1);
-    };
-    lds_barrier();  // the last segment's readers are done
-    if (t < t_end) {
-      Stage &st0 = wide_stage<Stage, 0>(), &st1 = wide_stage<Stage, 1>();
-      int page = page_of(t);
-      uint32_t now = octets_of(page);
-      fetch(a, st0, kbase, vbase, t * kKeys, page, wave, lane);
-      page = page_of(t + 1);
-      // The copies of the next step are under way while this one is computed.
-      auto step = [&](const Stage& here, Stage& there) __attribute__((always_inline)) -> bool {
-        wait_all_loads();
-        lds_barrier();
-        const uint32_t next = octets_of(page);
-        if (t + 1 < t_end) fetch(a, there, kbase, vbase, (t + 1) * kKeys, page, wave, lane);
-        page = page_of(t + 2);
-        if (active) compute(here, t, now);
-        now = next;
-        return ++t < t_end;
-      };
-      while (step(st0, st1) && step(st1, st0)) {
+    Pages next;
+    if (t + kAhead < t_end) next = pages_of(t + kAhead);
+    wait_loads<0>();  // the queries among them
+    for (; t < t_end; ++t) {
+      // This step's tiles have arrived, for all wavefronts, and its predecessor's place is free.
+      if (t + kAhead <= t_end) wait_loads<(kAhead - 1) * Ring::kCopies>();
+      else wait_loads<0>();
+      lds_barrier();
+      const int tn = t + kAhead;
+      if (tn < t_end) {
+        queue |= there(next) << (4 * kS * kAhead);
+        fetch_step(tn, next);
       }
+      if (active) {
+#pragma unroll
+        for (int u = 0; u < kS; u += kU)
+          if (u == 0 || t * kStepKeys + 32 * u < end)
+            compute(ring + (t % Ring::kSteps) * Ring::kStep + u * Ring::kTile, t * kStepKeys + 32 * u,
+                    queue >> (4 * u) & ((1u << (4 * kU)) - 1));
+      }
+      queue >>= 4 * kS;
+      if (tn + 1 < t_end) next = pages_of(tn + 1);
     }
     if (!active) return;
 
@@ -303,23 +386,18 @@ struct WideSegment {
         const float inv = l[i] == 0.f ? 0.f : vs / l[i];
         uint16_t* out = a.out + row * a.out_stride + (int64_t)head * kDh;
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-          for (int d = 0; d < Tl::kDims; d += 4) {
-            uint2 four;
-            four.x = T::down(acc[i][d][x] * inv) | (T::down(acc[i][d + 1][x] * inv) << 16);
-            four.y = T::down(acc[i][d + 2][x] * inv) | (T::down(acc[i][d + 3][x] * inv) << 16);
-            *reinterpret_cast<uint2*>(out + Tl::out_dim(4 * g4 + x, d)) = four;
-          }
+        for (int d = 0; d < kBlocks; ++d) {
+          uint2 four;
+          four.x = pair_down(T(), acc[i][d][0] * inv, acc[i][d][1] * inv);
+          four.y = pair_down(T(), acc[i][d][2] * inv, acc[i][d][3] * inv);
+          *reinterpret_cast<uint2*>(out + 16 * d + 4 * g4) = four;
+        }
         if (g4 == 0 && a.lse)
           a.lse[row * a.n_heads + head] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * 0.6931471805599453f;
       } else {
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-          for (int d = 0; d < Tl::kDims; d += 4)
-            *reinterpret_cast<float4*>(part + 2 * block_columns + c * kDh + Tl::out_dim(4 * g4 + x, d)) =
-                make_float4(acc[i][d][x], acc[i][d + 1][x], acc[i][d + 2][x], acc[i][d + 3][x]);
+        for (int d = 0; d < kBlocks; ++d)
+          *reinterpret_cast<f32x4*>(part + 2 * block_columns + c * kDh + 16 * d + 4 * g4) = acc[i][d];
         if (g4 == 0) {
           part[c] = m[i];
           part[block_columns + c] = l[i];
@@ -331,7 +409,7 @@ struct WideSegment {
 
 // As paged_tree_kernel, but a block has 64 * kTiles columns and its four wavefronts take
 // every fourth tile of 16 of them: all of them read the same keys, which come into LDS
-// by direct copies, two steps in turn.  A wavefront so has few columns' statistics and
+// by direct copies, a ring of tiles ahead.  A wavefront so has few columns' statistics and
 // outputs, and two wavefronts to a SIMD have room for them.
 template <class T, bool kE4M3, int kDh, int kTiles, bool kShaped>
 __global__ __launch_bounds__(64 * kTreeWaves, 2) void paged_tree_wide_kernel(TreeArg a) {
@@ -348,7 +426,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void paged_tree_wide_kernel(Tre
     hk = pair % a.kv.n_kv_heads;
   }
   TreeChunk ch;
-  TreeRun r{1, 0, 1, 0, w, cb};
+  TreeRun r{0, 1, 0, w, cb, 1, 0};
   if (a.workers) {
     if (!find_run(a, w, kColumns, ch, r)) return;  // the same for the whole workgroup
   } else {
@@ -379,12 +457,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void paged_tree_wide_kernel(Tre
     else
       WideSegment<T, kE4M3, kDh, 1, kShaped>::run(a, r, w, hk, start, count, sq, n, first, end, units, s0, s1,
                                                   columns, kColumns, first_segment);
-    if (a.workers && s0 == 0 && threadIdx.x == 0) {
-      int32_t* h = a.heads_of + 3 * (((int64_t)r.tr * a.blocks + r.cb) * a.kv.n_kv_heads + hk);
-      h[0] = w;
-      h[1] = s1 == units ? 0 : (r.base + units - 1) / r.run - w + 1;
-      h[2] = first_segment ? 0 : 1;
-    }
+    if (a.workers && s0 == 0 && threadIdx.x == 0) note_parts(a, r, w, hk, units, s1, first_segment);
     r.u += s1 - s0;
     r.base += units;
     ++r.cb;
