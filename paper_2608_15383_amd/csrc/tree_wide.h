@@ -50,8 +50,11 @@ struct WideRing {
   }
 };
 
-// One block of columns of a tree over a run of its keys, of which this wavefront has
-// the tiles wave, wave + 4 .. of 16 columns.
+// One block of columns of a tree over a run of its keys.  The four wavefronts have every
+// fourth tile of 16 columns each, of all keys; or, where half of the block's tiles suffice,
+// two of them every second tile of columns, of the first tile of keys of each step, and
+// two the same columns of the second: what each makes of keys and values (reads,
+// conversions) then serves as many columns again.
 template <class T, bool kE4M3, int kDh, int kTiles, bool kShaped>
 struct WideSegment {
   typedef WideTile<T, kE4M3, kDh, kTiles> Tl;
@@ -124,7 +127,9 @@ struct WideSegment {
                                              int s1, int columns, int block_columns, bool first_segment) {
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l16 = lane & 15, g4 = lane >> 4;
-    const bool active = 16 * wave < columns;
+    const bool halves = kU < Ring::kStepTiles && columns <= 32 * kTiles;
+    const int apart = halves ? 2 : 4, cg = wave & (apart - 1), kg = halves ? wave >> 1 : 0;
+    const bool active = 16 * cg < columns;
 
     float scale = a.scale;
     if (!kShaped) scale *= 1.4426950408889634f;
@@ -189,7 +194,7 @@ struct WideSegment {
     float m[kTiles], l[kTiles];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
-      const int c = 16 * (wave + 4 * i) + l16, col = r.cb * block_columns + c;
+      const int c = 16 * (cg + apart * i) + l16, col = r.cb * block_columns + c;
       node[i] = c < columns ? (int)((uint32_t)col / (uint32_t)a.group) : 0;
       const int head = hk * a.group + (c < columns ? col - node[i] * a.group : 0);
       slope[i] = 0.f;
@@ -362,12 +367,39 @@ struct WideSegment {
       if (active) {
 #pragma unroll
         for (int u = 0; u < kS; u += kU)
-          if (u == 0 || t * kStepKeys + 32 * u < end)
+          if ((!halves || u == kg) && (u == 0 || t * kStepKeys + 32 * u < end))
             compute(ring + (t % Ring::kSteps) * Ring::kStep + u * Ring::kTile, t * kStepKeys + 32 * u,
                     queue >> (4 * u) & ((1u << (4 * kU)) - 1));
       }
       queue >>= 4 * kS;
       if (tn + 1 < t_end) next = pages_of(tn + 1);
+    }
+    // Both halves' sums, by the wavefronts of the first.
+    if (halves) {
+      f32x4* sums = reinterpret_cast<f32x4*>(ring) + cg * kTiles * (kBlocks + 1) * 64 + lane;
+      static_assert(2 * kTiles * (kBlocks + 1) * 1024 <= Ring::kSteps * Ring::kStep || kU == Ring::kStepTiles, "");
+      lds_barrier();  // the ring's readers are done
+      if (kg == 1 && active) {
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+#pragma unroll
+          for (int c = 0; c < kBlocks; ++c) sums[(i * (kBlocks + 1) + c) * 64] = acc[i][c];
+          sums[(i * (kBlocks + 1) + kBlocks) * 64] = f32x4{m[i], l[i], 0.f, 0.f};
+        }
+      }
+      lds_barrier();
+      if (kg == 1) return;
+      if (active) {
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+          const f32x4 ml = sums[(i * (kBlocks + 1) + kBlocks) * 64];
+          const float M = fmaxf(m[i], ml[0]), f0 = part_weight(m[i], M), f1 = part_weight(ml[0], M);
+          m[i] = M;
+          l[i] = l[i] * f0 + ml[1] * f1;
+#pragma unroll
+          for (int c = 0; c < kBlocks; ++c) acc[i][c] = acc[i][c] * f0 + sums[(i * (kBlocks + 1) + c) * 64] * f1;
+        }
+      }
     }
     if (!active) return;
 
@@ -378,7 +410,7 @@ struct WideSegment {
     for (int i = 0; i < kTiles; ++i) {
       l[i] += __shfl_xor(l[i], 16);
       l[i] += __shfl_xor(l[i], 32);
-      const int c = 16 * (wave + 4 * i) + l16;
+      const int c = 16 * (cg + apart * i) + l16;
       if (c >= columns) continue;
       if (full) {
         const int64_t row = start + node[i];
@@ -407,10 +439,10 @@ struct WideSegment {
   }
 };
 
-// As paged_tree_kernel, but a block has 64 * kTiles columns and its four wavefronts take
-// every fourth tile of 16 of them: all of them read the same keys, which come into LDS
-// by direct copies, a ring of tiles ahead.  A wavefront so has few columns' statistics and
-// outputs, and two wavefronts to a SIMD have room for them.
+// As paged_tree_kernel, but a block has 64 * kTiles columns, which the four wavefronts
+// share: all of them read the same keys, which come into LDS by direct copies, a ring of
+// steps ahead.  A wavefront so has few columns' statistics and outputs, and two
+// wavefronts to a SIMD have room for them.
 template <class T, bool kE4M3, int kDh, int kTiles, bool kShaped>
 __global__ __launch_bounds__(64 * kTreeWaves, 2) void paged_tree_wide_kernel(TreeArg a) {
   constexpr int kColumns = 64 * kTiles;
@@ -451,12 +483,8 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void paged_tree_wide_kernel(Tre
     const int units = a.workers ? __builtin_amdgcn_readlane(ch.units, i64) : 1;
     const int s0 = r.u - r.base, s1 = min(units, s0 + (r.u_end - r.u));
     const int columns = min(kColumns, count * a.group - r.cb * kColumns);
-    if (kTiles > 1 && columns > 64)
-      WideSegment<T, kE4M3, kDh, kTiles, kShaped>::run(a, r, w, hk, start, count, sq, n, first, end, units, s0, s1,
-                                                       columns, kColumns, first_segment);
-    else
-      WideSegment<T, kE4M3, kDh, 1, kShaped>::run(a, r, w, hk, start, count, sq, n, first, end, units, s0, s1,
-                                                  columns, kColumns, first_segment);
+    WideSegment<T, kE4M3, kDh, kTiles, kShaped>::run(a, r, w, hk, start, count, sq, n, first, end, units, s0, s1,
+                                                     columns, kColumns, first_segment);
     if (a.workers && s0 == 0 && threadIdx.x == 0) note_parts(a, r, w, hk, units, s1, first_segment);
     r.u += s1 - s0;
     r.base += units;
