@@ -86,7 +86,8 @@ typedef struct emoe_paged_tree_args {
   float cap;                  /* 0: none; else 2^-60 .. 2^60 */
   int32_t dtype;              /* of q and out: EMOE_BF16 or EMOE_F16; a 16-bit cache has the same */
   int32_t rows, trees;        /* >= 0 */
-  int32_t n_heads;            /* a multiple of n_kv_heads, at most 2^20 */
+  int32_t n_heads;            /* a multiple of n_kv_heads, at most 2^20; those of a key head times
+                                 max_nodes at most 2^20 */
   int32_t n_seqs, table_width;
   int32_t max_keys;           /* bound of lengths[] and nodes together, 0 .. 2^30 */
   int32_t max_nodes;          /* bound of a tree's nodes, 1 .. 64 */

@@ -40,6 +40,32 @@ void launch_tree_fp16(const TreeArg& a, const TreePlan& p, int head_dim, bool e4
 
 constexpr int kTreeWaves = 4;
 
+// A kernel's arguments lie in memory of the host, a microsecond away, and where scalar
+// registers run out the compiler reads them again in the middle of the kernel (30 trees of
+// 46 keys 24 us instead of 10).  Values that it knows nothing of are kept, in lanes of
+// vector registers if need be.
+template <class P>
+__device__ __forceinline__ void keep_argument(P*& p) {
+  auto g = (__attribute__((address_space(1))) P*)p;
+  asm volatile("" : "+s"(g));
+  p = (P*)g;
+}
+template <class V>
+__device__ __forceinline__ void keep_argument(V& v) {
+  asm volatile("" : "+s"(v));
+}
+template <class... V>
+__device__ __forceinline__ void keep_arguments(V&... v) {
+  (keep_argument(v), ...);
+}
+__device__ __forceinline__ void keep_arguments(TreeArg& a) {
+  keep_arguments(a.kv.k, a.kv.v, a.kv.k_scale, a.kv.v_scale, a.kv.page_bytes, a.kv.slot_bytes, a.kv.head_bytes,
+                 a.kv.n_pages, a.kv.page_log2, a.kv.n_kv_heads, a.q, a.out, a.lse, a.lengths, a.starts, a.seqs,
+                 a.table, a.tree, a.slopes, a.heads_of, a.parts, a.q_stride, a.out_stride, a.table_stride, a.scale,
+                 a.cap, a.tree0, a.trees, a.rows, a.n_heads, a.group, a.blocks, a.n_seqs, a.table_width, a.max_keys,
+                 a.max_nodes, a.window, a.workers, a.slack, a.unit_keys, a.unit_log2, a.part_floats);
+}
+
 // A tree: its rows, and the keys [first, end) that some node of it may see, of
 // which those from n on are its nodes.
 struct TreeSpan {
@@ -47,17 +73,19 @@ struct TreeSpan {
 };
 __device__ __forceinline__ TreeSpan tree_span(const TreeArg& a, int g) {
   TreeSpan s;
-  int64_t count = a.max_nodes;
+  const int length = a.lengths[g];
+  int next = 0;
+  s.start = g * a.max_nodes;
+  s.seq = g;
   if (a.starts) {
     s.start = a.starts[g];
-    count = (int64_t)a.starts[g + 1] - s.start;
-    if (s.start < 0 || s.start > a.rows) s.start = a.rows;
-  } else {
-    s.start = g * a.max_nodes;
+    next = a.starts[g + 1];
   }
+  if (a.seqs) s.seq = a.seqs[g];
+  const int64_t count = a.starts ? (int64_t)next - s.start : a.max_nodes;
+  if (s.start < 0 || s.start > a.rows) s.start = a.rows;
   s.count = (int)max((int64_t)0, min(count, (int64_t)min(a.max_nodes, a.rows - s.start)));
-  s.seq = a.seqs ? a.seqs[g] : g;
-  s.n = min(a.lengths[g], 1 << 30);
+  s.n = min(length, 1 << 30);
   s.first = s.end = 0;
   if ((uint32_t)s.seq < (uint32_t)a.n_seqs && s.n >= 0) {
     const int64_t most = min((int64_t)a.max_keys, (int64_t)a.table_width << a.kv.page_log2);
@@ -103,6 +131,22 @@ __device__ __forceinline__ void cap_scores(float (&x)[kKeys], float cap, float i
     const float near = fmaf(y * z, s, y);
     x[j] = cap * (any_far && !(fabsf(y) < 0.3f) ? far[j] : near);
   }
+}
+
+// Lane group kg's weight j of each column.
+template <int kKeys>
+__device__ __forceinline__ float weight_of(const float (&p)[kKeys], int j, int kg) {
+  float own = p[0];
+#pragma unroll
+  for (int k = 1; k < kKeys; ++k) own = j == k ? p[k] : own;
+  return __shfl(own, 16 * kg + (lane_id() & 15));
+}
+// sum + weight * v where the column sees it.
+__device__ __forceinline__ f32x4 add_where(bool sees, float weight, const f32x4& v, const f32x4& sum) {
+  f32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = sees ? fmaf(weight, v[i], sum[i]) : sum[i];
+  return r;
 }
 
 // Tile (paged.h) for kTiles tiles of 16 columns, so that what is made of keys and
@@ -176,38 +220,58 @@ struct WideTile : Tile<T, kE4M3, kDh> {
     if constexpr (kW + 1 < B::kDims / 2) wide_add<kW + 1>(hi, lo, acc);
   }
 
-  __device__ static __forceinline__ int dim(int c, int g, int r) { return B::out_dim(4 * g + r, c); }
+  // Adds the values of the lanes' key j, of one lane group alone (`here`), times the
+  // columns' weights to those that see it: a weight of 1 brings them to the output's lanes.
+  template <int kW>
+  __device__ __forceinline__ void add_key(int j, bool here, const float (&weight)[kTiles],
+                                          const bool (&sees_it)[kTiles], f32x4 (&acc)[kTiles][B::kDims]) const {
+    constexpr uint32_t kOne = B::kF16Weights ? 0x3c00u : 0x3f80u;
+    uint32_t e[4], o[4], ones[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t a = this->template pair<kW>(2 * i), b = this->template pair<kW>(2 * i + 1);
+      const uint32_t mask = here && (j >> 1) == i ? (j & 1 ? 0xffff0000u : 0xffffu) : 0u;
+      e[i] = __builtin_amdgcn_perm(b, a, 0x05040100u) & mask;
+      o[i] = __builtin_amdgcn_perm(b, a, 0x07060302u) & mask;
+      ones[i] = (kOne | kOne << 16) & mask;
+    }
+    const uint4 one = make_uint4(ones[0], ones[1], ones[2], ones[3]);
+    const f32x4 ve = HW::mfma(make_uint4(e[0], e[1], e[2], e[3]), one, f32x4{0.f, 0.f, 0.f, 0.f});
+    const f32x4 vo = HW::mfma(make_uint4(o[0], o[1], o[2], o[3]), one, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+      acc[n][2 * kW] = add_where(sees_it[n], weight[n], ve, acc[n][2 * kW]);
+      acc[n][2 * kW + 1] = add_where(sees_it[n], weight[n], vo, acc[n][2 * kW + 1]);
+    }
+    if constexpr (kW + 1 < B::kDims / 2) add_key<kW + 1>(j, here, weight, sees_it, acc);
+  }
 
-  // Which of a lane's 8 keys have an infinity or a NaN among its values.
-  __device__ __forceinline__ uint32_t not_finite() const {
-    constexpr uint32_t kExp = kE4M3 ? 0x7f7f7f7fu : (T::kType == EMOE_F16 ? 0x7c007c00u : 0x7f807f80u);
-    uint32_t bad = 0;
+  // Whether any of a lane's values is infinite or NaN: an exponent of all ones carries.
+  __device__ __forceinline__ bool any_not_finite() const {
+    constexpr uint32_t kAbs = kE4M3 ? 0x7f7f7f7fu : 0x7fff7fffu;
+    constexpr uint32_t kOne = kE4M3 ? 0x01010101u : T::kType == EMOE_F16 ? 0x04000400u : 0x00800080u;
+    uint32_t any = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
-      for (int w = 0; w < B::kVWords; ++w) {
-        const uint32_t x = this->v[j][w] & kExp;
-        if constexpr (kE4M3) {
+      for (int w = 0; w < B::kVWords; ++w) any |= (this->v[j][w] & kAbs) + kOne;
+    return (any & ~kAbs) != 0;
+  }
+  // Which of its 8 keys have such a value.
+  __device__ __forceinline__ uint32_t not_finite() const {
+    constexpr uint32_t kAbs = kE4M3 ? 0x7f7f7f7fu : 0x7fff7fffu;
+    constexpr uint32_t kOne = kE4M3 ? 0x01010101u : T::kType == EMOE_F16 ? 0x04000400u : 0x00800080u;
+    uint32_t bad = 0;
 #pragma unroll
-          for (int b = 0; b < 32; b += 8) bad |= ((x >> b) & 0x7fu) == 0x7fu ? 1u << j : 0u;
-        } else {
-          bad |= (x & 0xffffu) == (kExp & 0xffffu) || (x >> 16) == (kExp >> 16) ? 1u << j : 0u;
-        }
-      }
+    for (int j = 0; j < 8; ++j) {
+      uint32_t any = 0;
+#pragma unroll
+      for (int w = 0; w < B::kVWords; ++w) any |= (this->v[j][w] & kAbs) + kOne;
+      bad |= (any & ~kAbs) != 0 ? 1u << j : 0u;
+    }
     return bad;
   }
 };
-
-// One value of the cache, as the formula takes it (before v_scale).
-template <class T, bool kE4M3>
-__device__ __forceinline__ float cache_value(const uint8_t* at) {
-  if constexpr (kE4M3) {
-    const uint32_t pair = Half16<Bf16>::from_e4m3<false>((uint32_t)*at);
-    return bf16_to_f32(pair & 0xffffu);
-  } else {
-    return T::up(*reinterpret_cast<const uint16_t*>(at));
-  }
-}
 
 // The scores of a tile in powers of two: capped, and less the bias by distance.
 // key_at[j] is the key's place from the tree's first node on: below 0 its position,
@@ -236,12 +300,33 @@ __device__ __forceinline__ void shape_scores(float (&z)[kTiles][kKeys], float ca
     }
 }
 
-// Whether a node with this mask and depth sees the key at key_at (as above, its own
-// depth key_depth) that has a page.
-__device__ __forceinline__ bool node_sees(uint64_t mask, int deep, int key_at, int key_depth, int window) {
-  bool yes = key_at < 0 || ((mask >> (key_at & 63)) & 1);
-  if (window > 0) yes = yes && (key_at < 0 ? key_at : key_depth) > deep - window;
-  return yes;
+// Which of the keys key0 .. key0 + 31 there are: within [first, end), in an octet that
+// has a page (4 bits).
+__device__ __forceinline__ uint32_t keys_there(int key0, int first, int end, uint32_t octets) {
+  uint32_t bits = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bits |= octets >> i & 1 ? 0xffu << (8 * i) : 0u;
+  if (first > key0) bits &= first - key0 > 31 ? 0u : ~0u << (first - key0);
+  if (end - key0 < 32) bits &= end <= key0 ? 0u : (1u << (end - key0)) - 1;
+  return bits;
+}
+// Which of them a node of this mask and depth sees, the tree's nodes being the keys from
+// n on; depth: that of node i in lane i.
+__device__ __forceinline__ uint32_t keys_seen(int key0, int n, uint64_t mask, int deep, int window, int depth) {
+  const int old = n - key0;  // keys before the tree
+  uint32_t bits = old >= 32 ? ~0u : old > 0 ? (uint32_t)(mask << old) | ((1u << old) - 1)
+                                  : -old < 64 ? (uint32_t)(mask >> -old) : 0u;
+  if (window > 0) {
+    const int low = old + deep - window + 1;  // the first old key within the window
+    const uint32_t nodes = old >= 32 ? 0u : old > 0 ? ~0u << old : ~0u;
+    bits &= nodes | (low > 31 ? 0u : low > 0 ? ~0u << low : ~0u);
+    if (window < 64) {
+#pragma unroll 1
+      for (int b = max(0, old); b < 32 && b - old < 64; ++b)
+        if (__builtin_amdgcn_readlane(depth, b - old) <= deep - window) bits &= ~(1u << b);
+    }
+  }
+  return bits;
 }
 
 // One tile's step of the softmax: weights p of the scores z, which a factor >= 0 makes
@@ -389,31 +474,6 @@ __device__ __forceinline__ uint4 signed_chunk(const uint16_t* at, uint32_t flip)
   return make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
 }
 
-// Adds one key's values, which are at `row`, weighted by p of lane group kg's key j, to
-// the columns that see it: lanes hold dimensions of their own.
-template <class T, bool kE4M3, class Tl, class Out, int kTiles, int kAcc, int kKeys>
-__device__ __forceinline__ void add_one_key(const uint8_t* row, int j, int kg, const float (&p)[kTiles][kKeys],
-                                            const bool (&seen)[kTiles], f32x4 (&acc)[kTiles][kAcc]) {
-  const int lane = lane_id(), l16 = lane & 15, g4 = lane >> 4;
-  float weight[kTiles];
-#pragma unroll
-  for (int i = 0; i < kTiles; ++i) {
-    float own = p[i][0];
-#pragma unroll
-    for (int k = 1; k < kKeys; ++k) own = j == k ? p[i][k] : own;
-    weight[i] = __shfl(own, 16 * kg + l16);
-  }
-#pragma unroll
-  for (int r = 0; r < 4; ++r)
-#pragma unroll
-    for (int c = 0; c < kAcc; ++c) {
-      const float v = cache_value<T, kE4M3>(row + Out::dim(c, g4, r) * Tl::kItem);
-#pragma unroll
-      for (int i = 0; i < kTiles; ++i) acc[i][c][r] = seen[i] ? fmaf(weight[i], v, acc[i][c][r]) : acc[i][c][r];
-      asm volatile("" ::: "memory");  // one load after the other: this is rare, registers are not to spare
-    }
-}
-
 // The trees of a chunk of 64, one per lane.
 struct TreeChunk {
   TreeSpan span;
@@ -487,6 +547,17 @@ __device__ __forceinline__ bool find_run(const TreeArg& a, int w, int columns, T
     r.base += all;
   }
 }
+// All of it the same for the whole wavefront, which the compiler does not see of loops
+// whose ends depend on other lanes' values.
+__device__ __forceinline__ void make_uniform(TreeRun& r) {
+  r.u = __builtin_amdgcn_readfirstlane(r.u);
+  r.u_end = __builtin_amdgcn_readfirstlane(r.u_end);
+  r.base = __builtin_amdgcn_readfirstlane(r.base);
+  r.tr = __builtin_amdgcn_readfirstlane(r.tr);
+  r.cb = __builtin_amdgcn_readfirstlane(r.cb);
+  r.run = __builtin_amdgcn_readfirstlane(r.run);
+  r.each = __builtin_amdgcn_readfirstlane(r.each);
+}
 // Leaves where the parts of an output are: first worker, parts (0: it is whole), and
 // which of its first worker's parts is the first.
 __device__ __forceinline__ void note_parts(const TreeArg& a, const TreeRun& r, int w, int hk, int units, int s1,
@@ -515,6 +586,7 @@ __device__ __forceinline__ void note_parts(const TreeArg& a, const TreeRun& r, i
 template <class T, bool kE4M3, int kDh, int kTiles, bool kShaped>
 __global__ __launch_bounds__(64 * kTreeWaves, kDh == 256 ? 1 : 2)
 void paged_tree_kernel(TreeArg a) {
+  keep_arguments(a);
   constexpr int kWaves = kTreeWaves, kThreads = 64 * kWaves, kColumns = 16 * kTiles;
   typedef WideTile<T, kE4M3, kDh, kTiles> Tl;
   constexpr int kRow = kDh + 4;  // padded: lanes 16 apart in dimensions, 1 in columns
@@ -525,21 +597,8 @@ void paged_tree_kernel(TreeArg a) {
   const uint32_t k_off = Tl::k_offset(lane, a.kv.slot_bytes);
   const uint32_t v_off = Tl::v_offset(lane, a.kv.slot_bytes);
 
-  // Workers of several key heads stand next to each other, as their keys do in memory.
-  // Where every output has a workgroup, a tree's blocks of one key head are 8 apart, on
-  // one die, so that its L2 serves what the others read again.
-  int w, hk, cb = 0;
-  if (a.workers) {
-    w = blockIdx.x / a.kv.n_kv_heads;
-    hk = blockIdx.x % a.kv.n_kv_heads;
-  } else {
-    const int chunk = blockIdx.x / (8 * a.blocks), at = blockIdx.x % (8 * a.blocks);
-    const int pairs = min(8, a.trees * a.kv.n_kv_heads - 8 * chunk), pair = 8 * chunk + at % pairs;
-    cb = at / pairs;
-    w = pair / a.kv.n_kv_heads;
-    hk = pair % a.kv.n_kv_heads;
-  }
-
+  // Workgroups of several key heads stand next to each other, as their keys do in memory.
+  const int hk = blockIdx.x, w = a.workers ? blockIdx.y : blockIdx.z, cb = a.workers ? 0 : blockIdx.y;
   TreeChunk ch;
   TreeRun r{0, 1, 0, w, cb, 1, 0};
   if (a.workers) {
@@ -561,7 +620,9 @@ void paged_tree_kernel(TreeArg a) {
   const int slot_mask = (1 << a.kv.page_log2) - 1;
   bool first_segment = true;
 
+  make_uniform(r);
   while (r.u < r.u_end) {
+    make_uniform(r);
     if (r.tr - ch.first >= 64) ch.load(a, r.tr & ~63, kColumns);
     const int i64 = __builtin_amdgcn_readfirstlane(r.tr - ch.first);
     if (r.cb >= __builtin_amdgcn_readlane(ch.blocks, i64)) {
@@ -579,13 +640,6 @@ void paged_tree_kernel(TreeArg a) {
     const int s0 = r.u - r.base, s1 = min(units, s0 + (r.u_end - r.u));
     const int columns = min(kColumns, count * a.group - r.cb * kColumns);
 
-    // What each node sees, and its depth: node i's in lane i.
-    uint64_t sees = 0;
-    if (lane < count)
-      sees = a.tree ? a.tree[start + lane] : (2ull << lane) - 1;
-    const int depth = __popcll(sees & ((1ull << lane) - 1));
-    const int deepest = a.window > 0 ? (int)wave_reduce_u32<true>((uint32_t)(lane < count ? depth : 0)) : 0;
-
     // This lane's columns: node, and what belongs to it.
     int node[kTiles];
     float slope[kTiles];
@@ -597,7 +651,6 @@ void paged_tree_kernel(TreeArg a) {
       node[i] = c < columns ? (int)((uint32_t)col / (uint32_t)a.group) : 0;
       const int head = hk * a.group + (c < columns ? col - node[i] * a.group : 0);
       slope[i] = 0.f;
-      deep_at[i] = kShaped ? __shfl(depth, node[i]) : 0;
       if (kShaped && a.slopes) slope[i] = a.slopes[head] * 1.4426950408889634f;
 #pragma unroll
       for (int s = 0; s < Tl::kSteps; ++s) {
@@ -621,8 +674,6 @@ void paged_tree_kernel(TreeArg a) {
     const int t_end = a.workers ? min(t0 + s1 * kWaves, t_all) : t_all;
     int t = t0 + s0 * kWaves + wave;
     const ConstI32 table = (ConstI32)(a.table + (int64_t)sq * a.table_stride);
-    // Keys of a tile that every column sees lie between these.
-    const int low = a.window > 0 ? max(0, n + deepest + 1 - a.window) : 0, high = min(n, end);
 
     auto place = [&](const Octets& o, int key0, int64_t (&off)[4]) {
 #pragma unroll
@@ -650,6 +701,17 @@ void paged_tree_kernel(TreeArg a) {
       load_v(off);
       if (t + kWaves < t_end) next = octets_of(a.kv, table, (t + kWaves) * kTileKeys, end);
     }
+    // What each node sees, and its depth: node i's in lane i.
+    uint64_t sees = 0;
+    if (lane < count)
+      sees = a.tree ? a.tree[start + lane] : (2ull << lane) - 1;
+    const int depth = __popcll(sees & ((1ull << lane) - 1));
+    const int deepest = a.window > 0 ? (int)wave_reduce_u32<true>((uint32_t)(lane < count ? depth : 0)) : 0;
+
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) deep_at[i] = kShaped ? __shfl(depth, node[i]) : 0;
+    // Keys of a tile that every column sees lie between these.
+    const int low = a.window > 0 ? max(0, n + deepest + 1 - a.window) : 0, high = min(n, end);
     while (t < t_end) {
       const int key0 = t * kTileKeys, tn = t + kWaves;
       const bool more = tn < t_end;
@@ -674,47 +736,49 @@ void paged_tree_kernel(TreeArg a) {
         for (int j = 0; j < 8; ++j) key_at[j] = key_of(j, g4) - n;
         shape_scores(z, a.cap, inv_cap, a.slopes != nullptr, slope, deep_at, key_at, key0 + kTileKeys > n, depth);
       }
-      uint32_t there = 0xff, bad = 0;
+      uint32_t bad = 0, seen[kTiles];
       if (!whole) {
-        there = 0;
+        uint32_t octets = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int key = key_of(j, g4);
-          if (key >= first && key < end && (uint32_t)now.page[j >> 1] < (uint32_t)a.kv.n_pages)
-            there |= 1u << j;
+        for (int i = 0; i < 4; ++i) octets |= (uint32_t)now.page[i] < (uint32_t)a.kv.n_pages ? 1u << i : 0u;
+        const uint32_t there = keys_there(key0, first, end, octets), own = there >> (2 * g4);
+        uint32_t keep = 0;  // a bit for each of the lane's keys
+#pragma unroll
+        for (int j = 0; j < 8; ++j) keep |= (own >> (8 * (j >> 1) + (j & 1)) & 1) << j;
+        tile.clear_v(keep);
+        if (__builtin_expect(__any(tile.any_not_finite()), 0)) {
+          bad = tile.not_finite();
+          bad |= __shfl_xor(bad, 1);
+          bad |= __shfl_xor(bad, 2);
+          bad |= __shfl_xor(bad, 4);
+          bad |= __shfl_xor(bad, 8);
         }
-        bad = tile.not_finite() & there;
-        bad |= __shfl_xor(bad, 1);
-        bad |= __shfl_xor(bad, 2);
-        bad |= __shfl_xor(bad, 4);
-        bad |= __shfl_xor(bad, 8);
-        tile.clear_v(there & ~bad);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int key_at = key_of(j, g4) - n, key_depth = __shfl(depth, key_at & 63);
+        for (int i = 0; i < kTiles; ++i) {
+          seen[i] = there & keys_seen(key0, n, __shfl(sees, node[i]), __shfl(depth, node[i]), a.window, depth);
+          const uint32_t mine = seen[i] >> (2 * g4);
 #pragma unroll
-          for (int i = 0; i < kTiles; ++i) {
-            const uint64_t mask = __shfl(sees, node[i]);
-            const int deep = __shfl(depth, node[i]);
-            if (!((there >> j) & 1) || !node_sees(mask, deep, key_at, key_depth, a.window)) z[i][j] = -INFINITY;
-          }
+          for (int j = 0; j < 8; ++j) z[i][j] = mine >> (8 * (j >> 1) + (j & 1)) & 1 ? z[i][j] : -INFINITY;
         }
       }
       float p[kTiles][8];
       soft_step<Tl>(z, kShaped ? 1.f : scale, !whole, m, l, acc, p);
-      if (__any(bad != 0)) {
+      if (__builtin_expect(__any(bad != 0), 0)) {
+#pragma unroll 1
         for (int x = 0; x < 32; ++x) {
-          const int j = x & 7, kg = x >> 3, key = key_of(j, kg);
+          const int j = x & 7, kg = x >> 3;
           if (!((__builtin_amdgcn_readlane((int)bad, 16 * kg) >> j) & 1)) continue;
-          const uint8_t* row = vbase + table[key >> a.kv.page_log2] * a.kv.page_bytes +
-                               (int64_t)(key & slot_mask) * a.kv.slot_bytes;
-          const int key_depth = __shfl(depth, (key - n) & 63);
-          bool seen[kTiles];
+          const int at = 8 * (j >> 1) + 2 * kg + (j & 1);
+          float weight[kTiles];
+          bool sees_it[kTiles];
 #pragma unroll
-          for (int i = 0; i < kTiles; ++i)
-            seen[i] = node_sees(__shfl(sees, node[i]), __shfl(depth, node[i]), key - n, key_depth, a.window);
-          add_one_key<T, kE4M3, Tl, Tl>(row, j, kg, p, seen, acc);
+          for (int i = 0; i < kTiles; ++i) {
+            weight[i] = weight_of(p[i], j, kg);
+            sees_it[i] = seen[i] >> at & 1;
+          }
+          tile.template add_key<0>(j, g4 == kg, weight, sees_it, acc);
         }
+        tile.clear_v(~bad);
       }
       bool again = false;
       add_in_halves<Tl>(p, acc, [&](const uint4(&hi)[kTiles][1], const uint4(&lo)[kTiles][1]) __attribute__((always_inline)) {
@@ -809,6 +873,7 @@ void paged_tree_kernel(TreeArg a) {
 // dimension and part, and writes the output.
 template <class T, bool kE4M3, int kDh, int kStripes>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArg a, int tiles) {
+  keep_arguments(a);
   __shared__ float4 so[256];
   __shared__ float sm[256], sl[256];
   constexpr int kItems = 256 / kStripes, kFours = kDh / 4;

@@ -6,14 +6,15 @@ using namespace emoe;
 
 namespace {
 
-constexpr int kPlaces = 512, kWholeKeys = 256, kManyOutputs = 1024;
+constexpr int64_t kMostColumns = 1 << 20;  // query heads of a key head, of all nodes: blocks are a grid's second axis
+constexpr int kPlaces = 512, kWholeKeys = 512, kManyOutputs = 1024;
 
 TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int64_t max_keys,
                    int32_t max_nodes, int32_t window) {
   TreePlan p;
   const int64_t columns = (int64_t)(n_heads / kv.n_kv_heads) * max_nodes;
   const bool deep = kv.head_dim == 256;
-  p.wide = columns > (deep ? 16 : 32);
+  p.wide = columns > (kv.head_dim >= 128 ? 16 : 32);
   p.tiles = columns <= 16 ? 1 : !p.wide ? 2 : columns <= 64 || deep ? 4 : 8;
   p.blocks = (int)((columns + 16 * p.tiles - 1) / (16 * p.tiles));
   p.lines = kv.n_kv_heads * p.blocks;
@@ -28,7 +29,7 @@ TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int6
   p.trees_per_launch = (((int64_t)1 << 31) - 1 - kPlaces) / most_units;
   const bool whole = keys <= kWholeKeys || outputs >= kManyOutputs || kv.n_kv_heads > places ||
                      p.trees_per_launch < 1;
-  if (whole) p.trees_per_launch = trees;
+  if (whole) p.trees_per_launch = trees < 65535 ? trees : 65535;  // the grid's third axis
   const int64_t most_outputs = whole ? (int64_t)1 << 23 : kManyOutputs;
   if (p.trees_per_launch > most_outputs / p.lines) p.trees_per_launch = most_outputs / p.lines;
   p.workers = whole ? 0 : places / kv.n_kv_heads;
@@ -50,7 +51,8 @@ size_t emoe_paged_tree_attention_workspace_bytes(const emoe_paged_kv* kv, int32_
                                                  int32_t n_heads, int32_t max_keys,
                                                  int32_t max_nodes) {
   if (check_kv(kv) || trees < 0 || n_heads < 1 || n_heads % kv->n_kv_heads || max_keys < 0 ||
-      max_keys > kMostKeys || n_heads > kMostHeads || max_nodes < 1 || max_nodes > EMOE_MAX_NODES)
+      max_keys > kMostKeys || n_heads > kMostHeads || max_nodes < 1 || max_nodes > EMOE_MAX_NODES ||
+      (int64_t)(n_heads / kv->n_kv_heads) * max_nodes > kMostColumns)
     return 0;
   const TreePlan p = tree_plan(*kv, trees, n_heads, max_keys, max_nodes, 0);
   return 16 + shared_bytes(p) + (size_t)p.most_parts * p.part_floats * 4;
@@ -74,6 +76,9 @@ int32_t emoe_paged_tree_attention(const emoe_paged_kv* kv, const emoe_paged_tree
   if (A.max_keys > kMostKeys || A.n_heads > kMostHeads)
     return report_error(EMOE_ESHAPE, "max_keys %d or n_heads %d: need at most 2^30 and 2^20", A.max_keys,
                         A.n_heads);
+  if ((int64_t)(A.n_heads / kv->n_kv_heads) * A.max_nodes > kMostColumns)
+    return report_error(EMOE_ESHAPE, "%d query heads to a key head, of %d nodes: need a product of at most 2^20",
+                        A.n_heads / kv->n_kv_heads, A.max_nodes);
   if (!A.starts && A.rows != (int64_t)A.trees * A.max_nodes)
     return report_error(EMOE_ESHAPE, "%d rows without starts: need %d trees of %d nodes", A.rows, A.trees,
                         A.max_nodes);

@@ -25,7 +25,10 @@ __device__ __forceinline__ void lds_barrier() {
 // would have every read of LDS wait for all copies under way; it has no registers as
 // outputs, and the kernel itself waits for it.
 __device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(to), "v"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(
+                   __builtin_amdgcn_readfirstlane(to)),
+               "v"(from)
+               : "memory");
 }
 
 // A ring of tiles of 32 keys and their values in LDS.  Row r of a tile holds its 16-byte
@@ -66,18 +69,12 @@ struct WideSegment {
   // a product or a read is under way), and a lane's keys of them.
   static constexpr int kU = kTiles == 1 ? Ring::kStepTiles : 1, kKeys = 8 * kU;
   static constexpr int kBlocks = kDh / 16;            // of output dimensions
-  struct Out {                                       // dimension of row r of block c, in lane group g
-    __device__ static __forceinline__ int dim(int c, int g, int r) { return 16 * c + 4 * g + r; }
-  };
 
-  // Which of a lane's 8 keys have an infinity or a NaN among these values.
-  __device__ static __forceinline__ uint32_t not_finite(const uint4& v) {
-    constexpr uint32_t kExp = Tl::kF16Weights ? 0x7c00u : 0x7f80u;
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    uint32_t bad = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) bad |= ((w[j >> 1] >> (16 * (j & 1))) & kExp) == kExp ? 1u << j : 0u;
-    return bad;
+  // The halves of these values whose exponent is of ones only (infinities and NaN): each
+  // one's highest bit.
+  __device__ static __forceinline__ uint4 not_finite(const uint4& v) {
+    constexpr uint32_t kOne = Tl::kF16Weights ? 0x04000400u : 0x00800080u, kAbs = 0x7fff7fffu;
+    return make_uint4((v.x & kAbs) + kOne, (v.y & kAbs) + kOne, (v.z & kAbs) + kOne, (v.w & kAbs) + kOne);
   }
   // The values of the keys that are not in `keep` become 0.
   __device__ static __forceinline__ uint4 cleared_values(const uint4& v, uint32_t keep) {
@@ -286,49 +283,72 @@ struct WideSegment {
         shape_scores(z, a.cap, inv_cap, a.slopes != nullptr, slope, deep_at, key_at, key0 + 32 * kU > n, depth);
       }
       uint32_t bad = 0, keep = ~0u;
+      uint32_t seen[kTiles] = {}, seen_next[kTiles] = {};  // keys of the first and of the second tile
       const bool masked = !(key0 >= low && key0 + 32 * kU <= high && octets == (1u << (4 * kU)) - 1);
       if (masked) {
-        uint32_t there = 0;
+        keep = 0;
+        uint32_t any = 0;
 #pragma unroll
-        for (int j = 0; j < kKeys; ++j) {
-          const int at = key_of(j, g4), key = key0 + at;
-          if (key >= first && key < end && (octets >> (at >> 3)) & 1) there |= 1u << j;
-        }
+        for (int u = 0; u < kU; ++u) {
+          const uint32_t there = keys_there(key0 + 32 * u, first, end, octets >> (4 * u));
+          const uint32_t own = there >> (4 * g4);
+          keep |= ((own & 15) | (own >> 12 & 0xf0)) << (8 * u);
 #pragma unroll
-        for (int u = 0; u < kU; ++u)
-#pragma unroll 1
-          for (int c = 0; c < kBlocks; ++c) bad |= not_finite(values(c, u)) << (8 * u);
-        bad &= there;
-        bad |= __shfl_xor(bad, 1);
-        bad |= __shfl_xor(bad, 2);
-        bad |= __shfl_xor(bad, 4);
-        bad |= __shfl_xor(bad, 8);
-        keep = there & ~bad;
-#pragma unroll
-        for (int j = 0; j < kKeys; ++j) {
-          const int key_at = key0 + key_of(j, g4) - n, key_depth = __shfl(depth, key_at & 63);
+          for (int c = 0; c < kBlocks; ++c) {
+            const uint4 x = not_finite(cleared_values(values(c, u), keep >> (8 * u)));
+            any |= x.x | x.y | x.z | x.w;
+          }
 #pragma unroll
           for (int i = 0; i < kTiles; ++i) {
-            const uint64_t mask = __shfl(sees, node[i]);
-            const int deep = __shfl(depth, node[i]);
-            if (!((there >> j) & 1) || !node_sees(mask, deep, key_at, key_depth, a.window)) z[i][j] = -INFINITY;
+            const uint32_t bits =
+                there & keys_seen(key0 + 32 * u, n, __shfl(sees, node[i]), __shfl(depth, node[i]), a.window, depth);
+            if (u == 0) seen[i] = bits;
+            else seen_next[i] = bits;
+            const uint32_t mine = bits >> (4 * g4);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              z[i][8 * u + j] = mine >> (16 * (j >> 2) + (j & 3)) & 1 ? z[i][8 * u + j] : -INFINITY;
           }
+        }
+        if (__builtin_expect(__any((any & 0x80008000u) != 0), 0)) {
+#pragma unroll
+          for (int u = 0; u < kU; ++u)
+#pragma unroll 1
+            for (int c = 0; c < kBlocks; ++c) {
+              const uint4 x = not_finite(cleared_values(values(c, u), keep >> (8 * u)));
+              const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+              for (int j = 0; j < 8; ++j) bad |= (w[j >> 1] >> (16 * (j & 1) + 15) & 1) << (8 * u + j);
+            }
+          bad |= __shfl_xor(bad, 1);
+          bad |= __shfl_xor(bad, 2);
+          bad |= __shfl_xor(bad, 4);
+          bad |= __shfl_xor(bad, 8);
+          keep &= ~bad;
         }
       }
       soft_step<Tl>(z, kShaped ? 1.f : scale, masked, m, l, acc, p);
-      if (__any(bad != 0)) {
+      if (__builtin_expect(__any(bad != 0), 0)) {
 #pragma unroll 1
         for (int x = 0; x < 4 * kKeys; ++x) {
-          const int j = x % kKeys, kg = x / kKeys, key = key0 + key_of(j, kg);
+          const int j = x % kKeys, kg = x / kKeys, at = key_of(j, kg);
           if (!((__builtin_amdgcn_readlane((int)bad, 16 * kg) >> j) & 1)) continue;
-          const uint8_t* row = vbase + table[key >> a.kv.page_log2] * a.kv.page_bytes +
-                               (int64_t)(key & ((1 << a.kv.page_log2) - 1)) * a.kv.slot_bytes;
-          const int key_depth = __shfl(depth, (key - n) & 63);
-          bool seen[kTiles];
+          float weight[kTiles];
+          bool sees_it[kTiles];
 #pragma unroll
-          for (int i = 0; i < kTiles; ++i)
-            seen[i] = node_sees(__shfl(sees, node[i]), __shfl(depth, node[i]), key - n, key_depth, a.window);
-          add_one_key<T, kE4M3, Tl, Out>(row, j, kg, p, seen, acc);
+          for (int i = 0; i < kTiles; ++i) {
+            weight[i] = weight_of(p[i], j, kg);
+            sees_it[i] = (((uint64_t)seen_next[i] << 32 | seen[i]) >> at) & 1;
+          }
+          const uint32_t only = g4 == kg ? 1u << (j & 7) : 0u;
+          constexpr uint32_t kOne = Tl::kF16Weights ? 0x3c003c00u : 0x3f803f80u;
+          const uint4 one = cleared_values(make_uint4(kOne, kOne, kOne, kOne), only);
+#pragma unroll
+          for (int c = 0; c < kBlocks; ++c) {  // a weight of 1 brings its values to the output's lanes
+            const f32x4 v = Tl::HW::mfma(cleared_values(values(c, j >> 3), only), one, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) acc[i][c] = add_where(sees_it[i], weight[i], v, acc[i][c]);
+          }
         }
       }
       add_in_halves<Tl>(p, acc, [&](const uint4(&hi)[kTiles][kU], const uint4(&lo)[kTiles][kU])
@@ -445,18 +465,9 @@ struct WideSegment {
 // wavefronts to a SIMD have room for them.
 template <class T, bool kE4M3, int kDh, int kTiles, bool kShaped>
 __global__ __launch_bounds__(64 * kTreeWaves, 2) void paged_tree_wide_kernel(TreeArg a) {
+  keep_arguments(a);
   constexpr int kColumns = 64 * kTiles;
-  int w, hk, cb = 0;
-  if (a.workers) {
-    w = blockIdx.x / a.kv.n_kv_heads;
-    hk = blockIdx.x % a.kv.n_kv_heads;
-  } else {
-    const int chunk = blockIdx.x / (8 * a.blocks), at = blockIdx.x % (8 * a.blocks);
-    const int pairs = min(8, a.trees * a.kv.n_kv_heads - 8 * chunk), pair = 8 * chunk + at % pairs;
-    cb = at / pairs;
-    w = pair / a.kv.n_kv_heads;
-    hk = pair % a.kv.n_kv_heads;
-  }
+  const int hk = blockIdx.x, w = a.workers ? blockIdx.y : blockIdx.z, cb = a.workers ? 0 : blockIdx.y;
   TreeChunk ch;
   TreeRun r{0, 1, 0, w, cb, 1, 0};
   if (a.workers) {
@@ -466,7 +477,9 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void paged_tree_wide_kernel(Tre
     if (cb >= __builtin_amdgcn_readlane(ch.blocks, w & 63)) return;
   }
   bool first_segment = true;
+  make_uniform(r);
   while (r.u < r.u_end) {
+    make_uniform(r);
     if (r.tr - ch.first >= 64) ch.load(a, r.tr & ~63, kColumns);
     const int i64 = __builtin_amdgcn_readfirstlane(r.tr - ch.first);
     if (r.cb >= __builtin_amdgcn_readlane(ch.blocks, i64)) {
@@ -496,8 +509,8 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void paged_tree_wide_kernel(Tre
 // ---------------------------------------------------------------- launches
 template <class T, bool kE4M3, int kDh, int kTiles, bool kWide>
 void launch_tree_tiles(const TreeArg& a, const TreePlan& p, hipStream_t stream) {
-  const int64_t grid_x = a.workers ? (int64_t)a.workers * a.kv.n_kv_heads : (int64_t)a.trees * p.lines;
-  const dim3 grid((unsigned)grid_x), block(64 * kTreeWaves);
+  const dim3 block(64 * kTreeWaves);
+  const dim3 grid = a.workers ? dim3(a.kv.n_kv_heads, a.workers) : dim3(a.kv.n_kv_heads, a.blocks, a.trees);
   const bool shaped = a.cap > 0.f || a.slopes;
   if constexpr (kWide) {
     if (shaped)
@@ -530,7 +543,7 @@ void launch_tree_dim(const TreeArg& a, const TreePlan& p, hipStream_t stream) {
       if (p.tiles == 4) launch_tree_tiles<T, kE4M3, kDh, 1, true>(a, p, stream);
       else launch_tree_tiles<T, kE4M3, kDh, 2, true>(a, p, stream);
     }
-  } else if constexpr (kDh == 256) {
+  } else if constexpr (kDh >= 128) {
     launch_tree_tiles<T, kE4M3, kDh, 1, false>(a, p, stream);
   } else {
     if (p.tiles == 1) launch_tree_tiles<T, kE4M3, kDh, 1, false>(a, p, stream);
