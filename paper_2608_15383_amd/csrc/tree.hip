@@ -27,7 +27,7 @@ TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int6
   const int places = !p.wide && deep ? kPlaces / 2 : kPlaces;
   // A launch's units stay below 2^31, its threads below 2^32.
   p.trees_per_launch = (((int64_t)1 << 31) - 1 - kPlaces) / most_units;
-  const bool whole = keys <= kWholeKeys || outputs >= kManyOutputs || kv.n_kv_heads > places ||
+  const bool whole = keys <= (p.wide ? kWholeKeys / 2 : kWholeKeys) || outputs >= kManyOutputs || kv.n_kv_heads > places ||
                      p.trees_per_launch < 1;
   if (whole) p.trees_per_launch = trees < 65535 ? trees : 65535;  // the grid's third axis
   const int64_t most_outputs = whole ? (int64_t)1 << 23 : kManyOutputs;

@@ -21,10 +21,17 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
-// Copies 16 bytes per lane to LDS, at `to` + 16 * lane, past the caches (131,072 keys: 122 -> 104 us).  As assembly, since the compiler
-// would have every read of LDS wait for all copies under way; it has no registers as
-// outputs, and the kernel itself waits for it.
-__device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint32_t to) {
+// Copies 16 bytes per lane, from `from` + offset, to LDS, at `to` + 16 * lane, past the
+// caches (131,072 keys: 122 -> 104 us).  As assembly, since the compiler would have every
+// read of LDS wait for all copies under way; it has no registers as outputs, and the
+// kernel itself waits for it.
+__device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(
+                   __builtin_amdgcn_readfirstlane(to)),
+               "v"(offset), "s"(from)
+               : "memory");
+}
+__device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint32_t to) {  // from: of each lane
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(
                    __builtin_amdgcn_readfirstlane(to)),
                "v"(from)
@@ -50,6 +57,11 @@ struct WideRing {
   __device__ static __forceinline__ uint8_t* memory() {
     __shared__ __attribute__((aligned(1024))) uint8_t ring[kSteps * kStep];
     return ring;
+  }
+  // Of each step and wavefront, whether all octets that it copies are there.
+  __device__ static __forceinline__ uint32_t (*whole())[4] {
+    __shared__ __attribute__((aligned(16))) uint32_t words[kSteps][4];
+    return words;
   }
 };
 
@@ -109,8 +121,8 @@ struct WideSegment {
         const int row = i * kRowsAtOnce + in;
         const uint32_t slot = row * a.kv.slot_bytes;
         const uint32_t to = tile_at + (8 * wave + i * kRowsAtOnce) * kRow;
-        copy_to_lds(kbase + at + (slot + 16 * (chunk ^ Ring::swizzle(row))), to);
-        copy_to_lds(vbase + at + (slot + 16 * (chunk ^ Ring::swizzle_v(8 * wave + row))), to + Ring::kSide);
+        copy_to_lds(kbase + at, slot + 16 * (chunk ^ Ring::swizzle(row)), to);
+        copy_to_lds(vbase + at, slot + 16 * (chunk ^ Ring::swizzle_v(8 * wave + row)), to + Ring::kSide);
       }
     }
   }
@@ -144,38 +156,31 @@ struct WideSegment {
     const int t_end = a.workers ? min(t0 + s1, t_all) : t_all;
     uint8_t* ring = Ring::memory();
     const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)ring;
+    auto page_of = [&](int key) -> int { return key < end ? table[key >> a.kv.page_log2] : -1; };
     struct Pages {
-      Octets tile[kS];
+      int32_t tile[kS];
     };
-    auto pages_of = [&](int step) -> Pages {
+    auto pages_of = [&](int step) -> Pages {  // of the octets that this wavefront copies
       Pages o;
 #pragma unroll
-      for (int u = 0; u < kS; ++u) o.tile[u] = octets_of(a.kv, table, step * kStepKeys + 32 * u, end);
+      for (int u = 0; u < kS; ++u) o.tile[u] = page_of(step * kStepKeys + 32 * u + 8 * wave);
       return o;
     };
-    auto there = [&](const Pages& o) -> uint32_t {
-      uint32_t bits = 0;
-#pragma unroll
-      for (int i = 0; i < 4 * kS; ++i)
-        bits |= (uint32_t)o.tile[i >> 2].page[i & 3] < (uint32_t)a.kv.n_pages ? 1u << i : 0u;
-      return bits;
-    };
     auto fetch_step = [&](int step, const Pages& o) {
+      bool all = true;
 #pragma unroll
       for (int u = 0; u < kS; ++u) {
-        const Octets& x = o.tile[u];
-        const int page = wave == 0 ? x.page[0] : wave == 1 ? x.page[1] : wave == 2 ? x.page[2] : x.page[3];
+        all = all && (uint32_t)o.tile[u] < (uint32_t)a.kv.n_pages;
         fetch(a, ring_at + (step % Ring::kSteps) * Ring::kStep + u * Ring::kTile, kbase, vbase,
-              step * kStepKeys + 32 * u, page, wave, lane);
+              step * kStepKeys + 32 * u, o.tile[u], wave, lane);
       }
+      if (lane == 0) Ring::whole()[step % Ring::kSteps][wave] = all ? 1u : 0u;
     };
-    uint32_t queue = 0;  // which octets the steps from t on have, 4 kU bits each
     lds_barrier();  // the last segment's readers are done
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       if (t + i < t_end) {
         const Pages o = pages_of(t + i);
-        queue |= there(o) << (4 * kS * i);
         fetch_step(t + i, o);
       }
     }
@@ -221,7 +226,7 @@ struct WideSegment {
     const int v_swizzle = Ring::swizzle_v(v_row);
     constexpr int kHalf = kMixed ? 2048 : 16 * kRow;  // from row r to row r + 16
 
-    auto compute = [&](const uint8_t* held, int key0, uint32_t octets) __attribute__((always_inline)) {
+    auto compute = [&](const uint8_t* held, int key0, bool all) __attribute__((always_inline)) {
       f32x4 s[kTiles][2 * kU];
 #pragma unroll
       for (int i = 0; i < kTiles; ++i)
@@ -284,13 +289,17 @@ struct WideSegment {
       }
       uint32_t bad = 0, keep = ~0u;
       uint32_t seen[kTiles] = {}, seen_next[kTiles] = {};  // keys of the first and of the second tile
-      const bool masked = !(key0 >= low && key0 + 32 * kU <= high && octets == (1u << (4 * kU)) - 1);
+      const bool masked = !(key0 >= low && key0 + 32 * kU <= high && all);
       if (masked) {
         keep = 0;
         uint32_t any = 0;
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
-          const uint32_t there = keys_there(key0 + 32 * u, first, end, octets >> (4 * u));
+          uint32_t octets = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            octets |= (uint32_t)page_of(key0 + 32 * u + 8 * i) < (uint32_t)a.kv.n_pages ? 1u << i : 0u;
+          const uint32_t there = keys_there(key0 + 32 * u, first, end, octets);
           const uint32_t own = there >> (4 * g4);
           keep |= ((own & 15) | (own >> 12 & 0xf0)) << (8 * u);
 #pragma unroll
@@ -381,17 +390,16 @@ struct WideSegment {
       lds_barrier();
       const int tn = t + kAhead;
       if (tn < t_end) {
-        queue |= there(next) << (4 * kS * kAhead);
         fetch_step(tn, next);
       }
       if (active) {
+        const uint4 words = *reinterpret_cast<const uint4*>(Ring::whole()[t % Ring::kSteps]);
+        const bool all = __builtin_amdgcn_readfirstlane(words.x & words.y & words.z & words.w) != 0;
 #pragma unroll
         for (int u = 0; u < kS; u += kU)
           if ((!halves || u == kg) && (u == 0 || t * kStepKeys + 32 * u < end))
-            compute(ring + (t % Ring::kSteps) * Ring::kStep + u * Ring::kTile, t * kStepKeys + 32 * u,
-                    queue >> (4 * u) & ((1u << (4 * kU)) - 1));
+            compute(ring + (t % Ring::kSteps) * Ring::kStep + u * Ring::kTile, t * kStepKeys + 32 * u, all);
       }
-      queue >>= 4 * kS;
       if (tn + 1 < t_end) next = pages_of(tn + 1);
     }
     // Both halves' sums, by the wavefronts of the first.
