@@ -7,7 +7,7 @@ using namespace emoe;
 namespace {
 
 constexpr int64_t kMostColumns = 1 << 20;  // query heads of a key head, of all nodes: blocks are a grid's second axis
-constexpr int kPlaces = 512, kWholeKeys = 512, kManyOutputs = 1024;
+constexpr int kUnits = 256, kWholeKeys = 512, kManyOutputs = 1024;
 
 TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int64_t max_keys,
                    int32_t max_nodes, int32_t window) {
@@ -15,7 +15,7 @@ TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int6
   const int64_t columns = (int64_t)(n_heads / kv.n_kv_heads) * max_nodes;
   const bool deep = kv.head_dim == 256;
   p.wide = columns > (kv.head_dim >= 128 ? 16 : 32);
-  p.tiles = columns <= 16 ? 1 : !p.wide ? 2 : columns <= 64 || deep ? 4 : 8;
+  p.tiles = p.wide ? 4 : columns <= 16 ? 1 : 2;
   p.blocks = (int)((columns + 16 * p.tiles - 1) / (16 * p.tiles));
   p.lines = kv.n_kv_heads * p.blocks;
   const int64_t span = (int64_t)window + max_nodes;
@@ -24,9 +24,9 @@ TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int6
   p.unit_keys = !p.wide ? kTreeWaves * kTileKeys : deep && kv.dtype != EMOE_E4M3 ? kTileKeys : 2 * kTileKeys;
   const int64_t most_units = (keys / p.unit_keys + 2) * p.blocks;
   const int64_t outputs = (int64_t)trees * p.lines;
-  const int places = !p.wide && deep ? kPlaces / 2 : kPlaces;
+  const int places = p.wide ? kUnits * wide_workgroups(kv.head_dim, kv.dtype == EMOE_E4M3) : deep ? kUnits : 2 * kUnits;
   // A launch's units stay below 2^31, its threads below 2^32.
-  p.trees_per_launch = (((int64_t)1 << 31) - 1 - kPlaces) / most_units;
+  p.trees_per_launch = (((int64_t)1 << 31) - 1 - 4 * kUnits) / most_units;
   const bool whole = keys <= (p.wide ? kWholeKeys / 2 : kWholeKeys) || outputs >= kManyOutputs || kv.n_kv_heads > places ||
                      p.trees_per_launch < 1;
   if (whole) p.trees_per_launch = trees < 65535 ? trees : 65535;  // the grid's third axis

@@ -41,12 +41,13 @@ __device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint32_t to) { 
 // A ring of tiles of 32 keys and their values in LDS.  Row r of a tile holds its 16-byte
 // chunks in the order c ^ swizzle(r) (values: swizzle_v), so that lanes that read the same
 // chunk of several rows use all banks.  The kernel takes steps of two tiles (one of 512-byte
-// rows); two to four steps in up to 64 KB: two workgroups to a CU.
+// rows), as many as the LDS of its workgroup's share of a CU holds, up to four.
 template <int kDh, bool kE4M3>
 struct WideRing {
   static constexpr int kRow = kDh * (kE4M3 ? 1 : 2), kSide = 32 * kRow, kTile = 2 * kSide;
   static constexpr int kStepTiles = kRow == 512 ? 1 : 2, kStep = kStepTiles * kTile;
-  static constexpr int kSteps = 65536 / kStep < 4 ? 65536 / kStep : 4;
+  static constexpr int kFit = 160 * 1024 / wide_workgroups(kDh, kE4M3) / (kStep + 64);
+  static constexpr int kSteps = kFit < 4 ? kFit : 4;
   static constexpr int kCopies = kStep / 4096;  // of a wavefront and step
 
   __device__ static __forceinline__ int swizzle(int row) { return kRow == 64 ? (row >> 1) & 3 : row & 7; }
@@ -65,21 +66,19 @@ struct WideRing {
   }
 };
 
-// One block of columns of a tree over a run of its keys.  The four wavefronts have every
-// fourth tile of 16 columns each, of all keys; or, where half of the block's tiles suffice,
-// two of them every second tile of columns, of the first tile of keys of each step, and
-// two the same columns of the second: what each makes of keys and values (reads,
-// conversions) then serves as many columns again.
-template <class T, bool kE4M3, int kDh, int kTiles, bool kShaped>
+// One block of 64 columns of a tree over a run of its keys, 16 columns to a wavefront.
+template <class T, bool kE4M3, int kDh, bool kShaped>
 struct WideSegment {
+  static constexpr int kTiles = 1;  // of 16 columns, of a wavefront
+  static constexpr int kColumns = 64 * kTiles;
   typedef WideTile<T, kE4M3, kDh, kTiles> Tl;
   typedef WideRing<kDh, kE4M3> Ring;
   static constexpr int kRow = Ring::kRow, kItem = Tl::kItem;
   static constexpr int kSub = kE4M3 ? 2 : 1;         // steps of a 16-byte chunk of keys
   static constexpr int kChunks = kRow / 64;          // chunks of a lane
-  // Tiles of 32 keys that are taken together (two where registers allow: more to do while
-  // a product or a read is under way), and a lane's keys of them.
-  static constexpr int kU = kTiles == 1 ? Ring::kStepTiles : 1, kKeys = 8 * kU;
+  // Tiles of 32 keys of a step, which are taken together (more to do while a product or a
+  // read is under way), and a lane's keys of them.
+  static constexpr int kU = Ring::kStepTiles, kKeys = 8 * kU;
   static constexpr int kBlocks = kDh / 16;            // of output dimensions
 
   // The halves of these values whose exponent is of ones only (infinities and NaN): each
@@ -133,12 +132,10 @@ struct WideSegment {
 
   __device__ static __forceinline__ void run(const TreeArg& a, const TreeRun& r, int w, int hk, int start,
                                              int count, int sq, int n, int first, int end, int units, int s0,
-                                             int s1, int columns, int block_columns, bool first_segment) {
+                                             int s1, int columns, bool first_segment) {
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l16 = lane & 15, g4 = lane >> 4;
-    const bool halves = kU < Ring::kStepTiles && columns <= 32 * kTiles;
-    const int apart = halves ? 2 : 4, cg = wave & (apart - 1), kg = halves ? wave >> 1 : 0;
-    const bool active = 16 * cg < columns;
+    const bool active = 16 * wave < columns;
 
     float scale = a.scale;
     if (!kShaped) scale *= 1.4426950408889634f;
@@ -150,7 +147,7 @@ struct WideSegment {
     const uint8_t* vbase = a.kv.v + (int64_t)hk * a.kv.head_bytes;
     const ConstI32 table = (ConstI32)(a.table + (int64_t)sq * a.table_stride);
 
-    constexpr int kS = Ring::kStepTiles, kStepKeys = 32 * kS, kAhead = Ring::kSteps - 1;
+    constexpr int kStepKeys = 32 * kU, kAhead = Ring::kSteps - 1;
     const int t_all = (end + kStepKeys - 1) / kStepKeys, t0 = first / kStepKeys;
     int t = t0 + s0;
     const int t_end = a.workers ? min(t0 + s1, t_all) : t_all;
@@ -158,18 +155,18 @@ struct WideSegment {
     const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)ring;
     auto page_of = [&](int key) -> int { return key < end ? table[key >> a.kv.page_log2] : -1; };
     struct Pages {
-      int32_t tile[kS];
+      int32_t tile[kU];
     };
     auto pages_of = [&](int step) -> Pages {  // of the octets that this wavefront copies
       Pages o;
 #pragma unroll
-      for (int u = 0; u < kS; ++u) o.tile[u] = page_of(step * kStepKeys + 32 * u + 8 * wave);
+      for (int u = 0; u < kU; ++u) o.tile[u] = page_of(step * kStepKeys + 32 * u + 8 * wave);
       return o;
     };
     auto fetch_step = [&](int step, const Pages& o) {
       bool all = true;
 #pragma unroll
-      for (int u = 0; u < kS; ++u) {
+      for (int u = 0; u < kU; ++u) {
         all = all && (uint32_t)o.tile[u] < (uint32_t)a.kv.n_pages;
         fetch(a, ring_at + (step % Ring::kSteps) * Ring::kStep + u * Ring::kTile, kbase, vbase,
               step * kStepKeys + 32 * u, o.tile[u], wave, lane);
@@ -196,7 +193,7 @@ struct WideSegment {
     float m[kTiles], l[kTiles];
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
-      const int c = 16 * (cg + apart * i) + l16, col = r.cb * block_columns + c;
+      const int c = 16 * wave + l16, col = r.cb * kColumns + c;
       node[i] = c < columns ? (int)((uint32_t)col / (uint32_t)a.group) : 0;
       const int head = hk * a.group + (c < columns ? col - node[i] * a.group : 0);
       slope[i] = 0.f;
@@ -395,39 +392,9 @@ struct WideSegment {
       if (active) {
         const uint4 words = *reinterpret_cast<const uint4*>(Ring::whole()[t % Ring::kSteps]);
         const bool all = __builtin_amdgcn_readfirstlane(words.x & words.y & words.z & words.w) != 0;
-#pragma unroll
-        for (int u = 0; u < kS; u += kU)
-          if ((!halves || u == kg) && (u == 0 || t * kStepKeys + 32 * u < end))
-            compute(ring + (t % Ring::kSteps) * Ring::kStep + u * Ring::kTile, t * kStepKeys + 32 * u, all);
+        compute(ring + (t % Ring::kSteps) * Ring::kStep, t * kStepKeys, all);
       }
       if (tn + 1 < t_end) next = pages_of(tn + 1);
-    }
-    // Both halves' sums, by the wavefronts of the first.
-    if (halves) {
-      f32x4* sums = reinterpret_cast<f32x4*>(ring) + cg * kTiles * (kBlocks + 1) * 64 + lane;
-      static_assert(2 * kTiles * (kBlocks + 1) * 1024 <= Ring::kSteps * Ring::kStep || kU == Ring::kStepTiles, "");
-      lds_barrier();  // the ring's readers are done
-      if (kg == 1 && active) {
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-#pragma unroll
-          for (int c = 0; c < kBlocks; ++c) sums[(i * (kBlocks + 1) + c) * 64] = acc[i][c];
-          sums[(i * (kBlocks + 1) + kBlocks) * 64] = f32x4{m[i], l[i], 0.f, 0.f};
-        }
-      }
-      lds_barrier();
-      if (kg == 1) return;
-      if (active) {
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-          const f32x4 ml = sums[(i * (kBlocks + 1) + kBlocks) * 64];
-          const float M = fmaxf(m[i], ml[0]), f0 = part_weight(m[i], M), f1 = part_weight(ml[0], M);
-          m[i] = M;
-          l[i] = l[i] * f0 + ml[1] * f1;
-#pragma unroll
-          for (int c = 0; c < kBlocks; ++c) acc[i][c] = acc[i][c] * f0 + sums[(i * (kBlocks + 1) + c) * 64] * f1;
-        }
-      }
     }
     if (!active) return;
 
@@ -438,11 +405,11 @@ struct WideSegment {
     for (int i = 0; i < kTiles; ++i) {
       l[i] += __shfl_xor(l[i], 16);
       l[i] += __shfl_xor(l[i], 32);
-      const int c = 16 * (cg + apart * i) + l16;
+      const int c = 16 * wave + l16;
       if (c >= columns) continue;
       if (full) {
         const int64_t row = start + node[i];
-        const int head = hk * a.group + r.cb * block_columns + c - node[i] * a.group;
+        const int head = hk * a.group + r.cb * kColumns + c - node[i] * a.group;
         const float inv = l[i] == 0.f ? 0.f : vs / l[i];
         uint16_t* out = a.out + row * a.out_stride + (int64_t)head * kDh;
 #pragma unroll
@@ -457,24 +424,23 @@ struct WideSegment {
       } else {
 #pragma unroll
         for (int d = 0; d < kBlocks; ++d)
-          *reinterpret_cast<f32x4*>(part + 2 * block_columns + c * kDh + 16 * d + 4 * g4) = acc[i][d];
+          *reinterpret_cast<f32x4*>(part + 2 * kColumns + c * kDh + 16 * d + 4 * g4) = acc[i][d];
         if (g4 == 0) {
           part[c] = m[i];
-          part[block_columns + c] = l[i];
+          part[kColumns + c] = l[i];
         }
       }
     }
   }
 };
 
-// As paged_tree_kernel, but a block has 64 * kTiles columns, which the four wavefronts
-// share: all of them read the same keys, which come into LDS by direct copies, a ring of
-// steps ahead.  A wavefront so has few columns' statistics and outputs, and two
-// wavefronts to a SIMD have room for them.
-template <class T, bool kE4M3, int kDh, int kTiles, bool kShaped>
-__global__ __launch_bounds__(64 * kTreeWaves, 2) void paged_tree_wide_kernel(TreeArg a) {
+// As paged_tree_kernel, but a block has 64 columns, which the four wavefronts share: all of
+// them read the same keys, which come into LDS by direct copies, a ring of steps ahead.
+template <class T, bool kE4M3, int kDh, bool kShaped>
+__global__ __launch_bounds__(64 * kTreeWaves, wide_workgroups(kDh, kE4M3)) void paged_tree_wide_kernel(TreeArg a) {
   keep_arguments(a);
-  constexpr int kColumns = 64 * kTiles;
+  typedef WideSegment<T, kE4M3, kDh, kShaped> Segment;
+  constexpr int kColumns = Segment::kColumns;
   const int hk = blockIdx.x, w = a.workers ? blockIdx.y : blockIdx.z, cb = a.workers ? 0 : blockIdx.y;
   TreeChunk ch;
   TreeRun r{0, 1, 0, w, cb, 1, 0};
@@ -504,8 +470,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void paged_tree_wide_kernel(Tre
     const int units = a.workers ? __builtin_amdgcn_readlane(ch.units, i64) : 1;
     const int s0 = r.u - r.base, s1 = min(units, s0 + (r.u_end - r.u));
     const int columns = min(kColumns, count * a.group - r.cb * kColumns);
-    WideSegment<T, kE4M3, kDh, kTiles, kShaped>::run(a, r, w, hk, start, count, sq, n, first, end, units, s0, s1,
-                                                     columns, kColumns, first_segment);
+    Segment::run(a, r, w, hk, start, count, sq, n, first, end, units, s0, s1, columns, first_segment);
     if (a.workers && s0 == 0 && threadIdx.x == 0) note_parts(a, r, w, hk, units, s1, first_segment);
     r.u += s1 - s0;
     r.base += units;
@@ -522,9 +487,9 @@ void launch_tree_tiles(const TreeArg& a, const TreePlan& p, hipStream_t stream) 
   const bool shaped = a.cap > 0.f || a.slopes;
   if constexpr (kWide) {
     if (shaped)
-      hipLaunchKernelGGL((paged_tree_wide_kernel<T, kE4M3, kDh, kTiles, true>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((paged_tree_wide_kernel<T, kE4M3, kDh, true>), grid, block, 0, stream, a);
     else
-      hipLaunchKernelGGL((paged_tree_wide_kernel<T, kE4M3, kDh, kTiles, false>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((paged_tree_wide_kernel<T, kE4M3, kDh, false>), grid, block, 0, stream, a);
   } else {
     if (shaped)
       hipLaunchKernelGGL((paged_tree_kernel<T, kE4M3, kDh, kTiles, true>), grid, block, 0, stream, a);
@@ -545,12 +510,7 @@ void launch_tree_tiles(const TreeArg& a, const TreePlan& p, hipStream_t stream) 
 template <class T, bool kE4M3, int kDh>
 void launch_tree_dim(const TreeArg& a, const TreePlan& p, hipStream_t stream) {
   if (p.wide) {
-    if constexpr (kDh == 256) {
-      launch_tree_tiles<T, kE4M3, kDh, 1, true>(a, p, stream);
-    } else {
-      if (p.tiles == 4) launch_tree_tiles<T, kE4M3, kDh, 1, true>(a, p, stream);
-      else launch_tree_tiles<T, kE4M3, kDh, 2, true>(a, p, stream);
-    }
+    launch_tree_tiles<T, kE4M3, kDh, 1, true>(a, p, stream);
   } else if constexpr (kDh >= 128) {
     launch_tree_tiles<T, kE4M3, kDh, 1, false>(a, p, stream);
   } else {
