@@ -497,12 +497,13 @@ PyObject* accept_drafts(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 std::vector<emoe_paged_kv> layers(PyObject* o, int device) {
   if (!PyList_Check(o) && !PyTuple_Check(o)) refuse("kvs: need a list of PagedKV");
   const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+  static PyObject* const names[2] = {PyUnicode_InternFromString("address"), PyUnicode_InternFromString("index")};
   std::vector<emoe_paged_kv> out;
   out.reserve((size_t)n);
   for (Py_ssize_t i = 0; i < n; ++i) {
     PyObject* item = PySequence_Fast_GET_ITEM(o, i);
-    PyObject* address = PyObject_GetAttrString(item, "address");
-    PyObject* index = address ? PyObject_GetAttrString(item, "index") : nullptr;
+    PyObject* address = PyObject_GetAttr(item, names[0]);
+    PyObject* index = address ? PyObject_GetAttr(item, names[1]) : nullptr;
     int64_t at = 0, dev = -1;
     const bool good = index && PyLong_Check(address) && PyLong_Check(index);
     if (good) {

@@ -99,6 +99,11 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(CompactArg a) {
   __shared__ int64_t from[64], to[64];
   __shared__ int moves;
   const int g = blockIdx.x / a.blocks, tid = threadIdx.x;
+  const int item = (blockIdx.x % a.blocks) * kThreads + tid, per = a.kv.n_kv_heads << a.kv.piece_log2;
+  const int which = item / per, rest = item % per;
+  const int64_t in_slot =
+      (int64_t)(rest >> a.kv.piece_log2) * a.kv.head_bytes + 16 * (rest & ((1 << a.kv.piece_log2) - 1));
+  uint8_t* base = a.kv.pages[min(which, 2 * a.kv.layers - 1)] + in_slot;  // on its way with the moves
   if (tid < 64) {
     const int s = a.seqs ? a.seqs[g] : g, n = a.lengths[g];
     const int count = min(a.accepted[g], a.max_nodes);
@@ -121,12 +126,7 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(CompactArg a) {
     if (tid == 0) moves = __popcll(all);
   }
   __syncthreads();
-  const int item = (blockIdx.x % a.blocks) * kThreads + tid, per = a.kv.n_kv_heads << a.kv.piece_log2;
-  const int which = item / per, rest = item % per;
   if (which >= 2 * a.kv.layers) return;
-  const int64_t in_slot =
-      (int64_t)(rest >> a.kv.piece_log2) * a.kv.head_bytes + 16 * (rest & ((1 << a.kv.piece_log2) - 1));
-  uint8_t* base = a.kv.pages[which] + in_slot;
   for (int i0 = 0; i0 < moves; i0 += 8) {
     uint4 x[8];
 #pragma unroll

@@ -45,6 +45,9 @@ constexpr int wide_workgroups(int head_dim, bool e4m3) {
   return head_dim == 64 || (head_dim == 128 && e4m3) ? 3 : 2;
 }
 
+// Its steps' tiles of 32 keys.
+constexpr int wide_step_tiles(int head_dim, bool e4m3) { return !e4m3 && head_dim != 128 ? 1 : 2; }
+
 // A kernel's arguments lie in memory of the host, a microsecond away, and where scalar
 // registers run out the compiler reads them again in the middle of the kernel (30 trees of
 // 46 keys 24 us instead of 10).  Values that it knows nothing of are kept, in lanes of

@@ -7,13 +7,23 @@ using namespace emoe;
 namespace {
 
 constexpr int64_t kMostColumns = 1 << 20;  // query heads of a key head, of all nodes: blocks are a grid's second axis
-constexpr int kUnits = 256, kWholeKeys = 512, kManyOutputs = 1024;
+constexpr int kUnits = 256;  // CUs
 
+// Which kernel, and how its work is cut.
+//  - Up to 16 columns (32 of 64 dimensions) paged_tree_kernel, whose wavefronts take keys
+//    of their own straight from memory to registers; more paged_tree_wide_kernel, whose
+//    wavefronts share them: 26 columns, 2,026 keys of 16 heads of 128 17.7 and 16.3 us,
+//    52 columns 95 and 51 (19 trees of up to 8,192 keys).
+//  - An output, that is a block of columns of a tree and key head, has one workgroup where
+//    there are 1,024 outputs or more, or few keys; else its keys are cut over the workers
+//    of its key head (find_run) and tree_join_kernel joins the parts, in a launch that
+//    costs 4 us: 328 keys, 16 heads, whole and cut 16.7 and 12.9 us (wide), 504 keys, 16
+//    columns 11.8 and 12.7 (not wide).
 TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int64_t max_keys,
                    int32_t max_nodes, int32_t window) {
   TreePlan p;
   const int64_t columns = (int64_t)(n_heads / kv.n_kv_heads) * max_nodes;
-  const bool deep = kv.head_dim == 256;
+  const bool e4m3 = kv.dtype == EMOE_E4M3;
   p.wide = columns > (kv.head_dim >= 128 ? 16 : 32);
   p.tiles = p.wide ? 4 : columns <= 16 ? 1 : 2;
   p.blocks = (int)((columns + 16 * p.tiles - 1) / (16 * p.tiles));
@@ -21,23 +31,28 @@ TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int6
   const int64_t span = (int64_t)window + max_nodes;
   const int64_t keys = window > 0 && span < max_keys ? span : max_keys;
   // A step of the wide kernel; a tile for each wavefront of the other.
-  p.unit_keys = !p.wide ? kTreeWaves * kTileKeys : deep && kv.dtype != EMOE_E4M3 ? kTileKeys : 2 * kTileKeys;
+  p.unit_keys = kTileKeys * (p.wide ? wide_step_tiles(kv.head_dim, e4m3) : kTreeWaves);
   const int64_t most_units = (keys / p.unit_keys + 2) * p.blocks;
   const int64_t outputs = (int64_t)trees * p.lines;
-  const int places = p.wide ? kUnits * wide_workgroups(kv.head_dim, kv.dtype == EMOE_E4M3) : deep ? kUnits : 2 * kUnits;
-  // A launch's units stay below 2^31, its threads below 2^32.
+  const int places = kUnits * (p.wide ? wide_workgroups(kv.head_dim, e4m3) : kv.head_dim == 256 ? 1 : 2);
+  constexpr int kManyOutputs = 1024;
+  const bool may_cut = keys > (p.wide ? 256 : 512) && outputs < kManyOutputs && kv.n_kv_heads <= places;
+  // A launch's units stay below 2^31, its threads below 2^32, its trees within the grid's
+  // third axis.
   p.trees_per_launch = (((int64_t)1 << 31) - 1 - 4 * kUnits) / most_units;
-  const bool whole = keys <= (p.wide ? kWholeKeys / 2 : kWholeKeys) || outputs >= kManyOutputs || kv.n_kv_heads > places ||
-                     p.trees_per_launch < 1;
-  if (whole) p.trees_per_launch = trees < 65535 ? trees : 65535;  // the grid's third axis
+  const bool whole = !may_cut || p.trees_per_launch < 1;
+  if (whole) p.trees_per_launch = trees < 65535 ? trees : 65535;
   const int64_t most_outputs = whole ? (int64_t)1 << 23 : kManyOutputs;
   if (p.trees_per_launch > most_outputs / p.lines) p.trees_per_launch = most_outputs / p.lines;
   p.workers = whole ? 0 : places / kv.n_kv_heads;
+  // How much longer than equal runs the parts may be: 40 trees over 8 bits within 1% of 163
+  // us from 4 to 40.
   p.slack = p.wide ? 12 : 6;
   p.part_floats = 16 * p.tiles * (2 + kv.head_dim);
   p.stripes = outputs * 16 * p.tiles * (kv.head_dim / 4) / 256 < 1024 ? 4 : 1;
-  p.most_parts = whole ? 0 : 2 * (int64_t)p.workers * kv.n_kv_heads;
-  p.most_shared = whole ? 0 : outputs;
+  // What a call with fewer keys (a window, a short table) takes is no more than this.
+  p.most_parts = may_cut ? 2 * (int64_t)(places / kv.n_kv_heads) * kv.n_kv_heads : 0;
+  p.most_shared = may_cut ? outputs : 0;
   return p;
 }
 

@@ -40,12 +40,12 @@ __device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint32_t to) { 
 
 // A ring of tiles of 32 keys and their values in LDS.  Row r of a tile holds its 16-byte
 // chunks in the order c ^ swizzle(r) (values: swizzle_v), so that lanes that read the same
-// chunk of several rows use all banks.  The kernel takes steps of two tiles (one of 512-byte
-// rows), as many as the LDS of its workgroup's share of a CU holds, up to four.
+// chunk of several rows use all banks.  The kernel takes steps of one or two tiles, and
+// as many as the LDS of a workgroup's share of a CU holds, up to four, are under way.
 template <int kDh, bool kE4M3>
 struct WideRing {
   static constexpr int kRow = kDh * (kE4M3 ? 1 : 2), kSide = 32 * kRow, kTile = 2 * kSide;
-  static constexpr int kStepTiles = kRow == 512 ? 1 : 2, kStep = kStepTiles * kTile;
+  static constexpr int kStepTiles = wide_step_tiles(kDh, kE4M3), kStep = kStepTiles * kTile;
   static constexpr int kFit = 160 * 1024 / wide_workgroups(kDh, kE4M3) / (kStep + 64);
   static constexpr int kSteps = kFit < 4 ? kFit : 4;
   static constexpr int kCopies = kStep / 4096;  // of a wavefront and step
