@@ -40,39 +40,16 @@ void launch_tree_fp16(const TreeArg& a, const TreePlan& p, int head_dim, bool e4
 
 constexpr int kTreeWaves = 4;
 
-// Workgroups of paged_tree_wide_kernel on a CU.
+// Workgroups of paged_tree_wide_kernel on a CU, as far as registers and LDS allow without
+// scratch memory: 40 trees over 8 bits 173 us with two and 163 with three, 64 dimensions over
+// 16 bits 34.5 with three and 40.9 with four (16 trees of up to 8,192 keys).
 constexpr int wide_workgroups(int head_dim, bool e4m3) {
   return head_dim == 64 || (head_dim == 128 && e4m3) ? 3 : 2;
 }
 
-// Its steps' tiles of 32 keys.
+// Its steps' tiles of 32 keys: 33 trees with scores by distance, 64 dimensions over 16 bits,
+// 34 us with one and 40 with two.
 constexpr int wide_step_tiles(int head_dim, bool e4m3) { return !e4m3 && head_dim != 128 ? 1 : 2; }
-
-// A kernel's arguments lie in memory of the host, a microsecond away, and where scalar
-// registers run out the compiler reads them again in the middle of the kernel (30 trees of
-// 46 keys 24 us instead of 10).  Values that it knows nothing of are kept, in lanes of
-// vector registers if need be.
-template <class P>
-__device__ __forceinline__ void keep_argument(P*& p) {
-  auto g = (__attribute__((address_space(1))) P*)p;
-  asm volatile("" : "+s"(g));
-  p = (P*)g;
-}
-template <class V>
-__device__ __forceinline__ void keep_argument(V& v) {
-  asm volatile("" : "+s"(v));
-}
-template <class... V>
-__device__ __forceinline__ void keep_arguments(V&... v) {
-  (keep_argument(v), ...);
-}
-__device__ __forceinline__ void keep_arguments(TreeArg& a) {
-  keep_arguments(a.kv.k, a.kv.v, a.kv.k_scale, a.kv.v_scale, a.kv.page_bytes, a.kv.slot_bytes, a.kv.head_bytes,
-                 a.kv.n_pages, a.kv.page_log2, a.kv.n_kv_heads, a.q, a.out, a.lse, a.lengths, a.starts, a.seqs,
-                 a.table, a.tree, a.slopes, a.heads_of, a.parts, a.q_stride, a.out_stride, a.table_stride, a.scale,
-                 a.cap, a.tree0, a.trees, a.rows, a.n_heads, a.group, a.blocks, a.n_seqs, a.table_width, a.max_keys,
-                 a.max_nodes, a.window, a.workers, a.slack, a.unit_keys, a.unit_log2, a.part_floats);
-}
 
 // A tree: its rows, and the keys [first, end) that some node of it may see, of
 // which those from n on are its nodes.
@@ -591,10 +568,14 @@ __device__ __forceinline__ void note_parts(const TreeArg& a, const TreeRun& r, i
 // infinity or a NaN among the values, which the columns share: keys with such
 // values are cleared from the product and added by themselves, to the columns that
 // see them.
+//
+// Bound by HBM where there are keys enough: 64 trees of one node and 1,001 keys of 8 heads of
+// 128 take 49 us, 5.4 TB/s.  Short calls are bound by the chain of trips to memory (lengths,
+// page table, keys, values) and two launches.  With four tiles of columns, 64 to a wavefront,
+// registers ran out: 40 trees over 8 bits 389 us, which the wide kernel takes in 160.
 template <class T, bool kE4M3, int kDh, int kTiles, bool kShaped>
 __global__ __launch_bounds__(64 * kTreeWaves, kDh == 256 ? 1 : 2)
 void paged_tree_kernel(TreeArg a) {
-  keep_arguments(a);
   constexpr int kWaves = kTreeWaves, kThreads = 64 * kWaves, kColumns = 16 * kTiles;
   typedef WideTile<T, kE4M3, kDh, kTiles> Tl;
   constexpr int kRow = kDh + 4;  // padded: lanes 16 apart in dimensions, 1 in columns
@@ -876,12 +857,12 @@ void paged_tree_kernel(TreeArg a) {
   }
 }
 
-// Joins the parts of an output that workers shared, kStripes threads to four
-// dimensions of a column, each over every kStripes-th part.  Reads 4 bytes a column,
-// dimension and part, and writes the output.
+// Joins the parts of an output that workers shared, kStripes threads to four dimensions of a
+// column, each over every kStripes-th part: weights of a part are 2^(its maximum - the
+// largest).  Reads 4 bytes a column, dimension and part, and writes the output; its time is
+// its launch and the chain descriptors, maxima, parts, about 4 us of the smallest calls.
 template <class T, bool kE4M3, int kDh, int kStripes>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArg a, int tiles) {
-  keep_arguments(a);
   __shared__ float4 so[256];
   __shared__ float sm[256], sl[256];
   constexpr int kItems = 256 / kStripes, kFours = kDh / 4;

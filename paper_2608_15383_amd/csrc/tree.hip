@@ -1,5 +1,5 @@
 // Attention of trees of drafted tokens over a paged cache (exactmoe_drafts.h): the
-// call's checks and how it is launched.  The kernels are in tree.h.
+// call's checks and how its work is cut.  The kernels are in tree.h and tree_wide.h.
 #include "tree.h"
 
 using namespace emoe;
@@ -7,18 +7,19 @@ using namespace emoe;
 namespace {
 
 constexpr int64_t kMostColumns = 1 << 20;  // query heads of a key head, of all nodes: blocks are a grid's second axis
-constexpr int kUnits = 256;  // CUs
+constexpr int kUnits = 256;                // CUs
 
 // Which kernel, and how its work is cut.
 //  - Up to 16 columns (32 of 64 dimensions) paged_tree_kernel, whose wavefronts take keys
 //    of their own straight from memory to registers; more paged_tree_wide_kernel, whose
-//    wavefronts share them: 26 columns, 2,026 keys of 16 heads of 128 17.7 and 16.3 us,
-//    52 columns 95 and 51 (19 trees of up to 8,192 keys).
+//    wavefronts share them.  4 columns, 64 trees of 1,001 keys of 8 heads of 128 49.3 and
+//    53.3 us; 26 columns of 16 heads 17.6 and 13.1 us over 328 keys, 23.9 and 16.6 over 2,026.
 //  - An output, that is a block of columns of a tree and key head, has one workgroup where
 //    there are 1,024 outputs or more, or few keys; else its keys are cut over the workers
-//    of its key head (find_run) and tree_join_kernel joins the parts, in a launch that
-//    costs 4 us: 328 keys, 16 heads, whole and cut 16.7 and 12.9 us (wide), 504 keys, 16
-//    columns 11.8 and 12.7 (not wide).
+//    of its key head (find_run) and tree_join_kernel joins the parts in a launch of its own.
+//    Whole and cut: 328 keys of 16 heads 18.3 and 12.8 us (wide), 504 keys, 16 columns 11.5
+//    and 12.2 (not wide); 1,200 outputs of up to 600 keys 52 and 71, 512 outputs of 1,001
+//    keys 46 and 49, 640 of up to 16,384 563 and 160.
 TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int64_t max_keys,
                    int32_t max_nodes, int32_t window) {
   TreePlan p;
@@ -49,6 +50,8 @@ TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int6
   // us from 4 to 40.
   p.slack = p.wide ? 12 : 6;
   p.part_floats = 16 * p.tiles * (2 + kv.head_dim);
+  // Threads to an item of the join: 1 and 4 of them 159 and 177 us with 640 outputs (40 trees
+  // over 8 bits), 100.6 and 97.3 with 8.
   p.stripes = outputs * 16 * p.tiles * (kv.head_dim / 4) / 256 < 1024 ? 4 : 1;
   // What a call with fewer keys (a window, a short table) takes is no more than this.
   p.most_parts = may_cut ? 2 * (int64_t)(places / kv.n_kv_heads) * kv.n_kv_heads : 0;
