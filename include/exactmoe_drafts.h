@@ -132,7 +132,8 @@ int32_t emoe_accept_drafts(const emoe_accept_args* args, hipStream_t stream);
 
 /* ---------------------------------------------------------------- moves in the caches */
 /* Both calls act on n_layers caches (a host array) of the same type, sizes and
- * strides, whose page tables are one and the same. */
+ * strides, whose page tables are one and the same; what is stored in them, keys and
+ * values of all layers, lies in places of its own. */
 
 /* For tree g of sequence s = seqs[g] and every i < accepted[g] with path[g][i] > i:
  * position lengths[g] + i of s takes the key and the value that position

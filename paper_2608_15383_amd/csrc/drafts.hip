@@ -219,6 +219,12 @@ int32_t check_layers(const emoe_paged_kv* kv, int32_t n_layers) {
         a.slot_stride != b.slot_stride || a.head_stride != b.head_stride)
       return report_error(EMOE_ESHAPE, "cache %d has another type, size or stride than the first one", i);
   }
+  // The same place twice would be moved twice, at once.
+  auto place = [&](int64_t i) { return i & 1 ? kv[i >> 1].v_pages : kv[i >> 1].k_pages; };
+  for (int64_t i = 1; i < 2 * (int64_t)n_layers; ++i)
+    for (int64_t j = 0; j < i; ++j)
+      if (place(i) == place(j))
+        return report_error(EMOE_EINVAL, "caches %d and %d have pages at the same place", (int)(j >> 1), (int)(i >> 1));
   return EMOE_OK;
 }
 

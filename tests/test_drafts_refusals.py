@@ -10,7 +10,8 @@ import torch
 
 from paper_2608_15383_amd import _lib, api
 from paper_2608_15383_amd._lib import EMOE_EINVAL, EMOE_ESHAPE, EMOE_F16, EMOE_F32, EMOE_OK
-from tests.test_serving_refusals import P, append, kv, status
+from tests.test_serving_refusals import P, append, status
+from tests.test_serving_refusals import kv as cache
 
 HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include",
                       "exactmoe_drafts.h")
@@ -31,6 +32,11 @@ def test_structures(name, view):
             pointer, n = "*" in n, n.replace("*", "").strip()
             want.append((n, C.c_void_p if pointer else SCALARS[kind]))
     assert [tuple(f) for f in view._fields_] == want
+
+
+def kv(layer=0, **kw):
+    at = P + (2 * layer << 20)
+    return cache(**{**dict(k_pages=at, v_pages=at + (1 << 20)), **kw})
 
 
 def axes(**kw):
@@ -92,6 +98,7 @@ def test_axes_checks(change, want):
     (dict(n_heads=0), EMOE_ESHAPE),
     (dict(n_heads=6), EMOE_ESHAPE),
     (dict(n_heads=1 << 21, q_stride=1 << 28, out_stride=1 << 28), EMOE_ESHAPE),
+    (dict(n_heads=1 << 20, max_nodes=64, q_stride=1 << 28, out_stride=1 << 28), EMOE_ESHAPE),
     (dict(max_keys=(1 << 30) + 1), EMOE_ESHAPE),
     (dict(scale=float("nan")), EMOE_EINVAL),
     (dict(scale=float("inf")), EMOE_EINVAL),
@@ -127,7 +134,7 @@ def test_tree_needs_its_workspace():
     assert status("emoe_paged_tree_attention", None, args[1], P, need, None) == EMOE_EINVAL
     assert status("emoe_paged_tree_attention", args[0], None, P, need, None) == EMOE_EINVAL
     for bad in ((-1, 16, 9, 5), (1, 0, 9, 5), (1, 6, 9, 5), (1, 16, -1, 5), (1, 16, 2 ** 31 - 1, 5),
-                (1, 1 << 21, 9, 5), (1, 16, 9, 0), (1, 16, 9, 65)):
+                (1, 1 << 21, 9, 5), (1, 1 << 20, 9, 64), (1, 16, 9, 0), (1, 16, 9, 65)):
         assert size(C.byref(kv()), *bad) == 0
     # No window needs more than none does.
     assert size(C.byref(kv()), 1, 16, 1 << 30, 64) < 1 << 30
@@ -198,10 +205,14 @@ def check_layers(name, args):
     assert status(name, C.byref(kv()), 0, C.byref(args), None) == EMOE_EINVAL
     for other in (dict(n_pages=9), dict(dtype=EMOE_F16), dict(page_size=8),
                   dict(slot_stride=1024, page_stride=16 * 1024), dict(head_dim=64)):
-        both = (_lib.PagedKVView * 2)(kv(), kv(**other))
+        both = (_lib.PagedKVView * 2)(kv(), kv(1, **other))
         assert status(name, both, 2, C.byref(args), None) == EMOE_ESHAPE
-    both = (_lib.PagedKVView * 2)(kv(), kv(k_pages=None))
+    both = (_lib.PagedKVView * 2)(kv(), kv(1, k_pages=None))
     assert status(name, both, 2, C.byref(args), None) == EMOE_EINVAL
+    # Keys or values of two layers, or the keys and values of one, in the same place.
+    for same in ([kv(), kv()], [kv(), kv(1, v_pages=P)], [kv(v_pages=P), kv(1)], [kv(), kv(1), kv(2), kv(1)]):
+        assert status(name, (_lib.PagedKVView * len(same))(*same), len(same), C.byref(args),
+                      None) == EMOE_EINVAL
 
 
 def test_binding_refuses_host_tensors():

@@ -432,6 +432,105 @@ def test_tree_many_small_trees():
              64, 8, seed=6, max_nodes=64)
 
 
+@pytest.mark.parametrize("lengths,hk", [([3, 2, 1, 0] * 80 + [2500, 900], 2), ([40] * 599 + [700], 1),
+                                        ([2000] * 90, 2)])
+def test_tree_many_trees_cut(lengths, hk):
+    """Long keys cut over workers, and more trees than a wavefront's lanes, or than there are workers."""
+    rng = np.random.default_rng(len(lengths))
+    run_tree("bf16", "bf16", lengths, rng.integers(0, 3, len(lengths)).tolist(), 2 * hk, hk, 64, 16, seed=8,
+             max_nodes=2)
+
+
+def test_tree_more_trees_than_a_launch():
+    """Seven trees over and over: each as often as it comes gives the same bits."""
+    n, times = 7, 10001
+    c = Cache("bf16", 40, 8, 1, 64, 1)
+    c.fill([(p, s) for p in range(40) for s in range(8)])
+    table = ids(np.arange(35).reshape(7, 5))
+    lengths, seqs = [0, 7, 31, 38, 8, 20, 33], list(range(n))
+    q = torch.randn(n, 2, 64, device="cuda:0").to(torch.bfloat16)
+    outs = []
+    for k in (1, times):
+        ws = torch.empty(api.paged_tree_attention_workspace_bytes(c.kv, n * k, 2, 40, 1), dtype=torch.uint8,
+                         device="cuda:0")
+        out = torch.empty(n * k, 2, 64, device="cuda:0", dtype=torch.bfloat16)
+        api.paged_tree_attention(c.kv, q.repeat(k, 1, 1), table, ids(lengths * k), out, ws, 40, 1,
+                                 seqs=ids(seqs * k))
+        outs.append(out.view(torch.int16).unflatten(0, (k, n)))
+    torch.cuda.synchronize()
+    assert outs[0].any() and bool((outs[1] == outs[0]).all())
+
+
+@pytest.mark.parametrize("kind,cache_kind,d,heads", [("fp16", "fp16", 64, 1), ("fp16", "fp16", 128, 8),
+                                                     ("fp16", "e4m3", 256, 1), ("bf16", "bf16", 128, 8)])
+def test_tree_of_small_weights(kind, cache_kind, d, heads):
+    """Values of 0 where the weights are large, large ones where they are small: a bias of half of
+    the distance leaves weights from 1 to e^-41."""
+    def poison(c, stored):                       # one page: a slot is its position
+        for p, s in stored:
+            x = 384.0 if s < 62 else 0.0
+            c.v[p, s] = torch.tensor(x).to(c.v.dtype)
+            stored[p, s][1][:] = x if c.vs is None else x * f64(c.vs)[:, None]
+
+    run_tree(kind, cache_kind, [80], [3], heads, 1, d, 128, seed=11, slopes=True, poison=poison, scale=0.05)
+
+
+def test_tree_workspace_and_graphs():
+    """One workspace for calls of different sizes, eager and in two captured graphs, replayed in turn
+    with other work between; a stream of its own; two streams with a workspace each."""
+    c = Cache("bf16", 600, 16, 2, 64, 4)
+    c.fill([(p, s) for p in range(600) for s in range(16)])
+    rng = np.random.default_rng(3)
+    calls = []
+    for trees, nodes, longest in ((3, 9, 1500), (40, 2, 900), (1, 40, 2900)):
+        table = ids(rng.integers(0, 600, (trees, -(-longest // 16) + 4)))
+        q = torch.randn(trees * nodes, 4, 64, device="cuda:0").to(torch.bfloat16)
+        calls.append((q, table, ids(rng.integers(0, longest, trees)), longest + nodes, nodes))
+    need = max(api.paged_tree_attention_workspace_bytes(c.kv, t[1].shape[0], 4, t[3], t[4]) for t in calls)
+    spaces = [torch.full((need,), 255, dtype=torch.uint8, device="cuda:0") for _ in range(2)]
+
+    def run(i, out, ws=0):
+        q, table, lengths, keys, nodes = calls[i]
+        api.paged_tree_attention(c.kv, q, table, lengths, out, spaces[ws], keys, nodes)
+
+    want, outs, graphs = [torch.empty_like(t[0]) for t in calls], [torch.empty_like(t[0]) for t in calls], []
+    for i in range(3):
+        run(i, want[i])
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run(i, outs[i])
+        graphs.append(g)
+    for turn in range(4):
+        for i in (0, 1):
+            outs[i].fill_(7)
+            graphs[i].replay()
+            if turn % 2:
+                run(2, outs[2])
+            torch.cuda.synchronize()
+            assert torch.equal(outs[i], want[i])
+    # Other lengths in place: the graph takes them.
+    calls[0][2].copy_(ids([1, 700, 3]))
+    graphs[0].replay()
+    run(0, want[0])
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want[0])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for i, s in enumerate(streams):
+        outs[i].fill_(7)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                run(i, outs[i], i)
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        assert torch.equal(outs[i], want[i])
+
+
 def test_tree_nothing():
     c = Cache("bf16", 1, 8, 1, 64, 2)
     e = torch.empty(0, 1, 64, device="cuda:0", dtype=torch.bfloat16)
@@ -797,7 +896,7 @@ def test_binding_checks_tensors():
             api.accept_drafts(**{**dict(tokens=ids([0] * 6), chosen=ids([0] * 6), lengths=n, path=path,
                                         accepted=acc), **bad})
     other = Cache("bf16", 4, 16, 2, 64, 0)
-    for kvs in ([], [c.kv, other.kv], [c.kv, None], [c.kv, 3]):
+    for kvs in ([], [c.kv, other.kv], [c.kv, c.kv], [c.kv, None], [c.kv, 3]):
         with pytest.raises(ExactMoEError):
             api.paged_compact(kvs, table, n, path, acc)
         with pytest.raises(ExactMoEError):
