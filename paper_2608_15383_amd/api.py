@@ -441,20 +441,24 @@ def accept_drafts(tokens, chosen, lengths, path, accepted, new_tokens=None, new_
     chosen after its parent.  tokens, chosen i32 [rows]; tree, starts as in paged_tree_attention;
     path, new_tokens i32 [trees][most nodes], accepted i32 [trees]; new_lengths = lengths +
     accepted, i32 [trees]."""
-    if not tokens.is_cuda:
-        _refuse(f"tokens is on {tokens.device}")
+    if not getattr(tokens, "is_cuda", False):
+        _refuse("tokens: need a tensor on a GPU")
     binding().accept_drafts(tokens, chosen, lengths, path, accepted, new_tokens, new_lengths, tree,
                             starts, _stream_on(tokens.device.index, stream))
+
+
+def _device_of(kvs) -> int:
+    if not isinstance(kvs, (list, tuple)) or not kvs or not isinstance(kvs[0], PagedKV):
+        _refuse("kvs: need a list of PagedKV")
+    return kvs[0].index
 
 
 def paged_compact(kvs, page_table, lengths, path, accepted, seqs=None, stream=None) -> None:
     """emoe_paged_compact: in every cache of the list kvs, position lengths[g] + i of a sequence
     takes what lengths[g] + path[g][i] held, for i < accepted[g].  path i32 [trees][most nodes];
     lengths (those before the acceptance), accepted, seqs i32 [trees]."""
-    if not kvs:
-        _refuse("kvs is empty")
-    binding().paged_compact(kvs, kvs[0].index, page_table, lengths, path, accepted, seqs,
-                            _stream_on(kvs[0].index, stream))
+    device = _device_of(kvs)
+    binding().paged_compact(kvs, device, page_table, lengths, path, accepted, seqs, _stream_on(device, stream))
 
 
 def paged_fork(kvs, page_table, parents, lengths, fresh, new_table, stream=None) -> None:
@@ -462,10 +466,8 @@ def paged_fork(kvs, page_table, parents, lengths, fresh, new_table, stream=None)
     parents[f]; a page in use only in part is copied to page fresh[f] of every cache of the list kvs
     (fresh None or outside the pool: shared).  parents, lengths, fresh i32 [forks]; new_table i32
     [forks][the width of page_table]."""
-    if not kvs:
-        _refuse("kvs is empty")
-    binding().paged_fork(kvs, kvs[0].index, page_table, parents, lengths, fresh, new_table,
-                         _stream_on(kvs[0].index, stream))
+    device = _device_of(kvs)
+    binding().paged_fork(kvs, device, page_table, parents, lengths, fresh, new_table, _stream_on(device, stream))
 
 
 def profile_begin(max_kernels: int) -> None:

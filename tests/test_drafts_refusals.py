@@ -217,8 +217,11 @@ def check_layers(name, args):
 
 def test_binding_refuses_host_tensors():
     n = torch.zeros(1, dtype=torch.int32)
-    for make in (lambda: api.accept_drafts(n, n, n, n[None], n), lambda: api.paged_compact([], n, n, n, n),
-                 lambda: api.paged_fork([], n, n, n, n, n)):
+    for make in (lambda: api.accept_drafts(n, n, n, n[None], n),
+                 lambda: api.accept_drafts([0], n, n, n[None], n), lambda: api.paged_compact([], n, n, n, n),
+                 lambda: api.paged_fork([], n, n, n, n, n), lambda: api.paged_compact([None], n, n, n, n),
+                 lambda: api.paged_compact(None, n, n, n, n), lambda: api.paged_fork(3, n, n, n, n, n),
+                 lambda: api.paged_fork(n, n, n, n, n, n)):
         with pytest.raises(_lib.ExactMoEError) as e:
             make()
         assert e.value.status == EMOE_EINVAL
