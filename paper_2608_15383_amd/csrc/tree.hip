@@ -17,8 +17,8 @@ constexpr int kUnits = 256;                // CUs
 //  - An output, that is a block of columns of a tree and key head, has one workgroup where
 //    there are 1,024 outputs or more, or few keys; else its keys are cut over the workers
 //    of its key head (find_run) and tree_join_kernel joins the parts in a launch of its own.
-//    Whole and cut: 328 keys of 16 heads 18.3 and 12.8 us (wide), 504 keys, 16 columns 11.5
-//    and 12.2 (not wide); 1,200 outputs of up to 600 keys 52 and 71, 512 outputs of 1,001
+//    Whole and cut: 328 keys of 16 heads 18.3 and 12.8 us, 226 keys 13.4 and 12.6, but 20 trees
+//    of 216 keys 11.0 and 17.0 (wide); 504 keys, 16 columns 11.5 and 12.2 (not wide); 1,200 outputs of up to 600 keys 52 and 71, 512 outputs of 1,001
 //    keys 46 and 49, 640 of up to 16,384 563 and 160.
 TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int64_t max_keys,
                    int32_t max_nodes, int32_t window) {
