@@ -570,7 +570,7 @@ __device__ __forceinline__ void note_parts(const TreeArg& a, const TreeRun& r, i
 // see them.
 //
 // Bound by HBM where there are keys enough: 64 trees of one node and 1,001 keys of 8 heads of
-// 128 take 49 us, 5.4 TB/s.  Short calls are bound by the chain of trips to memory (lengths,
+// 128 take 46 us, 5.7 TB/s.  Short calls are bound by the chain of trips to memory (lengths,
 // page table, keys, values) and two launches.  With four tiles of columns, 64 to a wavefront,
 // registers ran out: 40 trees over 8 bits 389 us, which the wide kernel takes in 160.
 template <class T, bool kE4M3, int kDh, int kTiles, bool kShaped>

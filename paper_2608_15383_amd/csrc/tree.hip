@@ -13,15 +13,18 @@ constexpr int kUnits = 256;                // CUs
 //  - Up to 16 columns (32 of 64 dimensions) paged_tree_kernel, whose wavefronts take keys
 //    of their own straight from memory to registers; more paged_tree_wide_kernel, whose
 //    wavefronts share them.  4 columns, 64 trees of 1,001 keys of 8 heads of 128 49.3 and
-//    53.3 us; 26 columns of 16 heads 17.6 and 13.1 us over 328 keys, 23.9 and 16.6 over 2,026.
+//    53.3 us (both cut); 26 columns of 16 heads 17.6 and 13.1 us over 328 keys, 23.9 and 16.6 over 2,026.
 //  - An output, that is a block of columns of a tree and key head, has one workgroup where
 //    there are 1,024 outputs or more, or few keys; else its keys are cut over the workers
 //    of its key head (find_run) and tree_join_kernel joins the parts in a launch of its own.
 //    Whole and cut: 328 keys of 16 heads 18.3 and 12.8 us, 226 keys 13.4 and 12.6, but 20 trees
-//    of 216 keys 11.0 and 17.0 (wide); 504 keys, 16 columns 11.5 and 12.2 (not wide); 1,200 outputs of up to 600 keys 52 and 71, 512 outputs of 1,001
-//    keys 46 and 49, 640 of up to 16,384 563 and 160.
+//    of 216 keys 11.0 and 17.0 (wide); 504 keys, 16 columns 11.5 and 12.2 (not wide); 1,200
+//    outputs of up to 600 keys 52 and 71, 640 of up to 16,384 563 and 160.  Few are twice as
+//    many keys where every CU has an output, 320 of 316 keys 22.4 and 26.2 us, 960 of up to
+//    506 44 and 63 (wide), 480 of up to 1,004 28 and 33 (not wide); but not of shaped scores,
+//    whose steps are longer: 280 of up to 496 39 and 31, of 492 41 and 38.
 TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int64_t max_keys,
-                   int32_t max_nodes, int32_t window) {
+                   int32_t max_nodes, int32_t window, bool shaped) {
   TreePlan p;
   const int64_t columns = (int64_t)(n_heads / kv.n_kv_heads) * max_nodes;
   const bool e4m3 = kv.dtype == EMOE_E4M3;
@@ -37,7 +40,8 @@ TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int6
   const int64_t outputs = (int64_t)trees * p.lines;
   const int places = kUnits * (p.wide ? wide_workgroups(kv.head_dim, e4m3) : kv.head_dim == 256 ? 1 : 2);
   constexpr int kManyOutputs = 1024;
-  const bool may_cut = keys > (p.wide ? 256 : 512) && outputs < kManyOutputs && kv.n_kv_heads <= places;
+  const int few_keys = (p.wide ? 256 : 512) * (outputs >= kUnits && !shaped ? 2 : 1);
+  const bool may_cut = keys > few_keys && outputs < kManyOutputs && kv.n_kv_heads <= places;
   // A launch's units stay below 2^31, its threads below 2^32, its trees within the grid's
   // third axis.
   p.trees_per_launch = (((int64_t)1 << 31) - 1 - 4 * kUnits) / most_units;
@@ -53,7 +57,8 @@ TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int6
   // Threads to an item of the join: 1 and 4 of them 159 and 177 us with 640 outputs (40 trees
   // over 8 bits), 100.6 and 97.3 with 8.
   p.stripes = outputs * 16 * p.tiles * (kv.head_dim / 4) / 256 < 1024 ? 4 : 1;
-  // What a call with fewer keys (a window, a short table) takes is no more than this.
+  // What a call with fewer keys (a window, a short table), or without shaped scores, takes is
+  // no more than this.
   p.most_parts = may_cut ? 2 * (int64_t)(places / kv.n_kv_heads) * kv.n_kv_heads : 0;
   p.most_shared = may_cut ? outputs : 0;
   return p;
@@ -72,7 +77,7 @@ size_t emoe_paged_tree_attention_workspace_bytes(const emoe_paged_kv* kv, int32_
       max_keys > kMostKeys || n_heads > kMostHeads || max_nodes < 1 || max_nodes > EMOE_MAX_NODES ||
       (int64_t)(n_heads / kv->n_kv_heads) * max_nodes > kMostColumns)
     return 0;
-  const TreePlan p = tree_plan(*kv, trees, n_heads, max_keys, max_nodes, 0);
+  const TreePlan p = tree_plan(*kv, trees, n_heads, max_keys, max_nodes, 0, true);
   return 16 + shared_bytes(p) + (size_t)p.most_parts * p.part_floats * 4;
 }
 
@@ -117,7 +122,7 @@ int32_t emoe_paged_tree_attention(const emoe_paged_kv* kv, const emoe_paged_tree
   if (!aligned16(workspace)) return report_error(EMOE_EINVAL, "workspace: need 16-byte alignment");
   const int64_t held = (int64_t)A.table_width * kv->page_size;  // no more keys than the table holds
   const TreePlan plan = tree_plan(*kv, A.trees, A.n_heads, held < A.max_keys ? held : A.max_keys,
-                                  A.max_nodes, A.window);
+                                  A.max_nodes, A.window, A.cap > 0.f || A.slopes);
   TreeArg a;
   a.kv = view_of(*kv);
   a.q = static_cast<const uint16_t*>(A.q);

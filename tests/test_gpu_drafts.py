@@ -433,12 +433,22 @@ def test_tree_many_small_trees():
 
 
 @pytest.mark.parametrize("lengths,hk", [([3, 2, 1, 0] * 80 + [2500, 900], 2), ([40] * 599 + [700], 1),
-                                        ([2000] * 90, 2)])
+                                        ([2000] * 90, 2), ([500] * 150 + [1, 0], 2), ([1001] * 64, 4)])
 def test_tree_many_trees_cut(lengths, hk):
     """Long keys cut over workers, and more trees than a wavefront's lanes, or than there are workers."""
     rng = np.random.default_rng(len(lengths))
     run_tree("bf16", "bf16", lengths, rng.integers(0, 3, len(lengths)).tolist(), 2 * hk, hk, 64, 16, seed=8,
              max_nodes=2)
+
+
+@pytest.mark.parametrize("slopes", [False, True])
+@pytest.mark.parametrize("kind,cache_kind,d", [("bf16", "bf16", 128), ("fp16", "e4m3", 64)])
+def test_tree_outputs_for_every_cu(kind, cache_kind, d, slopes):
+    """Some 300 outputs of up to 500 keys: whole, with a bias by distance cut."""
+    rng = np.random.default_rng(2)
+    lengths, nodes = rng.integers(0, 480, 38), rng.integers(1, 18, 38)
+    lengths[3], nodes[3] = 480, 17
+    run_tree(kind, cache_kind, lengths.tolist(), nodes.tolist(), 16, 8, d, 16, seed=9, slopes=slopes)
 
 
 def test_tree_more_trees_than_a_launch():
