@@ -24,19 +24,24 @@ __device__ __forceinline__ void lds_barrier() {
 // Copies 16 bytes per lane, from `from` + offset, to LDS, at `to` + 16 * lane, past the
 // caches (131,072 keys: 122 -> 104 us).  As assembly, since the compiler would have every
 // read of LDS wait for all copies under way; it has no registers as outputs, and the
-// kernel itself waits for it.
+// kernel itself waits for it.  M0, which it changes, is named, so that the compiler does not
+// take a value that it put there before for still there after; that it is none of those
+// that the compiler would save is what the warning says.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint32_t offset, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(
                    __builtin_amdgcn_readfirstlane(to)),
                "v"(offset), "s"(from)
-               : "memory");
+               : "memory", "m0");
 }
 __device__ __forceinline__ void copy_to_lds(const uint8_t* from, uint32_t to) {  // from: of each lane
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(
                    __builtin_amdgcn_readfirstlane(to)),
                "v"(from)
-               : "memory");
+               : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // A ring of tiles of 32 keys and their values in LDS.  Row r of a tile holds its 16-byte
 // chunks in the order c ^ swizzle(r) (values: swizzle_v), so that lanes that read the same
