@@ -402,17 +402,24 @@ def decoder_paged_workspace_bytes(dd: DecoderDims, n_tokens: int, n_out: int, ma
 
 # ---------------------------------------------------------------- drafted tokens
 # The calls of exactmoe_drafts.h.
+def _check_cache(kv) -> None:
+    if not isinstance(kv, PagedKV):
+        _refuse("kv: need a PagedKV")
+
+
 def paged_append_axes(kv: PagedKV, q, k, v, positions, angles, axes, page_table, inv_freq, seqs=None,
                       q_out=None, interleaved: bool = False, stream=None) -> None:
     """emoe_paged_append_axes: paged_append with angles[t][axes[i]] * inv_freq[i] in place of
     positions[t] * inv_freq[i].  angles i32 [n][axes]; axes i32 [rotary_dim / 2], the axis of each
     pair, or None: the first one.  A drafted node of depth d behind n keys: angles [[n + d]]."""
+    _check_cache(kv)
     binding().paged_append_axes(kv.address, kv.index, q, k, v, positions, page_table, inv_freq, seqs,
                                 q_out, interleaved, angles, axes, _stream_on(kv.index, stream))
 
 
 def paged_tree_attention_workspace_bytes(kv: PagedKV, trees: int, n_heads: int, max_keys: int,
                                          max_nodes: int) -> int:
+    _check_cache(kv)
     return int(lib().emoe_paged_tree_attention_workspace_bytes(C.byref(kv.view), trees, n_heads,
                                                                max_keys, max_nodes))
 
@@ -428,6 +435,7 @@ def paged_tree_attention(kv: PagedKV, q, page_table, lengths, out, workspace, ma
     [sequences][pages]; slopes f32 [heads]; lse f32 [rows][heads]; scale 1 / sqrt(dim) when None.
     max_keys bounds lengths and nodes together.  workspace: paged_tree_attention_workspace_bytes,
     of any content."""
+    _check_cache(kv)
     if scale is None:
         scale = kv.view.head_dim ** -0.5
     binding().paged_tree_attention(kv.address, kv.index, q, page_table, lengths, out, workspace,
@@ -458,7 +466,8 @@ def paged_compact(kvs, page_table, lengths, path, accepted, seqs=None, stream=No
     takes what lengths[g] + path[g][i] held, for i < accepted[g].  path i32 [trees][most nodes];
     lengths (those before the acceptance), accepted, seqs i32 [trees]."""
     device = _device_of(kvs)
-    binding().paged_compact(kvs, device, page_table, lengths, path, accepted, seqs, _stream_on(device, stream))
+    binding().paged_compact(kvs, PagedKV, device, page_table, lengths, path, accepted, seqs,
+                            _stream_on(device, stream))
 
 
 def paged_fork(kvs, page_table, parents, lengths, fresh, new_table, stream=None) -> None:
@@ -467,7 +476,8 @@ def paged_fork(kvs, page_table, parents, lengths, fresh, new_table, stream=None)
     (fresh None or outside the pool: shared).  parents, lengths, fresh i32 [forks]; new_table i32
     [forks][the width of page_table]."""
     device = _device_of(kvs)
-    binding().paged_fork(kvs, device, page_table, parents, lengths, fresh, new_table, _stream_on(device, stream))
+    binding().paged_fork(kvs, PagedKV, device, page_table, parents, lengths, fresh, new_table,
+                         _stream_on(device, stream))
 
 
 def profile_begin(max_kernels: int) -> None:

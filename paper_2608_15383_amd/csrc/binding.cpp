@@ -493,8 +493,9 @@ PyObject* accept_drafts(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   });
 }
 
-// The caches of a sequence of PagedKV, all on `device`.
-std::vector<emoe_paged_kv> layers(PyObject* o, int device) {
+// The caches of a sequence of PagedKV (which class that is, Python says), all on `device`.  An address
+// is taken from nothing else.
+std::vector<emoe_paged_kv> layers(PyObject* o, PyObject* paged_kv, int device) {
   if (!PyList_Check(o) && !PyTuple_Check(o)) refuse("kvs: need a list of PagedKV");
   const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
   static PyObject* const names[2] = {PyUnicode_InternFromString("address"), PyUnicode_InternFromString("index")};
@@ -502,6 +503,10 @@ std::vector<emoe_paged_kv> layers(PyObject* o, int device) {
   out.reserve((size_t)n);
   for (Py_ssize_t i = 0; i < n; ++i) {
     PyObject* item = PySequence_Fast_GET_ITEM(o, i);
+    if (PyObject_IsInstance(item, paged_kv) != 1) {
+      PyErr_Clear();
+      refuse("kvs: need a list of PagedKV");
+    }
     PyObject* address = PyObject_GetAttr(item, names[0]);
     PyObject* index = address ? PyObject_GetAttr(item, names[1]) : nullptr;
     int64_t at = 0, dev = -1;
@@ -520,20 +525,20 @@ std::vector<emoe_paged_kv> layers(PyObject* o, int device) {
   return out;
 }
 
-// (kvs, device, page_table, lengths, path, accepted, seqs, stream)
+// (kvs, PagedKV, device, page_table, lengths, path, accepted, seqs, stream)
 PyObject* paged_compact(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return guarded([&]() -> int32_t {
-    if (n_args != 8) refuse("paged_compact: 8 arguments");
-    const int device = (int)number(a[1], "device");
-    const std::vector<emoe_paged_kv> kvs = layers(a[0], device);
-    const at::Tensor& table = need(array(a[2], "page_table", kI32, {kAny, kAny}, device), "page_table");
-    const at::Tensor& path = need(array(a[4], "path", kI32, {kAny, kAny}, device), "path");
+    if (n_args != 9) refuse("paged_compact: 9 arguments");
+    const int device = (int)number(a[2], "device");
+    const std::vector<emoe_paged_kv> kvs = layers(a[0], a[1], device);
+    const at::Tensor& table = need(array(a[3], "page_table", kI32, {kAny, kAny}, device), "page_table");
+    const at::Tensor& path = need(array(a[5], "path", kI32, {kAny, kAny}, device), "path");
     const int64_t trees = path.size(0);
     emoe_compact_args A{};
-    A.lengths = pointer<const int32_t>(&need(array(a[3], "lengths", kI32, {trees}, device), "lengths"));
+    A.lengths = pointer<const int32_t>(&need(array(a[4], "lengths", kI32, {trees}, device), "lengths"));
     A.path = pointer<const int32_t>(&path);
-    A.accepted = pointer<const int32_t>(&need(array(a[5], "accepted", kI32, {trees}, device), "accepted"));
-    A.seqs = pointer<const int32_t>(array(a[6], "seqs", kI32, {trees}, device));
+    A.accepted = pointer<const int32_t>(&need(array(a[6], "accepted", kI32, {trees}, device), "accepted"));
+    A.seqs = pointer<const int32_t>(array(a[7], "seqs", kI32, {trees}, device));
     A.page_table = pointer<const int32_t>(&table);
     A.path_stride = path.stride(0);
     A.table_stride = table.stride(0);
@@ -541,32 +546,32 @@ PyObject* paged_compact(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     A.max_nodes = i32(path.size(1), "path");
     A.n_seqs = i32(table.size(0), "sequences");
     A.table_width = i32(table.size(1), "page_table");
-    return on_device(device, g_compact, kvs.data(), (int32_t)kvs.size(), &A, stream_of(a[7]));
+    return on_device(device, g_compact, kvs.data(), (int32_t)kvs.size(), &A, stream_of(a[8]));
   });
 }
 
-// (kvs, device, page_table, parents, lengths, fresh, new_table, stream)
+// (kvs, PagedKV, device, page_table, parents, lengths, fresh, new_table, stream)
 PyObject* paged_fork(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return guarded([&]() -> int32_t {
-    if (n_args != 8) refuse("paged_fork: 8 arguments");
-    const int device = (int)number(a[1], "device");
-    const std::vector<emoe_paged_kv> kvs = layers(a[0], device);
-    const at::Tensor& table = need(array(a[2], "page_table", kI32, {kAny, kAny}, device), "page_table");
-    const at::Tensor& parents = need(array(a[3], "parents", kI32, {kAny}, device), "parents");
+    if (n_args != 9) refuse("paged_fork: 9 arguments");
+    const int device = (int)number(a[2], "device");
+    const std::vector<emoe_paged_kv> kvs = layers(a[0], a[1], device);
+    const at::Tensor& table = need(array(a[3], "page_table", kI32, {kAny, kAny}, device), "page_table");
+    const at::Tensor& parents = need(array(a[4], "parents", kI32, {kAny}, device), "parents");
     const int64_t forks = parents.size(0);
-    const at::Tensor& to = need(array(a[6], "new_table", kI32, {forks, table.size(1)}, device), "new_table");
+    const at::Tensor& to = need(array(a[7], "new_table", kI32, {forks, table.size(1)}, device), "new_table");
     emoe_fork_args A{};
     A.page_table = pointer<const int32_t>(&table);
     A.parents = pointer<const int32_t>(&parents);
-    A.lengths = pointer<const int32_t>(&need(array(a[4], "lengths", kI32, {forks}, device), "lengths"));
-    A.fresh = pointer<const int32_t>(array(a[5], "fresh", kI32, {forks}, device));
+    A.lengths = pointer<const int32_t>(&need(array(a[5], "lengths", kI32, {forks}, device), "lengths"));
+    A.fresh = pointer<const int32_t>(array(a[6], "fresh", kI32, {forks}, device));
     A.new_table = pointer<int32_t>(&to);
     A.table_stride = table.stride(0);
     A.new_table_stride = to.stride(0);
     A.forks = i32(forks, "forks");
     A.n_seqs = i32(table.size(0), "sequences");
     A.table_width = i32(table.size(1), "page_table");
-    return on_device(device, g_fork, kvs.data(), (int32_t)kvs.size(), &A, stream_of(a[7]));
+    return on_device(device, g_fork, kvs.data(), (int32_t)kvs.size(), &A, stream_of(a[8]));
   });
 }
 

@@ -225,3 +225,48 @@ def test_binding_refuses_host_tensors():
         with pytest.raises(_lib.ExactMoEError) as e:
             make()
         assert e.value.status == EMOE_EINVAL
+
+
+class Other:
+    """Something else than a PagedKV, with the same numbers: of a cache that lives as long."""
+
+    def __init__(self, view, index=0):
+        self.view, self.address, self.index = view, C.addressof(view), index
+
+
+class SpecialKV(api.PagedKV):
+    pass
+
+
+def handle(view, kind=api.PagedKV):
+    """A PagedKV without tensors behind it, for calls that are refused."""
+    made = kind.__new__(kind)
+    made.view, made.address, made.index = view, C.addressof(view), 0
+    return made
+
+
+def refused_with(call):
+    with pytest.raises(_lib.ExactMoEError) as e:
+        call()
+    assert e.value.status == EMOE_EINVAL
+    return str(e.value)
+
+
+@pytest.mark.parametrize("other", [Other(kv(1)), None, 3, object(), Other(kv(1), "x"), kv(1)])
+def test_caches_are_paged_kvs(other):
+    """Whatever stands in a cache's place is refused before an address is taken from it."""
+    n, x = torch.zeros(1, dtype=torch.int32), torch.zeros(1, 2, 128, dtype=torch.bfloat16)
+    first, special = handle(kv(0)), handle(kv(2), SpecialKV)
+    compact = lambda kvs: refused_with(lambda: api.paged_compact(kvs, n[None], n, n[None], n, stream=0))
+    fork = lambda kvs: refused_with(lambda: api.paged_fork(kvs, n[None], n, n, None, n[None], stream=0))
+    for call in (compact, fork):
+        for kvs in ([other], [first, other], (first, special, other), [special, other, first]):
+            assert "kvs: need a list of PagedKV" in call(kvs), kvs
+        for kvs in ([first], [first, special], (special, first)):
+            assert "kvs" not in call(kvs), kvs               # refused for its host tensors
+    for call in (lambda c: api.paged_append_axes(c, None, x, x, n, n[None], None, n[None], None, stream=0),
+                 lambda c: api.paged_tree_attention(c, x, n[None], n, x, None, 8, 1, stream=0)):
+        assert "kv: need a PagedKV" in refused_with(lambda: call(other))
+        assert "kv: need" not in refused_with(lambda: call(special))
+    with pytest.raises(_lib.ExactMoEError):
+        api.paged_tree_attention_workspace_bytes(other, 1, 1, 1, 1)
