@@ -15,14 +15,26 @@ constexpr int kUnits = 256;                // CUs
 //    wavefronts share them.  4 columns, 64 trees of 1,001 keys of 8 heads of 128 49.3 and
 //    53.3 us (both cut); 26 columns of 16 heads 17.6 and 13.1 us over 328 keys, 23.9 and 16.6 over 2,026.
 //  - An output, that is a block of columns of a tree and key head, has one workgroup where
-//    there are 1,024 outputs or more, or few keys; else its keys are cut over the workers
-//    of its key head (find_run) and tree_join_kernel joins the parts in a launch of its own.
+//    there are few keys; else its keys are cut over the workers of its key head (find_run)
+//    and tree_join_kernel joins the parts in a launch of its own.
 //    Whole and cut: 328 keys of 16 heads 18.3 and 12.8 us, 226 keys 13.4 and 12.6, but 20 trees
-//    of 216 keys 11.0 and 17.0 (wide); 504 keys, 16 columns 11.5 and 12.2 (not wide); 1,200
-//    outputs of up to 600 keys 52 and 71, 640 of up to 16,384 563 and 160.  Few are twice as
-//    many keys where every CU has an output, 320 of 316 keys 22.4 and 26.2 us, 960 of up to
-//    506 44 and 63 (wide), 480 of up to 1,004 28 and 33 (not wide); but not of shaped scores,
-//    whose steps are longer: 280 of up to 496 39 and 31, of 492 41 and 38.
+//    of 216 keys 11.0 and 17.0 (wide); 504 keys, 16 columns 11.5 and 12.2 (not wide); 640
+//    outputs of up to 16,384 563 and 160.  Few are twice as many keys where every CU has an
+//    output, 320 of 316 keys 22.4 and 26.2 us, 960 of up to 506 44 and 63 (wide), 480 of up to
+//    1,004 28 and 33 (not wide); but not of shaped scores, whose steps are longer: 280 of up to
+//    496 39 and 31, of 492 41 and 38.
+//  - From 1,024 outputs on few are up to 2,048 keys: whole outputs fill the CUs several times,
+//    and what is left is that the longest one may come last.  128 ragged trees, 8 key heads of
+//    128, whole and cut: 16 nodes each (wide) over up to 600 keys 49 and 64 us, 1,000 67 and 78,
+//    2,000 106 and 110, 3,000 144 and 133, 4,096 187 and 166, 16,384 646 and 467; one node (not
+//    wide) 1,000 42 and 46, 2,000 72 and 68, 3,000 101 and 94, 16,384 523 and 387; one of 131,072
+//    keys among short ones 3,590 and 192, of one node 1,448 and 138.  400 trees of 2,000 keys 260
+//    and 290, 4,096 468 and 472, 16,384 1,619 and 1,473.  Trees of equal lengths lose about 1%
+//    (128 of 8,000 keys 702 and 706 us) or win what the last round of whole ones leaves idle (130 of
+//    8,000 883 and 755).  Against the rule are shaped scores of up to 2,000 keys (300 trees of 4
+//    key heads of 64 269 and 163), and thousands of trees of one key head, whose lengths every
+//    worker looks through (3,000 of up to 6,000 keys 487 and 548).  With key heads so many that
+//    fewer than 8 workers belong to each, outputs fill the CUs more evenly than workers.
 TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int64_t max_keys,
                    int32_t max_nodes, int32_t window, bool shaped) {
   TreePlan p;
@@ -39,15 +51,18 @@ TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int6
   const int64_t most_units = (keys / p.unit_keys + 2) * p.blocks;
   const int64_t outputs = (int64_t)trees * p.lines;
   const int places = kUnits * (p.wide ? wide_workgroups(kv.head_dim, e4m3) : kv.head_dim == 256 ? 1 : 2);
-  constexpr int kManyOutputs = 1024;
-  const int few_keys = (p.wide ? 256 : 512) * (outputs >= kUnits && !shaped ? 2 : 1);
-  const bool may_cut = keys > few_keys && outputs < kManyOutputs && kv.n_kv_heads <= places;
+  constexpr int kManyOutputs = 1024, kManyKeys = 2048, kLaunchOutputs = 1 << 14, kLaunchTrees = 1024;
+  const bool many = outputs >= kManyOutputs;
+  const int few_keys = many ? kManyKeys : (p.wide ? 256 : 512) * (outputs >= kUnits && !shaped ? 2 : 1);
+  const bool may_cut = keys > few_keys && kv.n_kv_heads <= (many ? places / 8 : places) && p.lines <= kLaunchOutputs;
   // A launch's units stay below 2^31, its threads below 2^32, its trees within the grid's
-  // third axis.
+  // third axis; those of one that is cut within what a worker looks through and the join's
+  // descriptors.
   p.trees_per_launch = (((int64_t)1 << 31) - 1 - 4 * kUnits) / most_units;
   const bool whole = !may_cut || p.trees_per_launch < 1;
   if (whole) p.trees_per_launch = trees < 65535 ? trees : 65535;
-  const int64_t most_outputs = whole ? (int64_t)1 << 23 : kManyOutputs;
+  else if (p.trees_per_launch > kLaunchTrees) p.trees_per_launch = kLaunchTrees;
+  const int64_t most_outputs = whole ? (int64_t)1 << 23 : kLaunchOutputs;
   if (p.trees_per_launch > most_outputs / p.lines) p.trees_per_launch = most_outputs / p.lines;
   p.workers = whole ? 0 : places / kv.n_kv_heads;
   // How much longer than equal runs the parts may be: 40 trees over 8 bits within 1% of 163
@@ -60,7 +75,7 @@ TreePlan tree_plan(const emoe_paged_kv& kv, int32_t trees, int32_t n_heads, int6
   // What a call with fewer keys (a window, a short table), or without shaped scores, takes is
   // no more than this.
   p.most_parts = may_cut ? 2 * (int64_t)(places / kv.n_kv_heads) * kv.n_kv_heads : 0;
-  p.most_shared = may_cut ? outputs : 0;
+  p.most_shared = !may_cut ? 0 : outputs < kLaunchOutputs ? outputs : kLaunchOutputs;
   return p;
 }
 

@@ -270,3 +270,16 @@ def test_caches_are_paged_kvs(other):
         assert "kv: need" not in refused_with(lambda: call(special))
     with pytest.raises(_lib.ExactMoEError):
         api.paged_tree_attention_workspace_bytes(other, 1, 1, 1, 1)
+
+
+@pytest.mark.parametrize("trees,max_nodes", [(127, 16), (128, 16), (2000, 1), (40000, 64)])
+def test_tree_cuts_long_keys_of_many_outputs(trees, max_nodes):
+    """The workspace has room for parts wherever keys may be long, however many trees there are, and
+    no more of it than the workers can fill."""
+    size = _lib.lib().emoe_paged_tree_attention_workspace_bytes
+    view = kv(n_kv_heads=8, slot_stride=1024, head_stride=128, page_stride=16 * 1024)
+    short, long = size(C.byref(view), trees, 32, 600, max_nodes), size(C.byref(view), trees, 32, 131072, max_nodes)
+    few = size(C.byref(view), 8, 32, 131072, max_nodes)
+    if trees > 127:
+        assert short == 16
+    assert few <= long <= few + 12 * (1 << 14)

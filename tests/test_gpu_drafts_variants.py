@@ -148,3 +148,38 @@ def test_long_keys_on_both_sides_of_many_outputs(trees, most):
     nodes = rng.integers(0, 2, trees)
     nodes[[2, 7, trees - 1]] = most, 0, 1
     run_tree("bf16", "bf16", lengths.tolist(), nodes.tolist(), 16, 8, 64, 16, seed=most, max_nodes=most)
+
+
+@pytest.mark.parametrize("lengths,most,heads,hk,max_keys", [
+    ([30] * 127 + [1900], 9, 16, 8, None),               # whole: no keys beyond 2,048
+    ([30] * 127 + [1900], 1, 16, 8, 2049),               # cut, and as its bound says
+    ([2100] + [5, 40, 0] * 340 + [3001, 70, 2500] * 5, 2, 2, 1, None),   # 1,036 trees: two launches
+    ([40, 2500] * 15 + [7], 1, 70, 70, None)])           # 2,170 outputs of many key heads: whole
+def test_many_outputs_whole_and_cut(lengths, most, heads, hk, max_keys):
+    rng = np.random.default_rng(len(lengths))
+    nodes = rng.integers(0, most + 1, len(lengths))
+    nodes[[0, -1]] = most
+    run_tree("bf16", "bf16", lengths, nodes.tolist(), heads, hk, 64, 16, seed=3, max_nodes=most,
+             max_keys=max_keys)
+
+
+def test_one_launch_and_several_give_the_same_bits():
+    """The trees of one launch, over and over: each as often as it comes, in whichever launch."""
+    n, times = 1024, 3
+    c = Cache("bf16", 400, 16, 1, 64, 1)
+    c.fill([(p, s) for p in range(400) for s in range(16)])
+    rng = np.random.default_rng(0)
+    table = ids(rng.integers(0, 400, (8, 200)))
+    lengths, seqs = rng.integers(0, 90, n), rng.integers(0, 8, n)
+    lengths[[3, 700]] = 3100, 2500
+    q = torch.randn(n, 2, 64, device="cuda:0").to(torch.bfloat16)
+    outs = []
+    for k in (1, times):
+        ws = torch.empty(api.paged_tree_attention_workspace_bytes(c.kv, n * k, 2, 3200, 1), dtype=torch.uint8,
+                         device="cuda:0")
+        out = torch.empty(n * k, 2, 64, device="cuda:0", dtype=torch.bfloat16)
+        api.paged_tree_attention(c.kv, q.repeat(k, 1, 1), table, ids(np.tile(lengths, k)), out, ws, 3200, 1,
+                                 seqs=ids(np.tile(seqs, k)))
+        outs.append(out.view(torch.int16).unflatten(0, (k, n)))
+    torch.cuda.synchronize()
+    assert outs[0].any() and bool((outs[1] == outs[0]).all())
