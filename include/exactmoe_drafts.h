@@ -13,7 +13,9 @@
  *                              positions that they then have, in all layers.
  * emoe_paged_fork begins sequences where others stand (beams, several answers to
  * one prompt).  Conventions of exactmoe_serving.h apply: no call allocates or
- * synchronizes, so each may be captured into a HIP graph.
+ * synchronizes, so each may be captured into a HIP graph.  emoe_decoder_forward_paged
+ * takes no trees: the append and the attention here are for a program that calls its
+ * layers itself.
  *
  * A tree of T nodes (0 .. 64) is given by what its nodes see: bit j of tree[i] is
  * set if node i sees node j, as a rule its ancestors and itself.  The depth of
@@ -90,7 +92,8 @@ typedef struct emoe_paged_tree_args {
                                  max_nodes at most 2^20 */
   int32_t n_seqs, table_width;
   int32_t max_keys;           /* bound of lengths[] and nodes together, 0 .. 2^30 */
-  int32_t max_nodes;          /* bound of a tree's nodes, 1 .. 64 */
+  int32_t max_nodes;          /* bound of a tree's nodes, 1 .. 64; the call is laid out for trees of
+                                 so many, so that a bound far above them costs time */
   int32_t window;             /* >= 0; 0: none */
 } emoe_paged_tree_args;
 
@@ -167,8 +170,9 @@ int32_t emoe_paged_compact(const emoe_paged_kv* kv, int32_t n_layers, const emoe
  *   children may.  A parent's page that is missing stays missing;
  *   all further entries are -1.
  * n is cut to the table.  A parent outside [0, n_seqs) or a negative length leaves
- * a row of -1.  new_table may not overlap page_table.  No fresh page comes twice,
- * nor may it hold anything of a parent's. */
+ * a row of -1.  new_table may not overlap page_table, from the first row's start to the
+ * last one's end: rows of one between rows of the other are refused too.  No fresh page
+ * comes twice, nor may it hold anything of a parent's. */
 typedef struct emoe_fork_args {
   const int32_t* page_table;  /* device [n_seqs][table_width] */
   const int32_t* parents;     /* device [forks] */

@@ -433,8 +433,8 @@ def paged_tree_attention(kv: PagedKV, q, page_table, lengths, out, workspace, ma
     [heads][dim]; lengths, seqs i32 [trees]; starts i32 [trees + 1], the trees' first rows (None:
     max_nodes rows each); tree i64 [rows], bit j: sees node j (None: chains); page_table i32
     [sequences][pages]; slopes f32 [heads]; lse f32 [rows][heads]; scale 1 / sqrt(dim) when None.
-    max_keys bounds lengths and nodes together.  workspace: paged_tree_attention_workspace_bytes,
-    of any content."""
+    max_keys bounds lengths and nodes together, max_nodes a tree's nodes (the nearer, the faster).
+    workspace: paged_tree_attention_workspace_bytes, of any content."""
     _check_cache(kv)
     if scale is None:
         scale = kv.view.head_dim ** -0.5

@@ -92,11 +92,12 @@ __device__ __forceinline__ int64_t slot_offset(const LayersArg& kv, const int32_
 }
 
 // A thread takes one piece of 16 bytes of a head, of keys or values of a layer, and
-// makes all of the tree's moves of it in turn, eight loads at a time.  The source
-// of a move lies behind the targets of the moves before it (path[i] > i), so what
-// is read has not been written by this call.
-// Bound by the chain lengths, path, page table, keys: 3.9 us for one tree, 11 for 61 trees
-// of 24 MB in 28 layers (2.2 TB/s; slots of 1 KB here and there in memory).
+// makes all of the tree's moves of it in turn, eight at a time: their loads, then their
+// stores.  The source of a move lies behind the targets of the moves before it (path[i] > i),
+// so what is read has not been written by this call.
+// The compiler keeps the eight pieces in scratch memory (144 bytes a thread) and waits for
+// each load before the next: 61 trees of 24 MB in 28 layers take 9.9 us, 2.5 TB/s.  Small calls
+// are bound by the chain lengths, path, page table, keys: 4.1 us for one tree in 16 layers.
 __global__ __launch_bounds__(kThreads) void compact_kernel(CompactArg a) {
   __shared__ int64_t from[64], to[64];
   __shared__ int moves;

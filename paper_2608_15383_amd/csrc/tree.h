@@ -40,9 +40,11 @@ void launch_tree_fp16(const TreeArg& a, const TreePlan& p, int head_dim, bool e4
 
 constexpr int kTreeWaves = 4;
 
-// Workgroups of paged_tree_wide_kernel on a CU, as far as registers and LDS allow without
-// scratch memory: 40 trees over 8 bits 173 us with two and 163 with three, 64 dimensions over
-// 16 bits 34.5 with three and 40.9 with four (16 trees of up to 8,192 keys).
+// Workgroups of paged_tree_wide_kernel on a CU.  128 dimensions over 8 bits: 40 trees 173 us with
+// two and 163 with three, which leave 168 registers and so 1 value in scratch memory, 14 with shaped
+// scores.  64 dimensions over 16 bits 34.5 with three and 40.9 with four (16 trees of up to 8,192
+// keys).  Of 256 dimensions two share the 512 registers, with 12 values in scratch memory under
+// shaped scores (fp16 over 16 bits 27, and 7 without); one alone has not been measured.
 constexpr int wide_workgroups(int head_dim, bool e4m3) {
   return head_dim == 64 || (head_dim == 128 && e4m3) ? 3 : 2;
 }
@@ -479,8 +481,10 @@ struct TreeChunk {
 // How the blocks of a launch are cut for the workers of a key head.  Either a block has
 // ceil(units / target) parts and every worker one, so that a worker never begins a
 // second block, which costs it as much as several units; or, where there are too few
-// workers for that, the units of all blocks stand behind each other and every worker
-// takes the same number of them.
+// workers for that, or more trees than the 64 that a wavefront holds a lane each, the units
+// of all blocks stand behind each other and every worker takes the same number of them.
+// Parts and equal runs: 64 trees of 2 key heads over up to 16,384 keys 71 and 89 us (8 nodes), 65
+// and 70 (2), 4 trees of 64 nodes over 8,192 83 and 103; 100 trees of 8 nodes take 125, in runs.
 struct TreeRun {
   int u, u_end, base;    // units: of the run, the first one of block cb of tree tr
   int tr, cb;

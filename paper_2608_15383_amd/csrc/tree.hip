@@ -14,6 +14,8 @@ constexpr int kUnits = 256;                // CUs
 //    of their own straight from memory to registers; more paged_tree_wide_kernel, whose
 //    wavefronts share them.  4 columns, 64 trees of 1,001 keys of 8 heads of 128 49.3 and
 //    53.3 us (both cut); 26 columns of 16 heads 17.6 and 13.1 us over 328 keys, 23.9 and 16.6 over 2,026.
+//    The bound of a tree's nodes decides, as it does on the number of blocks, since the host knows
+//    no other: those 64 rows take 46 us under a bound of 1 and 140 under 64, wide and whole.
 //  - An output, that is a block of columns of a tree and key head, has one workgroup where
 //    there are few keys; else its keys are cut over the workers of its key head (find_run)
 //    and tree_join_kernel joins the parts in a launch of its own.

@@ -444,11 +444,11 @@ struct WideSegment {
 // Columns of 128, 32 to a wavefront, need half the reads of LDS, but twice the registers:
 // 64 nodes x 4 trees of 8,192 keys 83 us where this takes 82, 40 trees over 8 bits 173 and 160.
 //
-// 131,072 keys of 8 heads of 128 take 97 us, 5.5 TB/s, bound by HBM (122 us without the
+// 131,072 keys of 8 heads of 128 take 98 us, 5.5 TB/s, bound by HBM (122 us without the
 // copies' nt where it made 104).  Ragged trees of many nodes are bound by the
 // SIMDs' issue: a key and column cost two products of values (the weight's two halves), an
-// exponential and, over 8 bits, the conversions of both tiles; 40 trees over 8 bits reach
-// 312 TFLOP/s and 2.8 TB/s, 64 nodes x 4 trees 417 TFLOP/s.
+// exponential and, over 8 bits, the conversions of both tiles; 40 trees over 8 bits reach, by
+// their lengths, 240 to 300 TFLOP/s and 2.3 to 2.6 TB/s, 64 nodes x 4 trees 413 TFLOP/s.
 template <class T, bool kE4M3, int kDh, bool kShaped>
 __global__ __launch_bounds__(64 * kTreeWaves, wide_workgroups(kDh, kE4M3)) void paged_tree_wide_kernel(TreeArg a) {
   typedef WideSegment<T, kE4M3, kDh, kShaped> Segment;
