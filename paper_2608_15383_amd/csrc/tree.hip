@@ -32,7 +32,7 @@ constexpr int kUnits = 256;                // CUs
 //    wide) 1,000 42 and 46, 2,000 72 and 68, 3,000 101 and 94, 16,384 523 and 387; one of 131,072
 //    keys among short ones 3,590 and 192, of one node 1,448 and 138.  400 trees of 2,000 keys 260
 //    and 290, 4,096 468 and 472, 16,384 1,619 and 1,473.  Trees of equal lengths lose about 1%
-//    (128 of 8,000 keys 702 and 706 us) or win what the last round of whole ones leaves idle (130 of
+//    (128 of 8,000 keys 702 and 706 us) or win what the last turn of whole ones leaves idle (130 of
 //    8,000 883 and 755).  Against the rule are shaped scores of up to 2,000 keys (300 trees of 4
 //    key heads of 64 269 and 163), and thousands of trees of one key head, whose lengths every
 //    worker looks through (3,000 of up to 6,000 keys 487 and 548).  With key heads so many that
